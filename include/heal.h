@@ -318,6 +318,160 @@ heal_status_t heal_scores_i16(int64_t M, int64_t N, int64_t K, const int16_t *Q,
                               int64_t strideK, const float *maxK, float alpha, float *S,
                               int64_t lds, int64_t strideS, int64_t batch, hipStream_t stream);
 
+/* ==========================================================================
+ * Key/value cache: appending with the rotation, attention, and the choice of
+ * the blocks that a query reads.
+ *
+ * The cache keeps the keys and values of many sequences in blocks of `block`
+ * tokens.  A complete block is held as INT8 codes with one scale for its keys and
+ * one for its values per head, as heal_quantize_i16 makes codes:
+ *     m = max|x| over the block's rows of that head,
+ *     code = Round(127 x / m), ties to even, decided exactly (m = 0: zeros),
+ *     x ~ code * m / 127.
+ * The rows of a sequence's last two blocks are also kept as they came, in FP32, in
+ * a ring of 2 * block rows per sequence (its slot) and head.  A block that is not
+ * complete is read from the ring; when its last token arrives it is quantised from
+ * the ring's rows, once.  The cache therefore does not depend on how tokens were cut
+ * into calls, and a sequence may be cut back (drafted tokens that were refused) as
+ * far as the beginning of the block before its last one, by passing a smaller length.
+ *
+ * Arrays (device, 16-byte aligned, owned by the caller, dense):
+ *   k_codes  [blocks][heads][block][dim]
+ *   v_codes  [blocks][heads][dim][block]; token 16 s + 4 g + i of a block (i, g < 4)
+ *            is at place g * block / 4 + 4 s + i, the order in which a lane of a
+ *            matrix instruction takes them
+ *   scales   [blocks][heads][2]         m of the keys, m of the values; for a block that is
+ *                                       not complete, of the rows it has
+ *   k_mean   [blocks][heads][dim]       mean of the block's (rotated) keys, FP64 sum
+ *   k_recent [slots][heads][2 * block][dim]    row of the token at place p: p % (2 * block)
+ *   v_recent [slots][heads][dim][2 * block]
+ * Nothing needs to be cleared before use.  A block holds one sequence's tokens for
+ * heal_kv_append; sequences may share complete blocks that they only read.
+ *
+ * Sequences: sequence i owns the tokens cu[i] .. cu[i + 1] - 1 of a call's token
+ * arrays, the last of its lens[i] tokens: token j of its n is at place
+ * lens[i] - n + j.  Block b of the sequence is cache block table[i * table_ld + b].
+ * These arrays are read on the device: a call does not wait for them and can be
+ * captured; so what they hold is not refused but bounded:
+ *   - table entries outside [0, blocks) and places past table_cols blocks hold no
+ *     tokens: nothing is written for them, attention does not see them;
+ *   - slots outside [0, slots): the FP32 rows are neither written nor seen;
+ *   - places below 0 (lens[i] < n) are not stored; their queries see nothing;
+ *   - cu is taken to ascend within [0, tokens]; tokens of no sequence are left alone,
+ *     and so are their outputs.
+ * ========================================================================== */
+
+typedef struct heal_kv_cache_t {
+    int64_t blocks, slots;  /* 1 .. 2^31 - 1 */
+    int64_t heads;          /* key/value heads, 1 .. 1024 */
+    int64_t dim;            /* 64, 96 or 128 */
+    int64_t block;          /* tokens of a block: 16, 32, 64 or 128 */
+    int8_t *k_codes, *v_codes;
+    float *scales, *k_mean, *k_recent, *v_recent;
+} heal_kv_cache_t;
+
+typedef struct heal_kv_batch_t {
+    int64_t seqs;           /* 0 .. 2^24 */
+    int64_t tokens;         /* 0 .. 2^30: rows of the token arrays */
+    const int32_t *cu;      /* [seqs + 1], or NULL: one token each (tokens == seqs) */
+    const int32_t *lens;    /* [seqs]: lengths with the call's tokens */
+    const int32_t *table;   /* [seqs][table_cols], row stride table_ld */
+    int64_t table_ld, table_cols;   /* table_cols * block < 2^31 */
+    const int32_t *slots;   /* [seqs], or NULL: sequence i has slot i */
+} heal_kv_batch_t;
+
+/*
+ * heal_kv_append -- the tokens' keys and values enter the cache (and their queries
+ * are rotated).
+ *   k, v    : [tokens][heads][dim] FP32, strides of tokens and heads in elements,
+ *             the last dimension dense; K and V may have strides of their own;
+ *   cos, sin: [places][rot / 2] FP32, dense, or NULL with rot == 0: the first rot
+ *             (even, <= dim) elements of a key at place p are rotated,
+ *                 a' = a cos - b sin,  b' = b cos + a sin,
+ *             the pairs (a, b) being elements j and j + rot / 2, or 2 j and 2 j + 1
+ *             with interleaved = 1.  Products and sum are formed in FP64 (exactly, and
+ *             with one rounding) and rounded to FP32.  A token whose place is not
+ *             below `places` is taken as it is, without rotation;
+ *   q, q_out: [tokens][heads_q][dim] or both NULL: queries rotated likewise; q_out
+ *             may be q itself with the same strides, and must not overlap it otherwise.
+ * Values are not rotated.  Rows must be finite for their block's codes to mean
+ * anything.
+ */
+heal_status_t heal_kv_append(const heal_kv_cache_t *cache, const heal_kv_batch_t *batch,
+                             const float *k, int64_t k_token, int64_t k_head,
+                             const float *v, int64_t v_token, int64_t v_head,
+                             const float *cos, const float *sin, int64_t places, int64_t rot,
+                             int interleaved,
+                             const float *q, int64_t q_token, int64_t q_head, int64_t heads_q,
+                             float *q_out, int64_t qo_token, int64_t qo_head, hipStream_t stream);
+
+/*
+ * heal_kv_read -- the cache's keys and values of the batch's tokens, back as FP32
+ * rows: code * m / 127 (one FP32 product of the code and m / 127), or the FP32 rows
+ * of a block that is not complete.  Tokens may be any number of a sequence's last
+ * ones.  Rows that the cache does not hold are written as zeros.
+ *   k, v : [tokens][heads][dim] FP32, dense; either may be NULL.
+ */
+heal_status_t heal_kv_read(const heal_kv_cache_t *cache, const heal_kv_batch_t *batch,
+                           float *k, float *v, hipStream_t stream);
+
+/*
+ * heal_kv_select -- for each token and key/value head the blocks worth reading:
+ * the first keep_first and the last keep_last blocks up to the token's own, and of
+ * the others those that score highest,
+ *     score(b) = max over the head's queries of  sum_d q_d k_mean[b]_d   (FP64),
+ * equal scores by the lower block; a score that is no number, or that belongs to a
+ * block that the cache does not hold, is -infinity.
+ *   q   : [tokens][heads_q][dim], heads_q a multiple of heads: head h has the queries
+ *         h * heads_q / heads and on;
+ *   sel : [tokens][heads][n_sel] int32, dense: block numbers of the sequence,
+ *         ascending, -1 behind the last one;
+ *   n_sel >= keep_first + keep_last, keep_first >= 0, keep_last >= 1,
+ *   table_cols <= 16384.
+ */
+heal_status_t heal_kv_select(const heal_kv_cache_t *cache, const heal_kv_batch_t *batch,
+                             const float *q, int64_t q_token, int64_t q_head, int64_t heads_q,
+                             int64_t n_sel, int64_t keep_first, int64_t keep_last,
+                             int32_t *sel, hipStream_t stream);
+
+/*
+ * heal_kv_attention -- attention of the tokens' queries over the cache:
+ *     s_t = scale * q . k_t,  o = sum_t softmax(s)_t v_t,  lse = ln sum_t exp(s_t)
+ * over the tokens t of the sequence with t <= place (causal = 1; all of them with
+ * causal = 0) and, with window > 0, t > place - window.  A row that sees nothing
+ * gives o = 0 and lse = -infinity.  Codes are exact in FP16; queries and softmax
+ * weights go to the matrix units as FP16 pairs (head and residual, scaled by powers
+ * of two, off by at most 2^-22 of the value), FP32 rows of the cache likewise, all
+ * sums in FP32: the output has FP32's accuracy, not FP16's.
+ *   sel  : NULL, or [tokens][heads][n_sel] int32, dense: only these blocks of the
+ *          sequence are read for a token and head (a block listed twice counts
+ *          twice; numbers outside the table hold nothing);
+ *   out  : [tokens][heads_q][dim], written; must not overlap q;
+ *   lse  : [tokens][heads_q] dense, or NULL;
+ *   chunk: 0, or a multiple of 64: each row's tokens are summed in chunks of so many
+ *          from the first one it can see, joined in ascending order.  0 chooses by the
+ *          call's sizes, so that a row's bits may depend on the batch it is in; with a
+ *          chunk of the caller's they depend on the row's own data only (in calls of
+ *          one token per sequence, with cu NULL, or with sel).  Results are bitwise
+ *          the same from run to run either way;
+ *   workspace: heal_kv_attention_workspace bytes of device memory for the chunks'
+ *          results, 16-byte aligned (NULL where that is 0).  It holds nothing between
+ *          calls; calls that may run at the same time need one each.
+ */
+heal_status_t heal_kv_attention(const heal_kv_cache_t *cache, const heal_kv_batch_t *batch,
+                                const float *q, int64_t q_token, int64_t q_head, int64_t heads_q,
+                                float scale, int causal, int64_t window,
+                                const int32_t *sel, int64_t n_sel,
+                                float *out, int64_t out_token, int64_t out_head, float *lse,
+                                int64_t chunk, void *workspace, int64_t workspace_bytes,
+                                hipStream_t stream);
+
+/* Bytes of workspace that heal_kv_attention needs for these arguments (which it reads
+ * sizes of only: cache, batch, whether cu is NULL), or -1 where it would refuse them
+ * (no HIP call). */
+int64_t heal_kv_attention_workspace(const heal_kv_cache_t *cache, const heal_kv_batch_t *batch,
+                                    int64_t heads_q, int64_t window, int64_t n_sel, int64_t chunk);
+
 #ifdef __cplusplus
 }
 #endif

@@ -20,6 +20,11 @@ Functions (names follow the C ABI):
   heal_gemm_f32_presplit(A, Bp, N)    -> bitwise equal to heal_gemm_f32(A, B)
   heal_quantize_i16(x)                -> (codes int16, max|x| 1-element tensor)
   heal_scores_i16(Q, Kt, maxQ, maxK, alpha)  -> dual-FP16 scores of INT16 codes, FP32
+  KVCache(...), KVCache.empty(...)    -> the arrays of a key/value cache (INT8 blocks)
+  heal_kv_append(cache, k, v, table, lens, ...)  -> tokens enter the cache; rotated queries
+  heal_kv_read(cache, tokens, table, lens, ...)  -> (k, v) rows of the cache as FP32
+  heal_kv_select(cache, q, n_sel, table, lens, ...)  -> the blocks that each token should read
+  heal_kv_attention(cache, q, table, lens, ...)  -> attention over the cache, FP32
   lib()                               -> the raw ctypes library
   build_id(), check_build()           -> the library's source hash; refuse a stale binary
 """
@@ -31,7 +36,8 @@ __all__ = ["HealError", "lib", "library_path", "build_id", "check_build", "heal_
            "INSTANCE_AUTO", "INSTANCE_LARGE", "INSTANCE_MEDIUM", "INSTANCE_SKINNY", "STATUS",
            "heal_split_f16", "heal_packed_size", "heal_maxabs_f32", "heal_f16_weight_exponent",
            "heal_pack_f16_weight", "heal_gemm_f16w", "heal_presplit_b", "heal_gemm_f32_presplit",
-           "heal_quantize_i16", "heal_scores_i16"]
+           "heal_quantize_i16", "heal_scores_i16", "KVCache", "heal_kv_append", "heal_kv_read",
+           "heal_kv_select", "heal_kv_attention"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 library_path = os.path.join(_HERE, "libheal.so")
@@ -110,6 +116,18 @@ def lib():
     L.heal_scores_i16.argtypes = [_i64, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _vp,
                                   ctypes.c_float, _vp, _i64, _i64, _i64, _vp]
     L.heal_scores_i16.restype = _c
+    L.heal_kv_append.argtypes = [_vp, _vp] + [_vp, _i64, _i64] * 2 + [_vp, _vp, _i64, _i64, _c] + [
+        _vp, _i64, _i64, _i64, _vp, _i64, _i64, _vp]
+    L.heal_kv_append.restype = _c
+    L.heal_kv_read.argtypes = [_vp, _vp, _vp, _vp, _vp]
+    L.heal_kv_read.restype = _c
+    L.heal_kv_select.argtypes = [_vp, _vp, _vp] + [_i64] * 6 + [_vp, _vp]
+    L.heal_kv_select.restype = _c
+    L.heal_kv_attention.argtypes = [_vp, _vp, _vp, _i64, _i64, _i64, ctypes.c_float, _c, _i64, _vp, _i64,
+                                    _vp, _i64, _i64, _vp, _i64, _vp, _i64, _vp]
+    L.heal_kv_attention.restype = _c
+    L.heal_kv_attention_workspace.argtypes = [_vp, _vp, _i64, _i64, _i64, _i64]
+    L.heal_kv_attention_workspace.restype = _i64
     _lib = L
     return L
 
@@ -393,3 +411,255 @@ def heal_scores_i16(Q, Kt, maxQ, maxK, alpha=1.0, out=None):
         maxK.data_ptr(), ctypes.c_float(alpha), S.data_ptr(), _ld(shape_s, stride_s), stride_s[0] if many else 0,
         bat, _stream()), "heal_scores_i16")
     return S[0] if squeeze else S
+
+
+# ---- key/value cache ---------------------------------------------------------
+
+class _CCache(ctypes.Structure):
+    _fields_ = [(n, _i64) for n in ("blocks", "slots", "heads", "dim", "block")] + [
+        (n, _vp) for n in ("k_codes", "v_codes", "scales", "k_mean", "k_recent", "v_recent")]
+
+
+class _CBatch(ctypes.Structure):
+    _fields_ = [("seqs", _i64), ("tokens", _i64), ("cu", _vp), ("lens", _vp), ("table", _vp),
+                ("table_ld", _i64), ("table_cols", _i64), ("slots", _vp)]
+
+
+class KVCache:
+    """The arrays of a key/value cache (``include/heal.h`` has their layouts):
+
+      k_codes  int8    (blocks, heads, block, dim)
+      v_codes  int8    (blocks, heads, dim, block)
+      scales   float32 (blocks, heads, 2)
+      k_mean   float32 (blocks, heads, dim)
+      k_recent float32 (slots, heads, 2 * block, dim)
+      v_recent float32 (slots, heads, dim, 2 * block)
+
+    dim is 64, 96 or 128, block 16, 32, 64 or 128 tokens.  The arrays are the
+    caller's: contiguous CUDA tensors of one device, kept as attributes.
+    """
+
+    def __init__(self, k_codes, v_codes, scales, k_mean, k_recent, v_recent):
+        shape, _ = _tensor(k_codes, "k_codes", torch.int8, 4)
+        blocks, heads, block, dim = shape
+        _tensor(k_recent, "k_recent", torch.float32, 4)
+        slots = k_recent.shape[0]
+        arrays = {"k_codes": k_codes, "v_codes": v_codes, "scales": scales, "k_mean": k_mean,
+                  "k_recent": k_recent, "v_recent": v_recent}
+        shapes = {"k_codes": (blocks, heads, block, dim), "v_codes": (blocks, heads, dim, block),
+                  "scales": (blocks, heads, 2), "k_mean": (blocks, heads, dim),
+                  "k_recent": (slots, heads, 2 * block, dim), "v_recent": (slots, heads, dim, 2 * block)}
+        for name, t in arrays.items():
+            want = shapes[name]
+            _tensor(t, name, torch.int8 if name.endswith("codes") else torch.float32, len(want))
+            if tuple(t.shape) != want:
+                raise HealError("%s has shape %s, expected %s" % (name, tuple(t.shape), want))
+            if not t.is_contiguous() or t.data_ptr() % 16:
+                raise HealError("%s must be contiguous and 16-byte aligned" % name)
+            if t.device != k_codes.device:
+                raise HealError("%s is on %s, k_codes on %s" % (name, t.device, k_codes.device))
+        if dim not in (64, 96, 128) or block not in (16, 32, 64, 128) or not (blocks and slots and heads):
+            raise HealError("no cache of %d blocks, %d slots, %d heads, dim %d, block %d"
+                            % (blocks, slots, heads, dim, block))
+        self.__dict__.update(arrays)
+        self.blocks, self.slots, self.heads, self.dim, self.block = blocks, slots, heads, dim, block
+        self.device = k_codes.device
+        self._index = k_codes.get_device()
+        self._c = _CCache(blocks, slots, heads, dim, block, *(t.data_ptr() for t in arrays.values()))
+        self._ref = ctypes.byref(self._c)
+
+    @classmethod
+    def empty(cls, blocks, slots, heads, dim, block=64, device="cuda"):
+        """A cache of its own, not cleared (nothing of it is read before it is written)."""
+        def f(*shape):
+            return torch.empty(shape, dtype=torch.float32, device=device)
+
+        def i(*shape):
+            return torch.empty(shape, dtype=torch.int8, device=device)
+        return cls(i(blocks, heads, block, dim), i(blocks, heads, dim, block), f(blocks, heads, 2),
+                   f(blocks, heads, dim), f(slots, heads, 2 * block, dim), f(slots, heads, dim, 2 * block))
+
+
+def _kv_on(cache, t, name):
+    if t.get_device() != cache._index:
+        raise HealError("%s is on %s, the cache on %s" % (name, t.device, cache.device))
+
+
+def _kv_ints(cache, t, name, ndim, size=None):
+    shape, stride = _tensor(t, name, torch.int32, ndim)
+    _kv_on(cache, t, name)
+    if size is not None and shape[0] != size:
+        raise HealError("%s has %d entries, expected %d" % (name, shape[0], size))
+    return shape, stride
+
+
+def _kv_rows(cache, t, name, tokens=None, heads=None):
+    """A (tokens, heads, dim) float32 tensor; returns shape, token and head strides."""
+    shape, stride = _tensor(t, name, torch.float32, 3)
+    _kv_on(cache, t, name)
+    if shape[2] != cache.dim or (tokens is not None and shape[0] != tokens) or (
+            heads is not None and shape[1] != heads):
+        raise HealError("%s has shape %s, expected (%s, %s, %d)"
+                        % (name, tuple(shape), "tokens" if tokens is None else tokens,
+                           "heads" if heads is None else heads, cache.dim))
+    return shape, stride[0], stride[1]
+
+
+def _kv_batch(cache, tokens, table, lens, cu, slots):
+    if not isinstance(cache, KVCache):
+        raise HealError("cache must be a KVCache")
+    if _device() != cache._index:
+        raise HealError("the cache is on %s, the current device is another" % cache.device)
+    shape, stride = _kv_ints(cache, table, "table", 2)
+    seqs = shape[0]
+    _kv_ints(cache, lens, "lens", 1, seqs)
+    if cu is not None:
+        _kv_ints(cache, cu, "cu", 1, seqs + 1)
+    elif tokens != seqs:
+        raise HealError("%d tokens of %d sequences need cu" % (tokens, seqs))
+    if slots is not None:
+        _kv_ints(cache, slots, "slots", 1, seqs)
+    elif seqs > cache.slots:
+        raise HealError("%d sequences, the cache has %d slots" % (seqs, cache.slots))
+    return _CBatch(seqs, tokens, cu.data_ptr() if cu is not None else None, lens.data_ptr(),
+                   table.data_ptr(), _ld(shape, stride), shape[1],
+                   slots.data_ptr() if slots is not None else None)
+
+
+def _device():
+    """The current device's number.  (The first call replaces itself.)"""
+    global _device
+    _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _device()
+
+
+def _kv_group(cache, heads_q):
+    if heads_q < 1 or heads_q % cache.heads:
+        raise HealError("%d query heads for %d key/value heads" % (heads_q, cache.heads))
+
+
+def heal_kv_append(cache, k, v, table, lens, cu=None, slots=None, cos=None, sin=None,
+                   interleaved=False, q=None, q_out=None):
+    """The tokens' keys (rotated by their places) and values enter the cache.
+
+    k, v: (tokens, heads, dim) float32; table (sequences, columns), lens and slots
+    (sequences), cu (sequences + 1): int32.  lens counts the new tokens.  cos, sin:
+    (places, rot / 2) float32 or None.  With q (tokens, any heads, dim) the queries
+    are rotated too, into q_out (which may be q) or a new tensor, and returned.
+    """
+    if not isinstance(cache, KVCache):
+        raise HealError("cache must be a KVCache")
+    shape, k_token, k_head = _kv_rows(cache, k, "k", None, cache.heads)
+    tokens = shape[0]
+    _, v_token, v_head = _kv_rows(cache, v, "v", tokens, cache.heads)
+    batch = _kv_batch(cache, tokens, table, lens, cu, slots)
+    places = rot = 0
+    if (cos is None) != (sin is None):
+        raise HealError("cos and sin come together")
+    if cos is not None:
+        for t, name in ((cos, "cos"), (sin, "sin")):
+            _tensor(t, name, torch.float32, 2)
+            _kv_on(cache, t, name)
+            if not t.is_contiguous() or t.shape != cos.shape:
+                raise HealError("cos and sin must be contiguous and of one shape")
+        places, rot = cos.shape[0], 2 * cos.shape[1]
+    heads_q = q_token = q_head = qo_token = qo_head = 0
+    if q is not None:
+        shape, q_token, q_head = _kv_rows(cache, q, "q", tokens)
+        heads_q = shape[1]
+        if q_out is None:
+            q_out = torch.empty(tuple(shape), dtype=torch.float32, device=q.device)
+        _, qo_token, qo_head = _kv_rows(cache, q_out, "q_out", tokens, heads_q)
+    elif q_out is not None:
+        raise HealError("q_out without q")
+    with_q = q is not None and q.numel() > 0
+    _check((_lib or lib()).heal_kv_append(
+        cache._ref, ctypes.byref(batch), k.data_ptr(), k_token, k_head, v.data_ptr(), v_token, v_head,
+        cos.data_ptr() if rot else None, sin.data_ptr() if rot else None, places, rot,
+        1 if interleaved else 0, q.data_ptr() if with_q else None, q_token, q_head, heads_q,
+        q_out.data_ptr() if with_q else None, qo_token, qo_head, _stream()), "heal_kv_append")
+    return q_out
+
+
+def heal_kv_read(cache, tokens, table, lens, cu=None, slots=None):
+    """(k, v), each (tokens, heads, dim) float32: what the cache holds of each
+    sequence's last tokens (cu says how many).  Rows it does not hold are zeros;
+    rows of no sequence are not written."""
+    batch = _kv_batch(cache, tokens, table, lens, cu, slots)
+    k = torch.empty((tokens, cache.heads, cache.dim), dtype=torch.float32, device=cache.device)
+    v = torch.empty((tokens, cache.heads, cache.dim), dtype=torch.float32, device=cache.device)
+    _check((_lib or lib()).heal_kv_read(cache._ref, ctypes.byref(batch), k.data_ptr(), v.data_ptr(),
+                                        _stream()), "heal_kv_read")
+    return k, v
+
+
+def heal_kv_select(cache, q, n_sel, table, lens, cu=None, slots=None, keep_first=1, keep_last=1, out=None):
+    """(tokens, heads, n_sel) int32: for each token and key/value head the first
+    keep_first and last keep_last blocks and the others that score highest,
+    ascending, -1 behind the last.  (slots is not needed; it is checked if given.)"""
+    if not isinstance(cache, KVCache):
+        raise HealError("cache must be a KVCache")
+    shape, q_token, q_head = _kv_rows(cache, q, "q")
+    tokens, heads_q = shape[0], shape[1]
+    _kv_group(cache, heads_q)
+    batch = _kv_batch(cache, tokens, table, lens, cu, slots)
+    if n_sel < 1:
+        raise HealError("n_sel must be positive, got %d" % n_sel)
+    if out is None:
+        out = torch.empty((tokens, cache.heads, n_sel), dtype=torch.int32, device=q.device)
+    else:
+        _kv_sel(cache, out, "out", tokens, n_sel)
+    _check((_lib or lib()).heal_kv_select(cache._ref, ctypes.byref(batch), q.data_ptr(), q_token, q_head,
+                                          heads_q, n_sel, keep_first, keep_last, out.data_ptr(), _stream()),
+           "heal_kv_select")
+    return out
+
+
+def _kv_sel(cache, t, name, tokens, n_sel=None):
+    shape, _ = _tensor(t, name, torch.int32, 3)
+    _kv_on(cache, t, name)
+    if shape[0] != tokens or shape[1] != cache.heads or shape[2] < 1 or (n_sel and shape[2] != n_sel):
+        raise HealError("%s has shape %s, expected (%d, %d, %s)"
+                        % (name, tuple(shape), tokens, cache.heads, n_sel or "n_sel"))
+    if not t.is_contiguous():
+        raise HealError("%s must be contiguous" % name)
+    return shape[2]
+
+
+def heal_kv_attention(cache, q, table, lens, cu=None, slots=None, scale=None, causal=True, window=0,
+                      sel=None, out=None, lse=None, chunk=0):
+    """Attention of q (tokens, heads_q, dim) float32 over the cache; returns out.
+
+    scale: dim ** -0.5 by default; window: 0, or how many tokens back a token sees;
+    sel: int32 (tokens, heads, n) of ``heal_kv_select``, or None for all blocks;
+    lse: a contiguous float32 (tokens, heads_q) that is written too; chunk: 0, or
+    tokens summed at a time (a multiple of 64), for bits that do not depend on the
+    batch.
+    """
+    if not isinstance(cache, KVCache):
+        raise HealError("cache must be a KVCache")
+    shape, q_token, q_head = _kv_rows(cache, q, "q")
+    tokens, heads_q = shape[0], shape[1]
+    _kv_group(cache, heads_q)
+    batch = _kv_batch(cache, tokens, table, lens, cu, slots)
+    n_sel = _kv_sel(cache, sel, "sel", tokens) if sel is not None else 0
+    if out is None:
+        out = torch.empty(tuple(shape), dtype=torch.float32, device=q.device)
+    _, out_token, out_head = _kv_rows(cache, out, "out", tokens, heads_q)
+    if lse is not None:
+        _tensor(lse, "lse", torch.float32, 2)
+        _kv_on(cache, lse, "lse")
+        if tuple(lse.shape) != (tokens, heads_q) or not lse.is_contiguous():
+            raise HealError("lse must be a contiguous (%d, %d) tensor" % (tokens, heads_q))
+    scale = cache.dim ** -0.5 if scale is None else scale
+    if tokens == 0:
+        return out
+    L, ref = _lib or lib(), ctypes.byref(batch)
+    size = L.heal_kv_attention_workspace(cache._ref, ref, heads_q, window, n_sel, chunk)
+    space = torch.empty(size, dtype=torch.uint8, device=q.device) if size > 0 else None
+    _check(L.heal_kv_attention(
+        cache._ref, ref, q.data_ptr(), q_token, q_head, heads_q, ctypes.c_float(scale), 1 if causal else 0,
+        window, sel.data_ptr() if n_sel else None, n_sel, out.data_ptr(), out_token, out_head,
+        lse.data_ptr() if lse is not None else None, chunk, space.data_ptr() if size > 0 else None,
+        max(size, 0), _stream()), "heal_kv_attention")
+    return out

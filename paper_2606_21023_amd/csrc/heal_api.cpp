@@ -8,6 +8,7 @@
 
 #include "heal.h"
 #include "heal_internal.h"
+#include "heal_kv.h"
 
 namespace {
 
@@ -173,6 +174,84 @@ heal_status_t run_packed(int op, int instance, int64_t M, int64_t N, int64_t K, 
         a.C = C + m0 * ldc + n0;
         return heal::launch_gemm_op(op, instance, a, stream);
     });
+}
+
+// ---- key/value cache ---------------------------------------------------------
+
+constexpr int64_t kMaxStride = (int64_t)1 << 40;
+constexpr int64_t kMaxSeqs = (int64_t)1 << 24, kMaxTokens = (int64_t)1 << 30, kMaxHeads = 1024;
+
+bool kv_stride(int64_t s) { return s >= 0 && s <= kMaxStride; }
+
+// tokens x heads rows of dim elements at these strides that do not overlap.
+bool kv_apart(int64_t tokens, int64_t heads, int64_t dim, int64_t token, int64_t head)
+{
+    if (!kv_stride(token) || !kv_stride(head)) return false;
+    if ((tokens > 1 && token < dim) || (heads > 1 && head < dim)) return false;
+    if (tokens <= 1 || heads <= 1) return true;
+    return token >= (heads - 1) * head + dim || head >= (tokens - 1) * token + dim;
+}
+
+bool kv_cache_sizes(const heal_kv_cache_t *c)
+{
+    const int64_t lim = ((int64_t)1 << 31) - 1;
+    return c && c->blocks >= 1 && c->blocks <= lim && c->slots >= 1 && c->slots <= lim && c->heads >= 1 &&
+           c->heads <= kMaxHeads && (c->dim == 64 || c->dim == 96 || c->dim == 128) &&
+           (c->block == 16 || c->block == 32 || c->block == 64 || c->block == 128);
+}
+
+bool kv_batch_sizes(const heal_kv_cache_t *c, const heal_kv_batch_t *b)
+{
+    return b && b->seqs >= 0 && b->seqs <= kMaxSeqs && b->tokens >= 0 && b->tokens <= kMaxTokens &&
+           (b->cu || b->tokens == b->seqs) && b->table_cols >= 0 && b->table_cols < ((int64_t)1 << 31) / c->block &&
+           b->table_ld >= (b->table_cols > 1 ? b->table_cols : 1) && b->table_ld <= kMaxStride;
+}
+
+bool kv_group(const heal_kv_cache_t *c, int64_t heads_q)
+{
+    return heads_q >= 1 && heads_q % c->heads == 0 && heads_q / c->heads <= kMaxHeads;
+}
+
+// Checks cache and batch and lays them out for the kernels; true in *nothing where
+// the call has no token of any sequence.
+heal_status_t kv_views(const heal_kv_cache_t *c, const heal_kv_batch_t *b, heal::KvCache *kc, heal::KvSeqs *ks,
+                       bool *nothing)
+{
+    if (!kv_cache_sizes(c) || !kv_batch_sizes(c, b)) return HEAL_ERR_INVALID_VALUE;
+    *nothing = b->seqs == 0 || b->tokens == 0;
+    if (*nothing) return HEAL_OK;
+    for (const void *p : {(const void *)c->k_codes, (const void *)c->v_codes, (const void *)c->scales,
+                          (const void *)c->k_mean, (const void *)c->k_recent, (const void *)c->v_recent})
+        if (!p || !aligned16(p)) return HEAL_ERR_INVALID_VALUE;
+    if (!b->lens || !aligned4(b->lens) || !aligned4(b->cu) || !aligned4(b->slots) || !aligned4(b->table) ||
+        (b->table_cols > 0 && !b->table))
+        return HEAL_ERR_INVALID_VALUE;
+    *kc = heal::KvCache{(int32_t)c->heads, (int32_t)c->dim, (int32_t)c->block, c->k_codes, c->v_codes,
+                        c->scales,         c->k_mean,       c->k_recent,       c->v_recent};
+    *ks = heal::KvSeqs{b->cu,
+                       b->lens,
+                       b->table,
+                       b->slots,
+                       b->table_ld,
+                       (int32_t)b->seqs,
+                       (int32_t)b->tokens,
+                       (int32_t)b->table_cols,
+                       (int32_t)c->blocks,
+                       (int32_t)c->slots};
+    return HEAL_OK;
+}
+
+bool kv_attention_sizes(const heal_kv_cache_t *c, const heal_kv_batch_t *b, int64_t heads_q, int64_t window,
+                        int64_t n_sel, int64_t chunk, heal::KvPlan *plan)
+{
+    const int64_t lim = ((int64_t)1 << 31) - 1;
+    if (!kv_cache_sizes(c) || !kv_batch_sizes(c, b) || !kv_group(c, heads_q)) return false;
+    if (window < 0 || window > lim || n_sel < 0 || n_sel * c->block > lim || chunk < 0 || chunk % 64 != 0 ||
+        chunk > lim)
+        return false;
+    *plan = heal::kv_plan(b->tokens, b->seqs, b->cu != nullptr, (int)c->heads, (int)(heads_q / c->heads),
+                          (int)c->dim, (int)c->block, b->table_cols, window, n_sel, chunk);
+    return plan->bytes >= 0;
 }
 
 }  // namespace
@@ -440,6 +519,148 @@ heal_status_t heal_scores_i16(int64_t M, int64_t N, int64_t K, const int16_t *Q,
         a.C = S + b0 * strideS + m0 * lds + n0;
         return heal::launch_gemm_op(heal::OP_SCORES, HEAL_INSTANCE_AUTO, a, stream);
     });
+}
+
+// ---- key/value cache ---------------------------------------------------------
+
+heal_status_t heal_kv_append(const heal_kv_cache_t *cache, const heal_kv_batch_t *batch, const float *k,
+                             int64_t k_token, int64_t k_head, const float *v, int64_t v_token,
+                             int64_t v_head, const float *cos, const float *sin, int64_t places,
+                             int64_t rot, int interleaved, const float *q, int64_t q_token,
+                             int64_t q_head, int64_t heads_q, float *q_out, int64_t qo_token,
+                             int64_t qo_head, hipStream_t stream)
+{
+    heal::KvAppendArgs a = {};
+    bool nothing = false;
+    heal_status_t st = kv_views(cache, batch, &a.c, &a.b, &nothing);
+    if (st != HEAL_OK) return st;
+    if (!kv_stride(k_token) || !kv_stride(k_head) || !kv_stride(v_token) || !kv_stride(v_head))
+        return HEAL_ERR_INVALID_VALUE;
+    if (rot < 0 || rot > cache->dim || rot % 2 != 0 || (interleaved != 0 && interleaved != 1) || places < 0 ||
+        places > ((int64_t)1 << 31))
+        return HEAL_ERR_INVALID_VALUE;
+    if ((q == nullptr) != (q_out == nullptr)) return HEAL_ERR_INVALID_VALUE;
+    if (q && (heads_q < 1 || heads_q > kMaxHeads * kMaxHeads || !aligned4(q) || !aligned4(q_out) ||
+              !kv_stride(q_token) || !kv_stride(q_head) ||
+              !kv_apart(batch->tokens, heads_q, cache->dim, qo_token, qo_head)))
+        return HEAL_ERR_INVALID_VALUE;
+    if (q && q == q_out && (q_token != qo_token || q_head != qo_head)) return HEAL_ERR_INVALID_VALUE;
+    if (nothing) return HEAL_OK;
+    if (!k || !v || !aligned4(k) || !aligned4(v)) return HEAL_ERR_INVALID_VALUE;
+    if (rot > 0 && places > 0 && (!cos || !sin || !aligned4(cos) || !aligned4(sin))) return HEAL_ERR_INVALID_VALUE;
+    st = check_device();
+    if (st != HEAL_OK) return st;
+    a.k = k;
+    a.v = v;
+    a.k_token = k_token;
+    a.k_head = k_head;
+    a.v_token = v_token;
+    a.v_head = v_head;
+    a.cos = cos;
+    a.sin = sin;
+    a.places = places;
+    a.rot = (int32_t)rot;
+    a.interleaved = interleaved;
+    a.q = q;
+    a.q_out = q_out;
+    a.q_token = q_token;
+    a.q_head = q_head;
+    a.qo_token = qo_token;
+    a.qo_head = qo_head;
+    a.heads_q = (int32_t)heads_q;
+    return heal::launch_kv_append(a, stream) == hipSuccess ? HEAL_OK : HEAL_ERR_LAUNCH;
+}
+
+heal_status_t heal_kv_read(const heal_kv_cache_t *cache, const heal_kv_batch_t *batch, float *k, float *v,
+                           hipStream_t stream)
+{
+    heal::KvCache c;
+    heal::KvSeqs b;
+    bool nothing = false;
+    heal_status_t st = kv_views(cache, batch, &c, &b, &nothing);
+    if (st != HEAL_OK) return st;
+    if (!aligned4(k) || !aligned4(v)) return HEAL_ERR_INVALID_VALUE;
+    if (nothing || (!k && !v)) return HEAL_OK;
+    st = check_device();
+    if (st != HEAL_OK) return st;
+    return heal::launch_kv_read(b, c, k, v, stream) == hipSuccess ? HEAL_OK : HEAL_ERR_LAUNCH;
+}
+
+heal_status_t heal_kv_select(const heal_kv_cache_t *cache, const heal_kv_batch_t *batch, const float *q,
+                             int64_t q_token, int64_t q_head, int64_t heads_q, int64_t n_sel,
+                             int64_t keep_first, int64_t keep_last, int32_t *sel, hipStream_t stream)
+{
+    heal::KvSelectArgs a = {};
+    bool nothing = false;
+    heal_status_t st = kv_views(cache, batch, &a.c, &a.b, &nothing);
+    if (st != HEAL_OK) return st;
+    if (!kv_group(cache, heads_q) || !kv_stride(q_token) || !kv_stride(q_head)) return HEAL_ERR_INVALID_VALUE;
+    if (keep_first < 0 || keep_last < 1 || n_sel > ((int64_t)1 << 30) || keep_first > n_sel ||
+        keep_last > n_sel - keep_first || batch->table_cols > heal::kMaxSelectBlocks)
+        return HEAL_ERR_INVALID_VALUE;
+    if (nothing) return HEAL_OK;
+    if (!q || !sel || !aligned4(q) || !aligned4(sel)) return HEAL_ERR_INVALID_VALUE;
+    st = check_device();
+    if (st != HEAL_OK) return st;
+    a.q = q;
+    a.q_token = q_token;
+    a.q_head = q_head;
+    a.group = (int32_t)(heads_q / cache->heads);
+    a.n_sel = (int32_t)n_sel;
+    a.keep_first = (int32_t)keep_first;
+    a.keep_last = (int32_t)keep_last;
+    a.sel = sel;
+    return heal::launch_kv_select(a, stream) == hipSuccess ? HEAL_OK : HEAL_ERR_LAUNCH;
+}
+
+int64_t heal_kv_attention_workspace(const heal_kv_cache_t *cache, const heal_kv_batch_t *batch, int64_t heads_q,
+                                    int64_t window, int64_t n_sel, int64_t chunk)
+{
+    heal::KvPlan plan;
+    return kv_attention_sizes(cache, batch, heads_q, window, n_sel, chunk, &plan) ? plan.bytes : -1;
+}
+
+heal_status_t heal_kv_attention(const heal_kv_cache_t *cache, const heal_kv_batch_t *batch, const float *q,
+                                int64_t q_token, int64_t q_head, int64_t heads_q, float scale, int causal,
+                                int64_t window, const int32_t *sel, int64_t n_sel, float *out,
+                                int64_t out_token, int64_t out_head, float *lse, int64_t chunk,
+                                void *workspace, int64_t workspace_bytes, hipStream_t stream)
+{
+    heal::KvAttnArgs a = {};
+    heal::KvPlan plan;
+    bool nothing = false;
+    if (!kv_attention_sizes(cache, batch, heads_q, window, n_sel, chunk, &plan)) return HEAL_ERR_INVALID_VALUE;
+    heal_status_t st = kv_views(cache, batch, &a.c, &a.b, &nothing);
+    if (st != HEAL_OK) return st;
+    if ((causal != 0 && causal != 1) || (sel != nullptr) != (n_sel > 0) || !aligned4(sel) ||
+        !(fabsf(scale) <= 3.4028235e38f))
+        return HEAL_ERR_INVALID_VALUE;
+    if (!kv_stride(q_token) || !kv_stride(q_head) ||
+        !kv_apart(batch->tokens, heads_q, cache->dim, out_token, out_head))
+        return HEAL_ERR_INVALID_VALUE;
+    if (nothing) return HEAL_OK;
+    if (!q || !out || !aligned4(q) || !aligned4(out) || !aligned4(lse)) return HEAL_ERR_INVALID_VALUE;
+    if (plan.bytes > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < plan.bytes))
+        return HEAL_ERR_INVALID_VALUE;
+    st = check_device();
+    if (st != HEAL_OK) return st;
+    a.q = q;
+    a.q_token = q_token;
+    a.q_head = q_head;
+    a.out = out;
+    a.out_token = out_token;
+    a.out_head = out_head;
+    a.lse = lse;
+    a.sel = sel;
+    a.n_sel = (int32_t)n_sel;
+    a.group = (int32_t)(heads_q / cache->heads);
+    a.scale = scale;
+    a.causal = causal;
+    a.window = (int32_t)window;
+    a.vec = aligned16(q) && aligned16(out) && (q_token | q_head | out_token | out_head) % 4 == 0;
+    a.ws_o = static_cast<float *>(workspace);
+    a.ws_ml = a.ws_o + batch->tokens * heads_q * plan.parts * cache->dim;
+    return heal::launch_kv_attention(a, plan, stream) == hipSuccess ? HEAL_OK : HEAL_ERR_LAUNCH;
 }
 
 }  // extern "C"

@@ -1,0 +1,489 @@
+// The key/value cache's own kernels: tokens appended (with the rotation of their
+// places), rows read back, and the blocks that a query should read.
+#include "heal_device.h"
+#include "heal_kv.h"
+
+namespace heal {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// INT8 code of one element: the real quotient 127 x / m rounded to the nearest
+// integer, ties to even.  127 x is exact in FP64; the product with inv = 1 / m is off
+// by less than 2^-44 and decides every quotient that is further than 2^-40 from a
+// half-integer; the others take the correctly rounded FP64 quotient, which cannot
+// cross a half-integer that it does not equal (x and m lie on the grid of x's last
+// place, 2^-31 of m or more where a quotient reaches 1/2, so the two are 2^-33 apart
+// or more).
+__device__ __forceinline__ int code_i8(float x, double m, double inv)
+{
+    const double n = 127.0 * (double)x, p = n * inv;
+    double r = __builtin_rint(p);
+    if (__builtin_expect(__builtin_fabs(p - r) > 0.5 - 0x1p-40, 0)) r = __builtin_rint(n / m);
+    return (int)r;
+}
+
+__device__ __forceinline__ f32x4 load4(const float *p, bool vec)
+{
+    if (vec) return *reinterpret_cast<const f32x4 *>(p);
+    return f32x4{p[0], p[1], p[2], p[3]};
+}
+
+__device__ __forceinline__ uint32_t max_over_workgroup(uint32_t m, uint32_t *part)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) m = max(m, part[w]);
+    return m;
+}
+
+// The pair (a, b) rotated: the FP64 products of FP32 values are exact and one sum of
+// two is rounded once, fused or not, so the bits do not depend on contraction.
+__device__ __forceinline__ void rotate(float &a, float &b, float co, float si)
+{
+    const double x = a, y = b, c = co, s = si;
+    a = (float)(x * c - y * s);
+    b = (float)(y * c + x * s);
+}
+
+// One block of one head, keys or values: rows staged in LDS as FP32, one more
+// element per row than dim so that columns spread over the banks.
+template <int D, int B>
+struct Stage {
+    float x[B][D + 1];
+    double sum[kThreads / D][D];
+    uint32_t part[kThreads / 64];
+};
+
+// New rows (place >= start) of block blk into the stage; keys are rotated.
+template <int D, int B, bool KEYS>
+__device__ __forceinline__ void stage_new(Stage<D, B> &st, const KvAppendArgs &a, const KvSeq &s,
+                                          int start, int head, int64_t blk)
+{
+    const float *src = KEYS ? a.k : a.v;
+    const int64_t ts = KEYS ? a.k_token : a.v_token;
+    src += head * (KEYS ? a.k_head : a.v_head);
+    const bool vec = ((reinterpret_cast<uintptr_t>(src) | (uintptr_t)(ts * 4)) & 15u) == 0;
+    const int64_t p0 = blk * B;
+    const int lo = p0 < start ? (int)(start - p0) : 0;
+    const int hi = s.len - p0 < B ? (int)(s.len - p0) : B;
+    const int64_t tok0 = (int64_t)s.first + (p0 - (s.len - s.n));
+    for (int i = threadIdx.x; i < (hi - lo) * (D / 4); i += kThreads) {
+        const int r = lo + i / (D / 4), c = i % (D / 4) * 4;
+        const f32x4 v = load4(src + (tok0 + r) * ts + c, vec);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) st.x[r][c + e] = v[e];
+    }
+    __syncthreads();
+    if (KEYS && a.rot > 0) {
+        const int half = a.rot / 2;
+        for (int i = threadIdx.x; i < (hi - lo) * half; i += kThreads) {
+            const int r = lo + i / half, j = i % half;
+            const int64_t p = p0 + r;
+            if (p >= a.places) continue;
+            const int ja = a.interleaved ? 2 * j : j, jb = a.interleaved ? 2 * j + 1 : j + half;
+            float x = st.x[r][ja], y = st.x[r][jb];
+            rotate(x, y, a.cos[p * half + j], a.sin[p * half + j]);
+            st.x[r][ja] = x;
+            st.x[r][jb] = y;
+        }
+        __syncthreads();
+    }
+}
+
+// The staged new rows of block blk into the sequence's ring.
+template <int D, int B, bool KEYS>
+__device__ __forceinline__ void store_ring(const Stage<D, B> &st, const KvAppendArgs &a,
+                                           const KvSeq &s, int start, int head, int64_t blk, int slot)
+{
+    const int64_t p0 = blk * B;
+    const int lo = p0 < start ? (int)(start - p0) : 0;
+    const int hi = s.len - p0 < B ? (int)(s.len - p0) : B;
+    const int half = (int)(blk & 1) * B;
+    const int64_t base = ((int64_t)slot * a.c.heads + head) * (2 * B * D);
+    if (KEYS) {
+        for (int i = threadIdx.x; i < (hi - lo) * D; i += kThreads) {
+            const int r = lo + i / D, c = i % D;
+            a.c.kr[base + (int64_t)(half + r) * D + c] = st.x[r][c];
+        }
+    } else {
+        for (int i = threadIdx.x; i < (hi - lo) * D; i += kThreads) {
+            const int c = i / (hi - lo), r = lo + i % (hi - lo);
+            a.c.vr[base + (int64_t)c * (2 * B) + half + r] = st.x[r][c];
+        }
+    }
+}
+
+// One block of one head: the rows that the ring holds of it and the new ones, their
+// maximum and mean, and, if the block is complete, its codes.
+template <int D, int B, bool KEYS>
+__device__ __forceinline__ void append_block(Stage<D, B> &st, const KvAppendArgs &a, int seq, int unit, int head)
+{
+    const KvSeq s = kv_seq(a.b, seq);
+    const KvTouched t = kv_touched(s, B);
+    const int64_t blk = (int64_t)t.first + unit;
+    if (blk > t.last || blk >= a.b.cols) return;
+    const int slot = kv_slot(a.b, seq);
+    const int page = kv_page(a.b, seq, (int)blk);
+    const int64_t p0 = blk * B;
+    const int old = p0 < t.start ? (int)(t.start - p0) : 0;   // rows from the ring
+    const int rows = s.len - p0 < B ? (int)(s.len - p0) : B;
+
+    // rows of the ring (zeros without one), and zeros behind the last row
+    const int64_t base = ((int64_t)slot * a.c.heads + head) * (2 * B * D);
+    const int half = (int)(blk & 1) * B;
+    for (int i = threadIdx.x; i < old * D; i += kThreads) {
+        if (KEYS) {
+            const int r = i / D, c = i % D;
+            st.x[r][c] = slot >= 0 ? a.c.kr[base + (int64_t)(half + r) * D + c] : 0.0f;
+        } else {
+            const int c = i / old, r = i % old;
+            st.x[r][c] = slot >= 0 ? a.c.vr[base + (int64_t)c * (2 * B) + half + r] : 0.0f;
+        }
+    }
+    for (int i = threadIdx.x; i < (B - rows) * D; i += kThreads) st.x[rows + i / D][i % D] = 0.0f;
+    stage_new<D, B, KEYS>(st, a, s, t.start, head, blk);
+
+    const int conflict = kv_ring_conflict(t);
+    if (slot >= 0 && blk >= t.last - 1 && blk != conflict)
+        store_ring<D, B, KEYS>(st, a, s, t.start, head, blk, slot);
+
+    if (page >= 0) {
+        uint32_t m = 0u;
+        for (int i = threadIdx.x; i < rows * D; i += kThreads)
+            m = max(m, __builtin_bit_cast(uint32_t, st.x[i / D][i % D]) & 0x7fffffffu);
+        m = max_over_workgroup(m, st.part);
+        const float mf = __builtin_bit_cast(float, m);
+        const int64_t ph = (int64_t)page * a.c.heads + head;
+        if (threadIdx.x == 0) a.c.scales[2 * ph + (KEYS ? 0 : 1)] = mf;
+        if (KEYS) {
+            // the mean: FP64 sums over whole parts of the block (zeros behind the last
+            // row add nothing), joined in their order
+            constexpr int P = kThreads / D;
+            const int c = threadIdx.x % D, w = threadIdx.x / D;
+            if (w < P) {
+                double sum = 0.0;
+                for (int r = w * (B / P); r < (w + 1) * (B / P); ++r) sum += (double)st.x[r][c];
+                st.sum[w][c] = sum;
+            }
+            __syncthreads();
+            if (threadIdx.x < D) {
+                double sum = st.sum[0][threadIdx.x];
+#pragma unroll
+                for (int w2 = 1; w2 < P; ++w2) sum += st.sum[w2][threadIdx.x];
+                a.c.mean[ph * D + threadIdx.x] = (float)(sum / (double)rows);
+            }
+        }
+        if (rows == B) {
+            const bool zero = !(mf > 0.0f);
+            const double md = zero ? 1.0 : (double)mf, inv = 1.0 / md;
+            uint32_t *out = reinterpret_cast<uint32_t *>(KEYS ? a.c.kc : a.c.vc) + ph * (B * D / 4);
+            for (int i = threadIdx.x; i < B * D / 4; i += kThreads) {
+                uint32_t w = 0u;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float x;
+                    if (KEYS) {
+                        x = st.x[i / (D / 4)][i % (D / 4) * 4 + e];
+                    } else {
+                        // dword i of [D][B]: value places 4 q .. 4 q + 3 of column i / (B / 4)
+                        const int q = i % (B / 4), g = q / (B / 16), sb = q % (B / 16);
+                        x = st.x[16 * sb + 4 * g + e][i / (B / 4)];
+                    }
+                    w |= (uint32_t)(zero ? 0 : code_i8(x, md, inv) & 0xff) << (8 * e);
+                }
+                out[i] = w;
+            }
+        }
+    }
+
+    // ring rows of a later block where unit 0's old rows were
+    if (unit == 0 && conflict >= 0 && conflict < a.b.cols && slot >= 0) {
+        __syncthreads();
+        stage_new<D, B, KEYS>(st, a, s, t.start, head, conflict);
+        store_ring<D, B, KEYS>(st, a, s, t.start, head, conflict, slot);
+    }
+}
+
+// Queries of one token, rotated.
+__device__ __forceinline__ void rotate_queries(const KvAppendArgs &a, int64_t token)
+{
+    const int seq = kv_last_at_most(a.b.seqs, token, [&](int i) { return (int64_t)kv_first(a.b, i); });
+    const KvSeq s = kv_seq(a.b, seq);
+    if (token < s.first || token >= (int64_t)s.first + s.n) return;
+    const int64_t p = (int64_t)s.len - s.n + (token - s.first);
+    const bool turn = p >= 0 && p < a.places;
+    const int half = a.rot / 2, D = a.c.dim, rest = D - a.rot;
+    const float *src = a.q + token * a.q_token;
+    float *dst = a.q_out + token * a.qo_token;
+    for (int i = threadIdx.x; i < a.heads_q * half; i += kThreads) {
+        const int h = i / half, j = i % half;
+        const int ja = a.interleaved ? 2 * j : j, jb = a.interleaved ? 2 * j + 1 : j + half;
+        float x = src[h * a.q_head + ja], y = src[h * a.q_head + jb];
+        if (turn) rotate(x, y, a.cos[p * half + j], a.sin[p * half + j]);
+        dst[h * a.qo_head + ja] = x;
+        dst[h * a.qo_head + jb] = y;
+    }
+    for (int i = threadIdx.x; i < a.heads_q * rest; i += kThreads) {
+        const int h = i / rest, j = a.rot + i % rest;
+        dst[h * a.qo_head + j] = src[h * a.q_head + j];
+    }
+}
+
+// One workgroup per (unit, head, keys or values), then one per token's queries.
+template <int D, int B>
+__global__ void __launch_bounds__(kThreads)
+kv_append_kernel(KvAppendArgs a, int64_t wg0, int64_t blocks_wg)
+{
+    __shared__ Stage<D, B> st;
+    const int64_t wg = wg0 + blockIdx.x;
+    if (wg >= blocks_wg) {
+        rotate_queries(a, wg - blocks_wg);
+        return;
+    }
+    const int64_t u = wg / (2 * a.c.heads);
+    const int role = (int)(wg % (2 * a.c.heads));
+    const int seq = kv_last_at_most(a.b.seqs, u, [&](int i) { return kv_unit(a.b, B, i); });
+    const int64_t j = u - kv_unit(a.b, B, seq);
+    if (j < 0) return;
+    if (role < a.c.heads)
+        append_block<D, B, true>(st, a, seq, (int)j, role);
+    else
+        append_block<D, B, false>(st, a, seq, (int)j, role - a.c.heads);
+}
+
+// One block of one head back as FP32 rows.
+template <int D, int B>
+__global__ void __launch_bounds__(kThreads)
+kv_read_kernel(KvSeqs b, KvCache c, float *k, float *v, int64_t wg0)
+{
+    __shared__ uint32_t codes[B * D / 4];
+    const int64_t wg = wg0 + blockIdx.x;
+    const int64_t u = wg / (2 * c.heads);
+    const int role = (int)(wg % (2 * c.heads));
+    const bool keys = role < c.heads;
+    const int head = keys ? role : role - c.heads;
+    float *out = keys ? k : v;
+    if (!out) return;
+    const int seq = kv_last_at_most(b.seqs, u, [&](int i) { return kv_unit(b, B, i); });
+    const int64_t j = u - kv_unit(b, B, seq);
+    if (j < 0) return;
+    const KvSeq s = kv_seq(b, seq);
+    const KvTouched t = kv_touched(s, B);
+    const int64_t ld = (int64_t)c.heads * D;
+    out += head * D;
+    if (j == 0)   // tokens before place 0 are nowhere
+        for (int64_t i = threadIdx.x; i < (int64_t)(s.n - s.len) * D; i += kThreads)
+            out[(s.first + i / D) * ld + i % D] = 0.0f;
+    const int64_t blk = t.first + j;
+    if (blk > t.last) return;
+    const int64_t p0 = blk * B;
+    const int lo = p0 < t.start ? (int)(t.start - p0) : 0;
+    const int hi = s.len - p0 < B ? (int)(s.len - p0) : B;
+    out += ((int64_t)s.first + (p0 - (s.len - s.n))) * ld;
+    const int page = blk < b.cols ? kv_page(b, seq, (int)blk) : -1;
+    const int slot = kv_slot(b, seq);
+    const bool full = p0 + B <= s.len;
+    if (page < 0 || (!full && slot < 0)) {
+        for (int i = threadIdx.x; i < (hi - lo) * D; i += kThreads)
+            out[(int64_t)(lo + i / D) * ld + i % D] = 0.0f;
+    } else if (full) {
+        const int64_t ph = (int64_t)page * c.heads + head;
+        const uint32_t *src = reinterpret_cast<const uint32_t *>(keys ? c.kc : c.vc) + ph * (B * D / 4);
+        const float step = c.scales[2 * ph + (keys ? 0 : 1)] / 127.0f;
+        for (int i = threadIdx.x; i < B * D / 4; i += kThreads) codes[i] = src[i];
+        __syncthreads();
+        const int8_t *x = reinterpret_cast<const int8_t *>(codes);
+        for (int i = threadIdx.x; i < (hi - lo) * D; i += kThreads) {
+            const int r = lo + i / D, col = i % D;
+            const int8_t q = keys ? x[r * D + col] : x[col * B + kv_value_place(B, r)];
+            out[(int64_t)r * ld + col] = (float)q * step;
+        }
+    } else {
+        const int64_t base = ((int64_t)slot * c.heads + head) * (2 * B * D);
+        const int half = (int)(blk & 1) * B;
+        for (int i = threadIdx.x; i < (hi - lo) * D; i += kThreads) {
+            const int r = lo + i / D, col = i % D;
+            out[(int64_t)r * ld + col] = keys ? c.kr[base + (int64_t)(half + r) * D + col]
+                                              : c.vr[base + (int64_t)col * (2 * B) + half + r];
+        }
+    }
+}
+
+// Scores in an order that unsigned integers keep: larger is better.
+__device__ __forceinline__ uint64_t score_key(double x)
+{
+    if (!(x == x)) return 0u;   // no number: below -infinity's key, and taken like it
+    uint64_t u = __builtin_bit_cast(uint64_t, x + 0.0);   // -0 counts as 0
+    return u >> 63 ? ~u : u | 0x8000000000000000ull;
+}
+constexpr uint64_t kLowest = 0x000fffffffffffffull;   // the key of -infinity
+
+constexpr int kSelectHeads = 8;   // queries scored at once
+
+// One workgroup per token and key/value head.  Every thread scores blocks of its
+// own: the FP64 sum over d in ascending order, so equal blocks score equally.  The
+// n-th best key is found digit by digit (8 bits each, a histogram in LDS), and one
+// wave writes the blocks above it, and the lowest of those equal to it, in order.
+template <int D>
+__global__ void __launch_bounds__(kThreads)
+kv_select_kernel(KvSelectArgs a, int B, int64_t wg0)
+{
+    extern __shared__ char lds[];
+    uint64_t *key = reinterpret_cast<uint64_t *>(lds);
+    __shared__ double q[kSelectHeads][D];
+    __shared__ uint32_t hist[256];
+    __shared__ uint32_t found[2];
+    const int64_t wg = wg0 + blockIdx.x;
+    const int64_t token = wg / a.c.heads;
+    const int head = (int)(wg % a.c.heads);
+    const int seq = kv_last_at_most(a.b.seqs, token, [&](int i) { return (int64_t)kv_first(a.b, i); });
+    const KvSeq s = kv_seq(a.b, seq);
+    if (token < s.first || token >= (int64_t)s.first + s.n) return;
+    int32_t *sel = a.sel + wg * a.n_sel;
+    const int64_t place = (int64_t)s.len - s.n + (token - s.first);
+    int64_t last = place < 0 ? -1 : place / B;
+    if (last >= a.b.cols) last = a.b.cols - 1;
+    const int nb = (int)last + 1;
+    if (nb <= a.n_sel) {   // all of them
+        for (int i = threadIdx.x; i < a.n_sel; i += kThreads) sel[i] = i < nb ? i : -1;
+        return;
+    }
+    // candidates lo .. hi - 1, of which r are taken; nb > n_sel >= keep_first + keep_last
+    const int lo = a.keep_first, hi = nb - a.keep_last, r = a.n_sel - a.keep_first - a.keep_last;
+    for (int g0 = 0; g0 < a.group && r > 0; g0 += kSelectHeads) {
+        const int ng = a.group - g0 < kSelectHeads ? a.group - g0 : kSelectHeads;
+        __syncthreads();
+        for (int i = threadIdx.x; i < kSelectHeads * D; i += kThreads) {
+            const int g = i / D, d = i % D;
+            // (queries behind the last one repeat the first: no score changes)
+            const int64_t h = (int64_t)head * a.group + g0 + (g < ng ? g : 0);
+            q[g][d] = (double)a.q[token * a.q_token + h * a.q_head + d];
+        }
+        __syncthreads();
+        for (int b = lo + threadIdx.x; b < hi; b += kThreads) {
+            const int page = kv_page(a.b, seq, b);
+            uint64_t best = kLowest;
+            if (page >= 0) {
+                const f32x4 *m = reinterpret_cast<const f32x4 *>(a.c.mean + ((int64_t)page * a.c.heads + head) * D);
+                double sum[kSelectHeads] = {};
+                for (int d = 0; d < D; d += 4) {
+                    const f32x4 x = m[d / 4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const double y = (double)x[e];
+#pragma unroll
+                        for (int g = 0; g < kSelectHeads; ++g) sum[g] = __builtin_fma(q[g][d + e], y, sum[g]);
+                    }
+                }
+#pragma unroll
+                for (int g = 0; g < kSelectHeads; ++g) {
+                    const uint64_t u = score_key(sum[g]);
+                    best = u > best ? u : best;
+                }
+            }
+            if (g0 > 0 && key[b] > best) best = key[b];
+            key[b] = best;
+        }
+    }
+    __syncthreads();
+    // the r-th largest key, and how many of its equals are taken
+    uint64_t top = 0u, mask = 0u;
+    uint32_t left = (uint32_t)r;
+    for (int shift = 56; shift >= 0 && r > 0; shift -= 8) {
+        for (int i = threadIdx.x; i < 256; i += kThreads) hist[i] = 0u;
+        __syncthreads();
+        for (int b = lo + threadIdx.x; b < hi; b += kThreads)
+            if ((key[b] & mask) == top) atomicAdd(&hist[(key[b] >> shift) & 255u], 1u);
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            uint32_t above = 0u;
+            int digit = 255;
+            while (digit > 0 && above + hist[digit] < left) above += hist[digit--];
+            found[0] = (uint32_t)digit;
+            found[1] = above;
+        }
+        __syncthreads();
+        top |= (uint64_t)found[0] << shift;
+        mask |= 255ull << shift;
+        left -= found[1];
+        __syncthreads();
+    }
+    if (threadIdx.x >= 64) return;
+    const int lane = threadIdx.x;
+    int at = 0;
+    uint32_t equals = 0u;
+    const uint64_t before = (1ull << lane) - 1;
+    for (int b0 = 0; b0 < nb; b0 += 64) {
+        const int b = b0 + lane;
+        const bool forced = b < nb && (b < lo || b >= hi);
+        const bool cand = r > 0 && b >= lo && b < hi;
+        const uint64_t x = cand ? key[b] : 0u;
+        const uint64_t same = __ballot(cand && x == top);
+        const uint32_t rank = equals + (uint32_t)__popcll(same & before);
+        const bool take = forced || (cand && (x > top || (x == top && rank < left)));
+        const uint64_t taken = __ballot(take);
+        if (take) sel[at + __popcll(taken & before)] = b;
+        at += __popcll(taken);
+        equals += (uint32_t)__popcll(same);
+    }
+}
+
+template <int D, int B>
+hipError_t append_sized(const KvAppendArgs &a, hipStream_t stream)
+{
+    const int64_t blocks_wg = kv_units(a.b.cu != nullptr, a.b.tokens, a.b.seqs, B) * 2 * a.c.heads;
+    return in_parts(blocks_wg + (a.q ? a.b.tokens : 0), [&](int64_t at, unsigned n) {
+        hipLaunchKernelGGL((kv_append_kernel<D, B>), dim3(n), dim3(kThreads), 0, stream, a, at, blocks_wg);
+    });
+}
+
+template <int D, int B>
+hipError_t read_sized(const KvSeqs &b, const KvCache &c, float *k, float *v, hipStream_t stream)
+{
+    const int64_t n = kv_units(b.cu != nullptr, b.tokens, b.seqs, B) * 2 * c.heads;
+    return in_parts(n, [&](int64_t at, unsigned m) {
+        hipLaunchKernelGGL((kv_read_kernel<D, B>), dim3(m), dim3(kThreads), 0, stream, b, c, k, v, at);
+    });
+}
+
+}  // namespace
+
+hipError_t launch_kv_append(const KvAppendArgs &a, hipStream_t stream)
+{
+    return sized(a.c.dim, a.c.block, [&](auto D, auto B) { return append_sized<D.value, B.value>(a, stream); });
+}
+
+hipError_t launch_kv_read(const KvSeqs &b, const KvCache &c, float *k, float *v, hipStream_t stream)
+{
+    return sized(c.dim, c.block, [&](auto D, auto B) { return read_sized<D.value, B.value>(b, c, k, v, stream); });
+}
+
+hipError_t launch_kv_select(const KvSelectArgs &a, hipStream_t stream)
+{
+    const int64_t n = (int64_t)a.b.tokens * a.c.heads;
+    const size_t lds = (size_t)a.b.cols * sizeof(uint64_t);
+    if (lds > 32768) {   // beyond what a kernel may ask for by itself
+        const void *f = a.c.dim == 64   ? reinterpret_cast<const void *>(kv_select_kernel<64>)
+                        : a.c.dim == 96 ? reinterpret_cast<const void *>(kv_select_kernel<96>)
+                                        : reinterpret_cast<const void *>(kv_select_kernel<128>);
+        const hipError_t err = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                   (int)(kMaxSelectBlocks * sizeof(uint64_t)));
+        if (err != hipSuccess) return err;
+    }
+    return in_parts(n, [&](int64_t at, unsigned m) {
+        const dim3 grid(m), block(kThreads);
+        if (a.c.dim == 64)
+            hipLaunchKernelGGL(kv_select_kernel<64>, grid, block, lds, stream, a, a.c.block, at);
+        else if (a.c.dim == 96)
+            hipLaunchKernelGGL(kv_select_kernel<96>, grid, block, lds, stream, a, a.c.block, at);
+        else
+            hipLaunchKernelGGL(kv_select_kernel<128>, grid, block, lds, stream, a, a.c.block, at);
+    });
+}
+
+}  // namespace heal
