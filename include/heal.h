@@ -332,8 +332,9 @@ heal_status_t heal_scores_i16(int64_t M, int64_t N, int64_t K, const int16_t *Q,
  * a ring of 2 * block rows per sequence (its slot) and head.  A block that is not
  * complete is read from the ring; when its last token arrives it is quantised from
  * the ring's rows, once.  The cache therefore does not depend on how tokens were cut
- * into calls, and a sequence may be cut back (drafted tokens that were refused) as
- * far as the beginning of the block before its last one, by passing a smaller length.
+ * into calls, and a sequence may be cut back (drafted tokens that were refused) by
+ * passing a smaller length: as far as the beginning of the block before the last one
+ * that it has reached, whose rows the ring still has.
  *
  * Arrays (device, 16-byte aligned, owned by the caller, dense):
  *   k_codes  [blocks][heads][block][dim]
@@ -438,7 +439,7 @@ heal_status_t heal_kv_select(const heal_kv_cache_t *cache, const heal_kv_batch_t
  * heal_kv_attention -- attention of the tokens' queries over the cache:
  *     s_t = scale * q . k_t,  o = sum_t softmax(s)_t v_t,  lse = ln sum_t exp(s_t)
  * over the tokens t of the sequence with t <= place (causal = 1; all of them with
- * causal = 0) and, with window > 0, t > place - window.  A row that sees nothing
+ * causal = 0) and, with window > 0 (causal = 1 only), t > place - window.  A row that sees nothing
  * gives o = 0 and lse = -infinity.  Codes are exact in FP16; queries and softmax
  * weights go to the matrix units as FP16 pairs (head and residual, scaled by powers
  * of two, off by at most 2^-22 of the value), FP32 rows of the cache likewise, all

@@ -632,7 +632,7 @@ heal_status_t heal_kv_attention(const heal_kv_cache_t *cache, const heal_kv_batc
     if (!kv_attention_sizes(cache, batch, heads_q, window, n_sel, chunk, &plan)) return HEAL_ERR_INVALID_VALUE;
     heal_status_t st = kv_views(cache, batch, &a.c, &a.b, &nothing);
     if (st != HEAL_OK) return st;
-    if ((causal != 0 && causal != 1) || (sel != nullptr) != (n_sel > 0) || !aligned4(sel) ||
+    if ((causal != 0 && causal != 1) || (window > 0 && !causal) || (sel != nullptr) != (n_sel > 0) || !aligned4(sel) ||
         !(fabsf(scale) <= 3.4028235e38f))
         return HEAL_ERR_INVALID_VALUE;
     if (!kv_stride(q_token) || !kv_stride(q_head) ||

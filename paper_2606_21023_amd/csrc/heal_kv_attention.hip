@@ -73,6 +73,17 @@ __device__ __forceinline__ int exponent(float x)
     return __builtin_amdgcn_frexp_expf(x);
 }
 
+// A value that all lanes have.  Matrix instructions take no notice of lanes that are
+// switched off, so every branch around them has to be one of the whole wave, and what
+// it depends on has to be known as such.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+__device__ __forceinline__ KvSeq uniform_seq(const KvSeqs &b, int i)
+{
+    const KvSeq s = kv_seq(b, i);
+    return KvSeq{uniform(s.first), uniform(s.n), uniform(s.len)};
+}
+
 __device__ __forceinline__ float max_over_groups(float x)
 {
     x = __builtin_fmaxf(x, __shfl_xor(x, 16));
@@ -106,14 +117,16 @@ __device__ __forceinline__ bool find_rows(const KvAttnArgs &a, bool by_token, in
         const int64_t token = u / per;
         t.seq = a.b.cu ? kv_last_at_most(a.b.seqs, token, [&](int i) { return (int64_t)kv_first(a.b, i); })
                        : (int)token;
-        t.s = kv_seq(a.b, t.seq);
+        t.seq = uniform(t.seq);
+        t.s = uniform_seq(a.b, t.seq);
         if (token < t.s.first || token >= (int64_t)t.s.first + t.s.n) return false;
         row0 = (int)(u % per) * R;
         rows = a.group - row0 < R ? a.group - row0 : R;
         row0 += (int)(token - t.s.first) * a.group;
     } else {
         t.seq = kv_last_at_most(a.b.seqs, u, [&](int i) { return kv_tile(a.b, a.group, R, i); });
-        t.s = kv_seq(a.b, t.seq);
+        t.seq = uniform(t.seq);
+        t.s = uniform_seq(a.b, t.seq);
         const int64_t j = u - kv_tile(a.b, a.group, R, t.seq);
         const int64_t n = (int64_t)t.s.n * a.group;
         if (j < 0 || j * R >= n) return false;
@@ -187,7 +200,7 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
     __shared__ float part_o[W][16][D + 4];
     __shared__ float part_m[W][16], part_l[W][16];
     __shared__ int part_row[16], part_head[16];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int64_t wg = wg0 + blockIdx.x;
     const int part = (int)(wg % a.parts);
     const int head = (int)(wg / a.parts % a.c.heads);
@@ -203,13 +216,13 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
     const int64_t from = base + (int64_t)part * a.part_tiles;
     const int64_t to = from + a.part_tiles < end ? from + a.part_tiles : end;
     const bool none = from >= to || t.last < t.first;
-    const int slot = kv_slot(a.b, t.seq);
+    const int slot = uniform(kv_slot(a.b, t.seq));
 
     f32x4 o[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) o[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     float m = -__builtin_inff(), l = 0.0f;
-    int ref = kNoScale;   // o is in units of 2^(ref - 14) / 127
+    int ref = kNoScale;   // this row's o is in units of 2^(ref - 14) / 127
 
     if (!none) {
         // the query row: lane (r, g) holds elements g D/4 .. of row r
@@ -241,7 +254,7 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
         for (int64_t kt = from + wave; kt < to; kt += W) {
             Group gr[4];
             bool coded = true;
-            float fk[4], mv[4];
+            float fk[4], mv[4], mr[4];
             int ev = kNoScale;
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
@@ -249,8 +262,8 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
                 const int64_t entry = at / B;
                 gr[s].off = (int)(at % B);
                 gr[s].blk = (int)entry;
-                if (a.sel) gr[s].blk = entry < a.n_sel ? list[entry] : -1;
-                gr[s].page = kv_page(a.b, t.seq, gr[s].blk);
+                if (a.sel) gr[s].blk = entry < a.n_sel ? uniform(list[entry]) : -1;
+                gr[s].page = uniform(kv_page(a.b, t.seq, gr[s].blk));
                 if (gr[s].page < 0) gr[s].blk = -1;
                 const bool full = gr[s].blk >= 0 && (int64_t)gr[s].blk * B + B <= t.s.len;
                 if (gr[s].blk >= 0 && !full && slot < 0) gr[s].blk = -1;
@@ -261,7 +274,10 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
                     fk[s] = sc[0];
                     mv[s] = sc[1];
                 }
-                ev = max(ev, exponent(mv[s]));
+                // (a row's units follow the blocks that it sees something of, and no others)
+                const int64_t t0 = (int64_t)gr[s].blk * B + gr[s].off;
+                mr[s] = gr[s].blk < 0 || t0 > t.hi || t0 + 15 < t.lo ? 0.0f : mv[s];
+                ev = max(ev, exponent(mr[s]));
             }
 
             f32x4 st[4];
@@ -393,8 +409,8 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 const bool full = gr[s].blk >= 0 && (int64_t)gr[s].blk * B + B <= t.s.len;
-                const int es = exponent(mv[s]);
-                wv[s] = full ? ldexpf(mv[s], 14 - rn) : es == kNoScale ? 0.0f : ldexpf(127.0f, es + 7 - rn);
+                const int es = exponent(mr[s]);
+                wv[s] = full ? ldexpf(mr[s], 14 - rn) : es == kNoScale ? 0.0f : ldexpf(127.0f, es + 7 - rn);
             }
             float sum = 0.0f;
             f16x8 ph[2], pl[2];

@@ -80,8 +80,9 @@ def attention(q, K, V, scale, seen):
     return p @ V[at], m + np.log(e.sum()), S, p @ np.abs(V[at])
 
 
-def bound(S, n, dim):
-    """(relative to A, absolute of lse): how far FP32 sums of FP16 pairs may be off.
+def bound(S, n, dim, q=0.0, k=0.0, v=0.0):
+    """(relative to A, absolute of o, absolute of lse): how far FP32 sums of FP16 pairs
+    may be off.
 
     A score's terms are off by 2^-22 (the pair of q) and, in an FP32 row, 2^-22 and
     2^-22 more (its pair, the residuals' product); its sum of 3 dim terms by
@@ -90,10 +91,20 @@ def bound(S, n, dim):
     argument by 2^-24 of it and its result by 2^-23.  A weight's relative error is the
     score's absolute one, twice (numerator and sum); the weights' pairs are off by
     2^-22 and the sums of 3 n terms by 4 sqrt(3 n) 2^-24, at most 32 factors exp2(m - m')
-    of 2^-23 each on the way."""
-    score = S * (3 * 2.0 ** -22 + (4 * np.sqrt(3 * dim) + 8) * 2.0 ** -24)
+    of 2^-23 each on the way.
+
+    FP16 steps do not go below 2^-24, half of one being 2^-25.  q and k: |scale| max|q|
+    sum|k| and its like, the terms that floors meet: rows of q and k are scaled below
+    2^14 with their largest element at 2^13 or more, so an element is off by 2^-25 of
+    2^13, 2^-38 of the largest.  v: the largest value that is seen.  A weight times a
+    block's maximum is below 2^14 where 2^ref <= 2 v meets a weight of 1, and off by
+    2^-25 or more: 2^-39 2 v of the product with m, and 2^-38 v for each token; a value
+    of an FP32 row is scaled below 2^7 and off by 2^-25, 2^-32 2 v of it.  Below 2^-126
+    every rounding to FP32 is off by up to 2^-150: two for each of four waves' sums, their
+    join and the division, less than 16 in all."""
+    score = S * (3 * 2.0 ** -22 + (4 * np.sqrt(3 * dim) + 8) * 2.0 ** -24) + 2.0 ** -38 * (q + k)
     rel = 2 * score + 2.0 ** -22 + 4 * np.sqrt(3 * n) * 2.0 ** -24 + 40 * 2.0 ** -23
-    return rel, score + 4 * np.sqrt(n) * 2.0 ** -24 + 40 * 2.0 ** -23
+    return rel, (n * 2.0 ** -38 + 2.0 ** -31) * v + 2.0 ** -146, score + 4 * np.sqrt(n) * 2.0 ** -24 + 40 * 2.0 ** -23
 
 
 def select(q, means, place, block, n_sel, keep_first, keep_last):

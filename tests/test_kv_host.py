@@ -100,7 +100,7 @@ def test_a_bad_batch_is_refused(call, kw):
 )] + [(_attention, kw) for kw in (
     dict(q=0), dict(out=0), dict(q=FAKE + 2), dict(out=FAKE + 1), dict(lse=FAKE + 2), dict(heads_q=5),
     dict(scale=ctypes.c_float(float("nan"))), dict(scale=ctypes.c_float(float("inf"))), dict(causal=2),
-    dict(window=-1), dict(sel=FAKE, n_sel=0), dict(sel=None, n_sel=3), dict(sel=FAKE + 2, n_sel=3),
+    dict(window=-1), dict(window=5, causal=0), dict(sel=FAKE, n_sel=0), dict(sel=None, n_sel=3), dict(sel=FAKE + 2, n_sel=3),
     dict(sel=FAKE, n_sel=-1), dict(sel=FAKE, n_sel=1 << 30), dict(chunk=-64), dict(chunk=100),
     dict(out_token=100), dict(out_head=100), dict(workspace=None, chunk=64), dict(workspace=FAKE + 8, chunk=64),
     dict(size=64, chunk=64),
