@@ -103,7 +103,8 @@ struct Rows {
     int32_t token;   // of this lane's row, or -1 where there is none
     int32_t head_q;
     int32_t lo, hi;  // the places it sees: lo .. hi (none where hi < lo)
-    int32_t first, last;   // ... of all rows
+    int32_t first, last;   // ... one row or another
+    int32_t all_lo, all_hi;   // ... all rows
 };
 
 // Finds the rows of tile u of a key/value head.  Returns false where the tile has none.
@@ -143,9 +144,8 @@ __device__ __forceinline__ bool find_rows(const KvAttnArgs &a, bool by_token, in
         lo = (int32_t)(l < 0 ? 0 : l);
         hi = (int32_t)h;
     };
-    int32_t unused;
-    bounds(row0, t.first, unused);
-    bounds(row0 + rows - 1, unused, t.last);
+    bounds(row0, t.first, t.all_hi);
+    bounds(row0 + rows - 1, t.all_lo, t.last);
     t.token = -1;
     t.lo = 0;
     t.hi = -1;
@@ -182,21 +182,212 @@ __device__ __forceinline__ float4 load16(const float *p, bool vec)
     return float4{p[0], p[1], p[2], p[3]};
 }
 
-// What a wave knows of the 64 tokens of a tile: four groups of 16, each within one block.
-struct Group {
-    int32_t blk;    // block of the sequence, or -1 where the group holds nothing
-    int32_t page;
-    int32_t off;    // first token within the block
+// The blocks of a wave's next tiles, one to a lane: a tile of 64 tokens has EPT of
+// them, so the lanes hold the blocks and scales of TILES tiles, which are read in two
+// round trips to memory for all of them together.
+template <int B>
+struct Blocks {
+    static constexpr int EPT = B < 64 ? 64 / B : 1, TILES = 64 / EPT, STEP = B < 64 ? B : 64;
+    int blk;     // block of the sequence, or -1 where the cache holds nothing of it
+    int page;    // its page, or -1 - page where it is read from the ring
+    float k, v;  // m of its keys and values
+
+    __device__ __forceinline__ void load(const KvAttnArgs &a, const KvSeq &s, int seq, int slot, int head,
+                                         const int32_t *list, int64_t first, int64_t to, int waves)
+    {
+        const int lane = threadIdx.x & 63;
+        const int64_t tile = first + (int64_t)(lane / EPT) * waves;
+        const int64_t entry = (tile * 64 + lane % EPT * STEP) / B;
+        blk = page = -1;
+        k = v = 0.0f;
+        if (tile < to) blk = !a.sel ? (int)entry : entry < a.n_sel ? list[entry] : -1;
+        if (blk >= 0) page = kv_page(a.b, seq, blk);
+        const bool full = (int64_t)blk * B + B <= s.len;
+        if (page < 0 || (!full && slot < 0)) blk = -1;
+        if (blk >= 0) {
+            const float *sc = a.c.scales + ((int64_t)page * a.c.heads + head) * 2;
+            k = sc[0];
+            v = sc[1];
+            if (!full) page = -1 - page;
+        }
+    }
 };
+
+__device__ __forceinline__ int from_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+__device__ __forceinline__ float from_lane(float x, int lane)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+}
+
+// One tile: groups of 16 tokens, NB blocks that hold GS groups each.
+template <int B>
+struct Tile {
+    static constexpr int NB = Blocks<B>::EPT, GS = 4 / NB;
+    int blk[NB], page[NB];
+    float k[NB], v[NB];
+    int off;      // of its first token within the block (B > 64)
+    bool coded;   // every group lies in a complete block
+
+    __device__ __forceinline__ void take(const Blocks<B> &b, int at, int64_t kt)
+    {
+        off = B > 64 ? (int)(kt & 1) * 64 : 0;
+        coded = true;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            blk[i] = from_lane(b.blk, at * NB + i);
+            page[i] = from_lane(b.page, at * NB + i);
+            k[i] = from_lane(b.k, at * NB + i);
+            v[i] = from_lane(b.v, at * NB + i);
+            coded = coded && blk[i] >= 0 && page[i] >= 0;
+        }
+    }
+    // place of the first token of group s
+    __device__ __forceinline__ int64_t place(int s) const
+    {
+        return (int64_t)blk[s / GS] * B + off + s % GS * 16;
+    }
+};
+
+// Codes of a tile as they come from memory, in the registers of one lane: of keys, the
+// D/4 bytes of row r of each group that belong to lanes g; of values, of row 16 n + r
+// of V^T the four bytes of each group that do.
+template <int D, int B>
+struct Codes {
+    static constexpr int N = D / 16;
+    uint32_t k[4][D / 16], v[N][4];
+
+    __device__ __forceinline__ void load_keys(const KvAttnArgs &a, const Tile<B> &t, int head, int r, int g)
+    {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int8_t *src = a.c.kc + ((int64_t)t.page[s / Tile<B>::GS] * a.c.heads + head) * (B * D) +
+                                (t.off + s % Tile<B>::GS * 16) * D;
+            const uint32_t at = r * D + g * (D / 4);
+            if constexpr (D % 64 == 0) {
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) {
+                    const u32x4 w = *reinterpret_cast<const u32x4 *>(src + 16 * i + at);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) k[s][4 * i + e] = w[e];
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    const u32x2 w = *reinterpret_cast<const u32x2 *>(src + 8 * i + at);
+                    k[s][2 * i] = w[0];
+                    k[s][2 * i + 1] = w[1];
+                }
+            }
+        }
+    }
+
+    __device__ __forceinline__ void load_values(const KvAttnArgs &a, const Tile<B> &t, int head, int r, int g)
+    {
+#pragma unroll
+        for (int i = 0; i < Tile<B>::NB; ++i) {
+            const int8_t *src = a.c.vc + ((int64_t)t.page[i] * a.c.heads + head) * (B * D) + t.off / 4;
+            const uint32_t at = r * B + g * (B / 4);
+#pragma unroll
+            for (int n = 0; n < N; ++n, src += 16 * B) {
+                if constexpr (B == 16) {
+                    v[n][i] = *reinterpret_cast<const uint32_t *>(src + at);
+                } else if constexpr (B == 32) {
+                    const u32x2 w = *reinterpret_cast<const u32x2 *>(src + at);
+                    v[n][2 * i] = w[0];
+                    v[n][2 * i + 1] = w[1];
+                } else {
+                    const u32x4 w = *reinterpret_cast<const u32x4 *>(src + at);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[n][e] = w[e];
+                }
+            }
+        }
+    }
+};
+
+// Keys of group s of a tile that is not coded throughout, times the queries; fk becomes
+// the factor of the scores.
+template <int D, int B>
+__device__ __forceinline__ f32x4 scores_of_group(const KvAttnArgs &a, const Tile<B> &t, int s, int slot, int head,
+                                                 int64_t len, int r, int g, const f16x8 *qh, const f16x8 *ql, float fq,
+                                                 float &fk)
+{
+    f32x4 st = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int i = s / Tile<B>::GS, off = t.off + s % Tile<B>::GS * 16;
+    fk = 0.0f;
+    if (t.blk[i] < 0) return st;
+    if (t.page[i] >= 0) {
+        const int8_t *src = a.c.kc + ((int64_t)t.page[i] * a.c.heads + head) * (B * D) + (off + r) * D + g * (D / 4);
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) {
+            const u32x2 w = *reinterpret_cast<const u32x2 *>(src + 8 * k);
+            const f16x8 c = codes8(w[0], w[1]);
+            st = mfma16(c, qh[k], st);
+            st = mfma16(c, ql[k], st);
+        }
+        fk = t.k[i] * (1.0f / 127.0f) * fq;
+        return st;
+    }
+    // FP32 rows; what lies behind the last one may be anything
+    const float *src = a.c.kr + ((int64_t)slot * a.c.heads + head) * (2 * B * D) + ((t.blk[i] & 1) * B + off + r) * D + g * (D / 4);
+    const bool there = t.place(s) + r < len;
+    const int e = exponent(t.k[i]), shift = e == kNoScale ? 0 : 14 - e;
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) {
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; j += 4) {
+            const f32x4 y = *reinterpret_cast<const f32x4 *>(src + 8 * k + j);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) x[j + b] = there ? ldexpf(y[b], shift) : 0.0f;
+        }
+        f16x8 hi, lo;
+        pairs8(x, hi, lo);
+        st = mfma16(hi, qh[k], st);
+        st = mfma16(hi, ql[k], st);
+        st = mfma16(lo, qh[k], st);
+    }
+    fk = ldexpf(fq, -shift);
+    return st;
+}
+
+// The lane's four values of group s in row 16 n + r of V^T as FP16 pairs.
+template <int D, int B>
+__device__ __forceinline__ void values_of_group(const KvAttnArgs &a, const Tile<B> &t, int s, int n, int slot, int head,
+                                                int64_t len, int r, int g, f16x2 &h0, f16x2 &h1, f16x2 &l0, f16x2 &l1)
+{
+    const int i = s / Tile<B>::GS, off = t.off + s % Tile<B>::GS * 16;
+    h0 = h1 = l0 = l1 = f16x2{(_Float16)0.0f, (_Float16)0.0f};
+    if (t.blk[i] < 0) return;
+    if (t.page[i] >= 0) {
+        const int8_t *src = a.c.vc + ((int64_t)t.page[i] * a.c.heads + head) * (B * D) + (16 * n + r) * B + g * (B / 4) + off / 4;
+        codes4(*reinterpret_cast<const uint32_t *>(src), h0, h1);
+        return;
+    }
+    const float *src = a.c.vr + ((int64_t)slot * a.c.heads + head) * (2 * B * D) + (int64_t)(16 * n + r) * (2 * B) + (t.blk[i] & 1) * B + off + 4 * g;
+    const int e = exponent(t.v[i]), shift = e == kNoScale ? 0 : 7 - e;
+    const int64_t rows = len - t.place(s);
+    const f32x4 y = *reinterpret_cast<const f32x4 *>(src);
+    float x[4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) x[b] = 4 * g + b < rows ? ldexpf(y[b], shift) : 0.0f;
+    h0 = __builtin_convertvector((f32x2{x[0], x[1]}), f16x2);
+    h1 = __builtin_convertvector((f32x2{x[2], x[3]}), f16x2);
+    l0 = __builtin_convertvector((f32x2{x[0] - (float)h0[0], x[1] - (float)h0[1]}), f16x2);
+    l1 = __builtin_convertvector((f32x2{x[2] - (float)h1[0], x[3] - (float)h1[1]}), f16x2);
+}
 
 // Attention of 16 rows by the four waves of a workgroup, each on 64-token tiles of
 // its own: keys and values go from memory to registers and the matrix units without
-// LDS, and the waves' results are joined at the end.
+// LDS, and the waves' results are joined at the end.  The next tile's keys are asked
+// for as soon as this one's are in the matrix units, its values likewise, so that a
+// wave has 16 KiB on the way while it computes.
 template <int D, int B>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 2)
 kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
 {
     constexpr int KC = D / 32, N = D / 16, W = 4;
+    using T = Tile<B>;
     __shared__ float part_o[W][16][D + 4];
     __shared__ float part_m[W][16], part_l[W][16];
     __shared__ int part_row[16], part_head[16];
@@ -209,13 +400,12 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
 
     // tiles of this part: of the places from the tile of the first one seen, or of
     // the listed blocks
-    const int64_t listed = a.sel ? (int64_t)__builtin_amdgcn_readfirstlane(t.token) * a.c.heads + head : 0;
+    const int64_t listed = a.sel ? (int64_t)uniform(t.token) * a.c.heads + head : 0;
     const int32_t *list = a.sel + listed * a.n_sel;
     const int64_t base = a.sel ? 0 : t.first / 64;
     const int64_t end = a.sel ? ((int64_t)a.n_sel * B + 63) / 64 : t.last < t.first ? 0 : (int64_t)t.last / 64 + 1;
     const int64_t from = base + (int64_t)part * a.part_tiles;
     const int64_t to = from + a.part_tiles < end ? from + a.part_tiles : end;
-    const bool none = from >= to || t.last < t.first;
     const int slot = uniform(kv_slot(a.b, t.seq));
 
     f32x4 o[N];
@@ -224,7 +414,16 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
     float m = -__builtin_inff(), l = 0.0f;
     int ref = kNoScale;   // this row's o is in units of 2^(ref - 14) / 127
 
-    if (!none) {
+    if (from + wave < to && t.last >= t.first) {
+        Blocks<B> blocks;
+        blocks.load(a, t.s, t.seq, slot, head, list, from + wave, to, W);
+        T cur;
+        Codes<D, B> codes;
+        cur.take(blocks, 0, from + wave);
+        if (cur.coded) {
+            codes.load_keys(a, cur, head, r, g);
+            codes.load_values(a, cur, head, r, g);
+        }
         // the query row: lane (r, g) holds elements g D/4 .. of row r
         f16x8 qh[KC], ql[KC];
         float fq;
@@ -251,150 +450,82 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
             fq = ldexpf(a.scale * kLog2e, -shift);
         }
 
+        int at = 0;
         for (int64_t kt = from + wave; kt < to; kt += W) {
-            Group gr[4];
-            bool coded = true;
-            float fk[4], mv[4], mr[4];
-            int ev = kNoScale;
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const int64_t at = kt * 64 + 16 * s;
-                const int64_t entry = at / B;
-                gr[s].off = (int)(at % B);
-                gr[s].blk = (int)entry;
-                if (a.sel) gr[s].blk = entry < a.n_sel ? uniform(list[entry]) : -1;
-                gr[s].page = uniform(kv_page(a.b, t.seq, gr[s].blk));
-                if (gr[s].page < 0) gr[s].blk = -1;
-                const bool full = gr[s].blk >= 0 && (int64_t)gr[s].blk * B + B <= t.s.len;
-                if (gr[s].blk >= 0 && !full && slot < 0) gr[s].blk = -1;
-                coded &= full;
-                fk[s] = mv[s] = 0.0f;
-                if (gr[s].blk >= 0) {
-                    const float *sc = a.c.scales + ((int64_t)gr[s].page * a.c.heads + head) * 2;
-                    fk[s] = sc[0];
-                    mv[s] = sc[1];
+            T next = cur;
+            const bool more = kt + W < to;
+            if (more) {
+                if (++at == Blocks<B>::TILES) {
+                    at = 0;
+                    blocks.load(a, t.s, t.seq, slot, head, list, kt + W, to, W);
                 }
-                // (a row's units follow the blocks that it sees something of, and no others)
-                const int64_t t0 = (int64_t)gr[s].blk * B + gr[s].off;
-                mr[s] = gr[s].blk < 0 || t0 > t.hi || t0 + 15 < t.lo ? 0.0f : mv[s];
-                ev = max(ev, exponent(mr[s]));
+                next.take(blocks, at, kt + W);
             }
+            const bool ask = more && next.coded;
 
+            // scores
             f32x4 st[4];
-            f16x8 vh[N][2], vl[N][2];
-            if (coded) {
-                uint32_t kw[4][KC][2], vw[N][4];
-#pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const int8_t *src = a.c.kc + (((int64_t)gr[s].page * a.c.heads + head) * B + gr[s].off + r) * D + g * (D / 4);
-#pragma unroll
-                    for (int k = 0; k < KC; ++k) {
-                        const u32x2 w = *reinterpret_cast<const u32x2 *>(src + 8 * k);
-                        kw[s][k][0] = w[0];
-                        kw[s][k][1] = w[1];
-                    }
-                }
-#pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const int8_t *src = a.c.vc + (((int64_t)gr[s].page * a.c.heads + head) * D + r) * B + g * (B / 4) + gr[s].off / 4;
-#pragma unroll
-                    for (int n = 0; n < N; ++n) vw[n][s] = *reinterpret_cast<const uint32_t *>(src + n * (16 * B));
-                }
+            float fk[4];
+            if (cur.coded) {
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
                     st[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                     for (int k = 0; k < KC; ++k) {
-                        const f16x8 c = codes8(kw[s][k][0], kw[s][k][1]);
+                        const f16x8 c = codes8(codes.k[s][2 * k], codes.k[s][2 * k + 1]);
                         st[s] = mfma16(c, qh[k], st[s]);
                         st[s] = mfma16(c, ql[k], st[s]);
                     }
-                    fk[s] = fk[s] / 127.0f * fq;
+                    if (s & 1) __builtin_amdgcn_sched_barrier(0);   // (two groups' keys as FP16 at a time)
+                    fk[s] = cur.k[s / T::GS] * (1.0f / 127.0f) * fq;
                 }
-#pragma unroll
-                for (int n = 0; n < N; ++n)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) vh[n][c] = codes8(vw[n][2 * c], vw[n][2 * c + 1]);
             } else {
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
-                    st[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                    const bool held = gr[s].blk >= 0, full = held && (int64_t)gr[s].blk * B + B <= t.s.len;
-                    const int64_t ph = (int64_t)gr[s].page * a.c.heads + head;
-                    const int64_t ring = ((int64_t)slot * a.c.heads + head) * (2 * B * D);
-                    const int half = (gr[s].blk & 1) * B + gr[s].off;
-                    const int ek = exponent(fk[s]), es = exponent(mv[s]);
-                    // rows behind the last token hold anything
-                    const int rows = held ? (int)(t.s.len - ((int64_t)gr[s].blk * B + gr[s].off)) : 0;
-                    if (full) {
-                        const int8_t *src = a.c.kc + (ph * B + gr[s].off + r) * D + g * (D / 4);
-#pragma unroll
-                        for (int k = 0; k < KC; ++k) {
-                            const u32x2 w = *reinterpret_cast<const u32x2 *>(src + 8 * k);
-                            const f16x8 c = codes8(w[0], w[1]);
-                            st[s] = mfma16(c, qh[k], st[s]);
-                            st[s] = mfma16(c, ql[k], st[s]);
-                        }
-                        fk[s] = fk[s] / 127.0f * fq;
-                    } else if (held) {
-                        const float *src = a.c.kr + ring + (int64_t)(half + r) * D + g * (D / 4);
-                        const int shift = ek == kNoScale ? 0 : 14 - ek;
-#pragma unroll
-                        for (int k = 0; k < KC; ++k) {
-                            float x[8];
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) x[i] = r < rows ? ldexpf(src[8 * k + i], shift) : 0.0f;
-                            f16x8 hi, lo;
-                            pairs8(x, hi, lo);
-                            st[s] = mfma16(hi, qh[k], st[s]);
-                            st[s] = mfma16(hi, ql[k], st[s]);
-                            st[s] = mfma16(lo, qh[k], st[s]);
-                        }
-                        fk[s] = ldexpf(fq, -shift);
-                    }
-                    // values: the lane's four tokens of the group
-#pragma unroll
-                    for (int n = 0; n < N; ++n) {
-                        f16x2 h0 = {}, h1 = {}, l0 = {}, l1 = {};
-                        if (full) {
-                            const int8_t *src = a.c.vc + (ph * D + 16 * n + r) * B + g * (B / 4) + gr[s].off / 4;
-                            codes4(*reinterpret_cast<const uint32_t *>(src), h0, h1);
-                        } else if (held) {
-                            const float *src = a.c.vr + ring + (int64_t)(16 * n + r) * (2 * B) + half + 4 * g;
-                            const int shift = es == kNoScale ? 0 : 7 - es;
-                            float x[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) x[i] = 4 * g + i < rows ? ldexpf(src[i], shift) : 0.0f;
-                            h0 = __builtin_convertvector((f32x2{x[0], x[1]}), f16x2);
-                            h1 = __builtin_convertvector((f32x2{x[2], x[3]}), f16x2);
-                            l0 = __builtin_convertvector((f32x2{x[0] - (float)h0[0], x[1] - (float)h0[1]}), f16x2);
-                            l1 = __builtin_convertvector((f32x2{x[2] - (float)h1[0], x[3] - (float)h1[1]}), f16x2);
-                        }
-                        const int c = s >> 1, b = (s & 1) * 4;
-                        vh[n][c][b] = h0[0];
-                        vh[n][c][b + 1] = h0[1];
-                        vh[n][c][b + 2] = h1[0];
-                        vh[n][c][b + 3] = h1[1];
-                        vl[n][c][b] = l0[0];
-                        vl[n][c][b + 1] = l0[1];
-                        vl[n][c][b + 2] = l1[0];
-                        vl[n][c][b + 3] = l1[1];
-                    }
+                    st[s] = scores_of_group<D, B>(a, cur, s, slot, head, t.s.len, r, g, qh, ql, fq, fk[s]);
+                    __builtin_amdgcn_sched_barrier(0);   // (rows of one group at a time in registers)
                 }
             }
+            if (ask) codes.load_keys(a, next, head, r, g);
 
-            // scores in log2 units, and what a row does not see
-            float big = -__builtin_inff();
+            // in log2 units, and without what a row does not see
+            float big = -__builtin_inff(), vm[T::NB];
+            int ev = kNoScale;
+            bool all = cur.coded;
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const int64_t t0 = (int64_t)gr[s].blk * B + gr[s].off + 4 * g;
+            for (int i = 0; i < T::NB; ++i) {
+                const int64_t p0 = cur.place(i * T::GS);
+                all = all && p0 >= t.all_lo && p0 + T::GS * 16 - 1 <= t.all_hi;
+                vm[i] = cur.v[i];
+            }
+            if (all) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const bool seen = gr[s].blk >= 0 && t0 + i >= t.lo && t0 + i <= t.hi;
-                    st[s][i] = seen ? st[s][i] * fk[s] : -__builtin_inff();
-                    big = __builtin_fmaxf(big, st[s][i]);
+                for (int s = 0; s < 4; ++s)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        st[s][i] *= fk[s];
+                        big = __builtin_fmaxf(big, st[s][i]);
+                    }
+            } else {
+#pragma unroll
+                for (int i = 0; i < T::NB; ++i) {
+                    // (a row's units follow the blocks that it sees something of, and no others)
+                    const int64_t p0 = cur.place(i * T::GS);
+                    if (cur.blk[i] < 0 || p0 > t.hi || p0 + T::GS * 16 - 1 < t.lo) vm[i] = 0.0f;
+                }
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const int64_t p0 = cur.place(s) + 4 * g;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const bool seen = cur.blk[s / T::GS] >= 0 && p0 + i >= t.lo && p0 + i <= t.hi;
+                        st[s][i] = seen ? st[s][i] * fk[s] : -__builtin_inff();
+                        big = __builtin_fmaxf(big, st[s][i]);
+                    }
                 }
             }
+#pragma unroll
+            for (int i = 0; i < T::NB; ++i) ev = max(ev, exponent(vm[i]));
             const float mn = __builtin_fmaxf(m, max_over_groups(big));
             const float mz = mn == -__builtin_inff() ? 0.0f : mn;
             const float alpha = __builtin_amdgcn_exp2f(m - mz);
@@ -403,14 +534,15 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
             const float turn = ref == kNoScale ? alpha : ldexpf(alpha, ref - rn);
             m = mn;
             ref = rn;
+            if (__ballot(turn != 1.0f)) {
 #pragma unroll
-            for (int n = 0; n < N; ++n) o[n] *= turn;
-            float wv[4];   // the factor of a weight for the values of a group
+                for (int n = 0; n < N; ++n) o[n] *= turn;
+            }
+            float wv[T::NB];   // the factor of a weight for the values of a block
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const bool full = gr[s].blk >= 0 && (int64_t)gr[s].blk * B + B <= t.s.len;
-                const int es = exponent(mr[s]);
-                wv[s] = full ? ldexpf(mr[s], 14 - rn) : es == kNoScale ? 0.0f : ldexpf(127.0f, es + 7 - rn);
+            for (int i = 0; i < T::NB; ++i) {
+                const int e = exponent(vm[i]);
+                wv[i] = cur.page[i] >= 0 ? ldexpf(vm[i], 14 - rn) : e == kNoScale ? 0.0f : ldexpf(127.0f, e + 7 - rn);
             }
             float sum = 0.0f;
             f16x8 ph[2], pl[2];
@@ -419,21 +551,45 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
                 float p[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float e = __builtin_amdgcn_exp2f(st[2 * c + i / 4][i % 4] - mz);
+                    const int s = 2 * c + i / 4;
+                    const float e = __builtin_amdgcn_exp2f(st[s][i % 4] - mz);
                     sum += e;
-                    p[i] = e * wv[2 * c + i / 4];
+                    p[i] = e * wv[s / T::GS];
                 }
                 pairs8(p, ph[c], pl[c]);
             }
             l = l * alpha + sum;
+
+            // values
+            if (cur.coded) {
 #pragma unroll
-            for (int n = 0; n < N; ++n)
+                for (int n = 0; n < N; ++n) {
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    o[n] = mfma16(vh[n][c], ph[c], o[n]);
-                    o[n] = mfma16(vh[n][c], pl[c], o[n]);
-                    if (!coded) o[n] = mfma16(vl[n][c], ph[c], o[n]);
+                    for (int c = 0; c < 2; ++c) {
+                        const f16x8 v = codes8(codes.v[n][2 * c], codes.v[n][2 * c + 1]);
+                        o[n] = mfma16(v, ph[c], o[n]);
+                        o[n] = mfma16(v, pl[c], o[n]);
+                    }
+                    if (n & 1) __builtin_amdgcn_sched_barrier(0);
                 }
+            } else {
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        f16x2 h[4], x[4];
+                        values_of_group<D, B>(a, cur, 2 * c, n, slot, head, t.s.len, r, g, h[0], h[1], x[0], x[1]);
+                        values_of_group<D, B>(a, cur, 2 * c + 1, n, slot, head, t.s.len, r, g, h[2], h[3], x[2], x[3]);
+                        const f16x8 vh = {h[0][0], h[0][1], h[1][0], h[1][1], h[2][0], h[2][1], h[3][0], h[3][1]};
+                        const f16x8 vl = {x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
+                        o[n] = mfma16(vh, ph[c], o[n]);
+                        o[n] = mfma16(vh, pl[c], o[n]);
+                        o[n] = mfma16(vl, ph[c], o[n]);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+            }
+            if (ask) codes.load_values(a, next, head, r, g);
+            cur = next;
         }
     }
 
@@ -482,14 +638,16 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
     if (a.parts == 1 && a.lse && c0 == 0) a.lse[row] = log_sum(top, total);
 }
 
-// The parts of a row joined in ascending order, one wave to a row.
+// The parts of a row joined in ascending order, one wave to a row.  A lane holds the
+// maximum and the sum of one part, and eight parts' results are asked for at once.
 template <int D>
 __global__ void __launch_bounds__(256)
 kv_combine_kernel(KvAttnArgs a, int64_t wg0)
 {
+    constexpr int J = (D + 63) / 64, U = 8;
     const int lane = threadIdx.x & 63;
     const int64_t rows = (int64_t)a.b.tokens * a.c.heads * a.group;
-    const int64_t row = (wg0 + blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int64_t row = (wg0 + blockIdx.x) * 4 + uniform(threadIdx.x >> 6);
     if (row >= rows) return;
     const int64_t token = row / (a.c.heads * a.group), head_q = row % (a.c.heads * a.group);
     if (a.b.cu && (token < kv_first(a.b, 0) || token >= kv_first(a.b, a.b.seqs))) return;
@@ -498,21 +656,41 @@ kv_combine_kernel(KvAttnArgs a, int64_t wg0)
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, off));
     const float tz = top == -__builtin_inff() ? 0.0f : top;
-    float total = 0.0f, x[(D + 63) / 64] = {};
-    for (int p = 0; p < a.parts; ++p) {
-        const float *ml = a.ws_ml + ((int64_t)p * rows + row) * 2;
-        const float lp = ml[1];
-        if (lp == 0.0f) continue;
-        const float w = __builtin_amdgcn_exp2f(ml[0] - tz);
-        total += w * lp;
-        const float *src = a.ws_o + ((int64_t)p * rows + row) * D;
+    float total = 0.0f, x[J] = {};
+    for (int p0 = 0; p0 < a.parts; p0 += 64) {
+        float w = 0.0f, l = 0.0f;
+        if (p0 + lane < a.parts) {
+            const f32x2 ml = *reinterpret_cast<const f32x2 *>(a.ws_ml + ((int64_t)(p0 + lane) * rows + row) * 2);
+            w = __builtin_amdgcn_exp2f(ml[0] - tz);
+            l = ml[1];
+        }
+        uint64_t left = __ballot(l != 0.0f);   // (a sum that is no number is one too)
+        while (left) {
+            int at[U];
+            float y[U][J];
 #pragma unroll
-        for (int j = 0; j < (D + 63) / 64; ++j)
-            if (j * 64 + lane < D) x[j] += w * src[j * 64 + lane];
+            for (int u = 0; u < U; ++u) {
+                at[u] = left ? __builtin_ctzll(left) : -1;
+                left &= left - 1;
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+                    y[u][j] = at[u] >= 0 && j * 64 + lane < D
+                                  ? a.ws_o[((int64_t)(p0 + at[u]) * rows + row) * D + j * 64 + lane]
+                                  : 0.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (at[u] < 0) continue;
+                const float wu = from_lane(w, at[u]);
+                total += wu * from_lane(l, at[u]);
+#pragma unroll
+                for (int j = 0; j < J; ++j) x[j] += wu * y[u][j];
+            }
+        }
     }
     float *dst = a.out + token * a.out_token + head_q * a.out_head;
 #pragma unroll
-    for (int j = 0; j < (D + 63) / 64; ++j)
+    for (int j = 0; j < J; ++j)
         if (j * 64 + lane < D) dst[j * 64 + lane] = total == 0.0f ? 0.0f : x[j] / total;
     if (a.lse && lane == 0) a.lse[row] = log_sum(top, total);
 }
