@@ -323,114 +323,188 @@ __device__ __forceinline__ uint64_t score_key(double x)
 }
 constexpr uint64_t kLowest = 0x000fffffffffffffull;   // the key of -infinity
 
-constexpr int kSelectHeads = 8;   // queries scored at once
+typedef double f64x4 __attribute__((ext_vector_type(4)));
 
-// One workgroup per token and key/value head.  Every thread scores blocks of its
-// own: the FP64 sum over d in ascending order, so equal blocks score equally.  The
-// n-th best key is found digit by digit (8 bits each, a histogram in LDS), and one
-// wave writes the blocks above it, and the lowest of those equal to it, in order.
-template <int D>
-__global__ void __launch_bounds__(kThreads)
-kv_select_kernel(KvSelectArgs a, int B, int64_t wg0)
+constexpr int kSelectThreads = 512;
+
+// Key `i` of a lane: candidates lie 64 apart.  Up to kHeld of them are held in registers.
+constexpr int kHeld = 16;
+
+// How many candidates (n of them, in LDS at `key`) have a key of at least x.
+__device__ __forceinline__ int keys_from(const uint64_t *key, const uint64_t *held, int n, uint64_t x)
 {
-    extern __shared__ char lds[];
-    uint64_t *key = reinterpret_cast<uint64_t *>(lds);
-    __shared__ double q[kSelectHeads][D];
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t found[2];
-    const int64_t wg = wg0 + blockIdx.x;
-    const int64_t token = wg / a.c.heads;
-    const int head = (int)(wg % a.c.heads);
-    const int seq = kv_last_at_most(a.b.seqs, token, [&](int i) { return (int64_t)kv_first(a.b, i); });
-    const KvSeq s = kv_seq(a.b, seq);
-    if (token < s.first || token >= (int64_t)s.first + s.n) return;
-    int32_t *sel = a.sel + wg * a.n_sel;
-    const int64_t place = (int64_t)s.len - s.n + (token - s.first);
-    int64_t last = place < 0 ? -1 : place / B;
-    if (last >= a.b.cols) last = a.b.cols - 1;
-    const int nb = (int)last + 1;
-    if (nb <= a.n_sel) {   // all of them
-        for (int i = threadIdx.x; i < a.n_sel; i += kThreads) sel[i] = i < nb ? i : -1;
-        return;
-    }
-    // candidates lo .. hi - 1, of which r are taken; nb > n_sel >= keep_first + keep_last
-    const int lo = a.keep_first, hi = nb - a.keep_last, r = a.n_sel - a.keep_first - a.keep_last;
-    for (int g0 = 0; g0 < a.group && r > 0; g0 += kSelectHeads) {
-        const int ng = a.group - g0 < kSelectHeads ? a.group - g0 : kSelectHeads;
-        __syncthreads();
-        for (int i = threadIdx.x; i < kSelectHeads * D; i += kThreads) {
-            const int g = i / D, d = i % D;
-            // (queries behind the last one repeat the first: no score changes)
-            const int64_t h = (int64_t)head * a.group + g0 + (g < ng ? g : 0);
-            q[g][d] = (double)a.q[token * a.q_token + h * a.q_head + d];
+    int c = 0;
+    if (n <= 64 * kHeld) {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            if (i * 64 < n) c += __popcll(__ballot(held[i] >= x));
         }
-        __syncthreads();
-        for (int b = lo + threadIdx.x; b < hi; b += kThreads) {
-            const int page = kv_page(a.b, seq, b);
-            uint64_t best = kLowest;
-            if (page >= 0) {
-                const f32x4 *m = reinterpret_cast<const f32x4 *>(a.c.mean + ((int64_t)page * a.c.heads + head) * D);
-                double sum[kSelectHeads] = {};
-                for (int d = 0; d < D; d += 4) {
-                    const f32x4 x = m[d / 4];
+    } else {
+        const int lane = threadIdx.x & 63;
+        for (int i = 0; i < n; i += 64) c += __popcll(__ballot(i + lane < n && key[i + lane] >= x));
+    }
+    return c;
+}
+
+// The blocks of one token: the forced ones, and the r best of the n candidates whose
+// keys are in LDS.  One wave: the r-th largest key is found bit by bit from the first
+// bit in which the keys differ, ending where a threshold parts exactly r from the rest;
+// then the blocks above it, and the lowest of those equal to it, are written in order.
+__device__ __forceinline__ void pick_blocks(const uint64_t *key, int lo, int n, int nb, int r, int32_t *sel)
+{
+    const int lane = threadIdx.x & 63;
+    uint64_t held[kHeld], top = 0u;
+    int left = 0;
+    if (r > 0) {
+        uint64_t most = 0u, least = ~0ull;
+        if (n <= 64 * kHeld) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const double y = (double)x[e];
+            for (int i = 0; i < kHeld; ++i) held[i] = i * 64 + lane < n ? key[i * 64 + lane] : 0u;
+        }
+        for (int i = lane; i < n; i += 64) {
+            const uint64_t k = key[i];
+            most = k > most ? k : most;
+            least = k < least ? k : least;
+        }
 #pragma unroll
-                        for (int g = 0; g < kSelectHeads; ++g) sum[g] = __builtin_fma(q[g][d + e], y, sum[g]);
-                    }
-                }
-#pragma unroll
-                for (int g = 0; g < kSelectHeads; ++g) {
-                    const uint64_t u = score_key(sum[g]);
-                    best = u > best ? u : best;
-                }
+        for (int off = 32; off > 0; off >>= 1) {
+            const uint64_t x = __shfl_xor(most, off), y = __shfl_xor(least, off);
+            most = x > most ? x : most;
+            least = y < least ? y : least;
+        }
+        top = most;
+        if (most != least) {
+            int bit = 63 - __builtin_clzll(most ^ least);
+            top = bit == 63 ? 0u : most >> (bit + 1) << (bit + 1);
+            for (; bit >= 0; --bit) {
+                const uint64_t x = top | 1ull << bit;
+                const int c = keys_from(key, held, n, x);
+                if (c >= r) top = x;
+                if (c == r) break;
             }
-            if (g0 > 0 && key[b] > best) best = key[b];
-            key[b] = best;
         }
+        left = r - (top == ~0ull ? 0 : keys_from(key, held, n, top + 1));
     }
-    __syncthreads();
-    // the r-th largest key, and how many of its equals are taken
-    uint64_t top = 0u, mask = 0u;
-    uint32_t left = (uint32_t)r;
-    for (int shift = 56; shift >= 0 && r > 0; shift -= 8) {
-        for (int i = threadIdx.x; i < 256; i += kThreads) hist[i] = 0u;
-        __syncthreads();
-        for (int b = lo + threadIdx.x; b < hi; b += kThreads)
-            if ((key[b] & mask) == top) atomicAdd(&hist[(key[b] >> shift) & 255u], 1u);
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            uint32_t above = 0u;
-            int digit = 255;
-            while (digit > 0 && above + hist[digit] < left) above += hist[digit--];
-            found[0] = (uint32_t)digit;
-            found[1] = above;
-        }
-        __syncthreads();
-        top |= (uint64_t)found[0] << shift;
-        mask |= 255ull << shift;
-        left -= found[1];
-        __syncthreads();
-    }
-    if (threadIdx.x >= 64) return;
-    const int lane = threadIdx.x;
-    int at = 0;
-    uint32_t equals = 0u;
+    int at = 0, equals = 0;
     const uint64_t before = (1ull << lane) - 1;
     for (int b0 = 0; b0 < nb; b0 += 64) {
         const int b = b0 + lane;
-        const bool forced = b < nb && (b < lo || b >= hi);
-        const bool cand = r > 0 && b >= lo && b < hi;
-        const uint64_t x = cand ? key[b] : 0u;
+        const bool forced = b < nb && (b < lo || b >= lo + n);
+        const bool cand = r > 0 && b >= lo && b < lo + n;
+        const uint64_t x = cand ? key[b - lo] : 0u;
         const uint64_t same = __ballot(cand && x == top);
-        const uint32_t rank = equals + (uint32_t)__popcll(same & before);
-        const bool take = forced || (cand && (x > top || (x == top && rank < left)));
+        const bool take = forced || (cand && (x > top || (x == top && equals + __popcll(same & before) < left)));
         const uint64_t taken = __ballot(take);
         if (take) sel[at + __popcll(taken & before)] = b;
         at += __popcll(taken);
-        equals += (uint32_t)__popcll(same);
+        equals += __popcll(same);
     }
+}
+
+// One workgroup per key/value head and `slots` tokens of one sequence (1 or 4).
+//
+// Scores are FP64 matrix products: 16 rows of queries by 16 blocks, dim in steps of
+// four that a lane has D/4 elements apart, so that its part of a mean is contiguous.
+// A lane of the result holds rows lane / 16 + 4 v of one block.  With four tokens the
+// row lane / 16 + 4 v is query v of token lane / 16 (queries behind the last repeat
+// it), so the maximum over a token's queries is taken within the lane; with one
+// token the 16 rows are its queries.  The order of the sum is the same for every block,
+// so equal blocks score equally.
+template <int D>
+__global__ void __launch_bounds__(kSelectThreads)
+kv_select_kernel(KvSelectArgs a, int B, int slots, int64_t wg0)
+{
+    extern __shared__ char lds[];
+    uint64_t *key = reinterpret_cast<uint64_t *>(lds);   // [slots][cols]
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, kk = lane >> 4;
+    const int64_t wg = wg0 + blockIdx.x;
+    const int64_t u = wg / a.c.heads;
+    const int head = (int)(wg % a.c.heads);
+    int seq;
+    int64_t first;   // token of slot 0
+    if (slots == 1) {
+        first = u;
+        seq = kv_last_at_most(a.b.seqs, u, [&](int i) { return (int64_t)kv_first(a.b, i); });
+    } else {
+        seq = kv_last_at_most(a.b.seqs, u, [&](int i) { return kv_tile(a.b, 1, 4, i); });
+        first = kv_first(a.b, seq) + (u - kv_tile(a.b, 1, 4, seq)) * 4;
+    }
+    const KvSeq s = kv_seq(a.b, seq);
+    if (first < s.first || first >= (int64_t)s.first + s.n) return;
+    const int tokens = (int)((int64_t)s.first + s.n - first < slots ? s.first + s.n - first : slots);
+    // blocks up to a token's own
+    auto blocks_of = [&](int slot) {
+        const int64_t place = (int64_t)s.len - s.n + (first + slot - s.first);
+        const int64_t nb = place < 0 ? 0 : place / B + 1;
+        return (int)(nb < a.b.cols ? nb : a.b.cols);
+    };
+    const int lo = a.keep_first, r = a.n_sel - a.keep_first - a.keep_last;
+    const int most = blocks_of(tokens - 1), hi = most - a.keep_last;
+    if (most > a.n_sel && r > 0) {
+        const int per = slots == 1 ? 16 : 4;   // queries of a token in 16 rows
+        for (int g0 = 0; g0 < a.group; g0 += per) {
+            const int slot = slots == 1 ? 0 : col % 4, g = g0 + (slots == 1 ? col : col / 4);
+            const int64_t token = first + (slot < tokens ? slot : tokens - 1);
+            const float *qs = a.q + token * a.q_token + ((int64_t)head * a.group + (g < a.group ? g : a.group - 1)) * a.q_head + kk * (D / 4);
+            double q[D / 4];
+#pragma unroll
+            for (int i = 0; i < D / 4; ++i) q[i] = (double)qs[i];
+            auto page_of = [&](int b0) { return b0 + col < hi ? kv_page(a.b, seq, b0 + col) : -1; };
+            auto mean_of = [&](int page, f32x4 *m) {
+                const f32x4 *src = reinterpret_cast<const f32x4 *>(a.c.mean + ((int64_t)page * a.c.heads + head) * D + kk * (D / 4));
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) m[i] = page >= 0 ? src[i] : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            };
+            constexpr int STEP = kSelectThreads / 64 * 16;
+            int b0 = lo + wave * 16;
+            int page = b0 < hi ? page_of(b0) : -1, next = b0 + STEP < hi ? page_of(b0 + STEP) : -1;
+            f32x4 m[D / 16];
+            mean_of(page, m);
+            for (; b0 < hi; b0 += STEP) {
+                // the next tile's means and the page behind it are on the way
+                f32x4 m2[D / 16];
+                mean_of(next, m2);
+                const int after = b0 + 2 * STEP < hi ? page_of(b0 + 2 * STEP) : -1;
+                f64x4 sum = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+                for (int i = 0; i < D / 4; ++i)
+                    sum = __builtin_amdgcn_mfma_f64_16x16x4f64(q[i], (double)m[i / 4][i % 4], sum, 0, 0, 0);
+                uint64_t best = kLowest;
+                if (page >= 0) {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const double x = sum[v];
+                        const uint64_t k = score_key(x);
+                        best = k > best ? k : best;
+                    }
+                }
+                if (slots == 1) {
+#pragma unroll
+                    for (int off = 16; off < 64; off <<= 1) {
+                        const uint64_t k = __shfl_xor(best, off);
+                        best = k > best ? k : best;
+                    }
+                }
+                if (kk < slots && b0 + col < hi) {
+                    uint64_t *at = key + (int64_t)kk * a.b.cols + (b0 + col - lo);
+                    *at = g0 > 0 && *at > best ? *at : best;
+                }
+                page = next;
+                next = after;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) m[i] = m2[i];
+            }
+        }
+    }
+    __syncthreads();
+    if (wave >= tokens) return;
+    const int nb = blocks_of(wave);
+    int32_t *sel = a.sel + ((first + wave) * a.c.heads + head) * a.n_sel;
+    if (nb <= a.n_sel) {   // all of them
+        for (int i = lane; i < a.n_sel; i += 64) sel[i] = i < nb ? i : -1;
+        return;
+    }
+    pick_blocks(key + (int64_t)wave * a.b.cols, lo, nb - a.keep_last - lo, nb, r, sel);
 }
 
 template <int D, int B>
@@ -465,8 +539,10 @@ hipError_t launch_kv_read(const KvSeqs &b, const KvCache &c, float *k, float *v,
 
 hipError_t launch_kv_select(const KvSelectArgs &a, hipStream_t stream)
 {
-    const int64_t n = (int64_t)a.b.tokens * a.c.heads;
-    const size_t lds = (size_t)a.b.cols * sizeof(uint64_t);
+    // four tokens of a sequence share its means, where their keys fit in LDS
+    const int slots = a.b.cu && a.b.cols * 4 <= kMaxSelectBlocks ? 4 : 1;
+    const int64_t n = (slots == 4 ? kv_tiles(a.b.tokens, a.b.seqs, 1, 4) : a.b.tokens) * a.c.heads;
+    const size_t lds = (size_t)a.b.cols * slots * sizeof(uint64_t);
     if (lds > 32768) {   // beyond what a kernel may ask for by itself
         const void *f = a.c.dim == 64   ? reinterpret_cast<const void *>(kv_select_kernel<64>)
                         : a.c.dim == 96 ? reinterpret_cast<const void *>(kv_select_kernel<96>)
@@ -476,13 +552,13 @@ hipError_t launch_kv_select(const KvSelectArgs &a, hipStream_t stream)
         if (err != hipSuccess) return err;
     }
     return in_parts(n, [&](int64_t at, unsigned m) {
-        const dim3 grid(m), block(kThreads);
+        const dim3 grid(m), block(kSelectThreads);
         if (a.c.dim == 64)
-            hipLaunchKernelGGL(kv_select_kernel<64>, grid, block, lds, stream, a, a.c.block, at);
+            hipLaunchKernelGGL(kv_select_kernel<64>, grid, block, lds, stream, a, a.c.block, slots, at);
         else if (a.c.dim == 96)
-            hipLaunchKernelGGL(kv_select_kernel<96>, grid, block, lds, stream, a, a.c.block, at);
+            hipLaunchKernelGGL(kv_select_kernel<96>, grid, block, lds, stream, a, a.c.block, slots, at);
         else
-            hipLaunchKernelGGL(kv_select_kernel<128>, grid, block, lds, stream, a, a.c.block, at);
+            hipLaunchKernelGGL(kv_select_kernel<128>, grid, block, lds, stream, a, a.c.block, slots, at);
     });
 }
 
