@@ -185,6 +185,7 @@ constexpr int64_t kMaxSelectBlocks = 16384;
 // How a call of heal_kv_attention is cut (host only).
 struct KvPlan {
     bool by_token;               // a row tile holds one token's queries
+    bool wide;                   // 128-row tiles
     int64_t tiles;               // row tiles of the grid
     int32_t parts, part_tiles;
     int64_t bytes;               // of workspace

@@ -25,6 +25,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int64_t kWantedWorkgroups = 1024;
+constexpr int64_t kWideRows = 64;
 constexpr int kNoScale = -100000;   // no value block with a scale seen yet
 
 __device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c)
@@ -96,66 +97,92 @@ __device__ __forceinline__ float sum_over_groups(float x)
     return x + __shfl_xor(x, 32);
 }
 
-// A row tile: 16 rows, one for each lane % 16.
+__device__ __forceinline__ f32x4 load4(const float *p, bool vec)
+{
+    if (vec) return *reinterpret_cast<const f32x4 *>(p);
+    return f32x4{p[0], p[1], p[2], p[3]};
+}
+
+// A row tile: R rows (token, query of the head) of one sequence.
 struct Rows {
     KvSeq s;
-    int32_t seq;
-    int32_t token;   // of this lane's row, or -1 where there is none
-    int32_t head_q;
-    int32_t lo, hi;  // the places it sees: lo .. hi (none where hi < lo)
-    int32_t first, last;   // ... one row or another
-    int32_t all_lo, all_hi;   // ... all rows
+    int32_t seq, row0, rows;   // row0: of the sequence's rows; how many the tile has
 };
 
-// Finds the rows of tile u of a key/value head.  Returns false where the tile has none.
+// Finds the rows of tile u.  Returns false where the tile has none.
 template <int R>
-__device__ __forceinline__ bool find_rows(const KvAttnArgs &a, bool by_token, int64_t u, int head, int r,
-                                          Rows &t)
+__device__ __forceinline__ bool find_rows(const KvAttnArgs &a, bool by_token, int64_t u, Rows &t)
 {
-    int32_t row0, rows;
     if (by_token) {
         const int per = (a.group + R - 1) / R;
         const int64_t token = u / per;
-        t.seq = a.b.cu ? kv_last_at_most(a.b.seqs, token, [&](int i) { return (int64_t)kv_first(a.b, i); })
-                       : (int)token;
-        t.seq = uniform(t.seq);
+        t.seq = uniform(a.b.cu ? kv_last_at_most(a.b.seqs, token, [&](int i) { return (int64_t)kv_first(a.b, i); })
+                               : (int)token);
         t.s = uniform_seq(a.b, t.seq);
         if (token < t.s.first || token >= (int64_t)t.s.first + t.s.n) return false;
-        row0 = (int)(u % per) * R;
-        rows = a.group - row0 < R ? a.group - row0 : R;
-        row0 += (int)(token - t.s.first) * a.group;
+        t.row0 = (int)(u % per) * R;
+        t.rows = a.group - t.row0 < R ? a.group - t.row0 : R;
+        t.row0 += (int)(token - t.s.first) * a.group;
     } else {
-        t.seq = kv_last_at_most(a.b.seqs, u, [&](int i) { return kv_tile(a.b, a.group, R, i); });
-        t.seq = uniform(t.seq);
+        t.seq = uniform(kv_last_at_most(a.b.seqs, u, [&](int i) { return kv_tile(a.b, a.group, R, i); }));
         t.s = uniform_seq(a.b, t.seq);
         const int64_t j = u - kv_tile(a.b, a.group, R, t.seq);
         const int64_t n = (int64_t)t.s.n * a.group;
         if (j < 0 || j * R >= n) return false;
-        row0 = (int)(j * R);
-        rows = n - row0 < R ? (int)(n - row0) : R;
-    }
-    const int64_t end = (int64_t)a.b.cols * a.c.block;   // places that the table has
-    auto bounds = [&](int row, int32_t &lo, int32_t &hi) {
-        const int64_t place = (int64_t)t.s.len - t.s.n + row / a.group;
-        int64_t h = a.causal ? place : t.s.len - 1, l = a.window > 0 ? place - a.window + 1 : 0;
-        if (place < 0) h = -1;
-        if (h >= t.s.len) h = t.s.len - 1;
-        if (h >= end) h = end - 1;
-        lo = (int32_t)(l < 0 ? 0 : l);
-        hi = (int32_t)h;
-    };
-    bounds(row0, t.first, t.all_hi);
-    bounds(row0 + rows - 1, t.all_lo, t.last);
-    t.token = -1;
-    t.lo = 0;
-    t.hi = -1;
-    t.head_q = 0;
-    if (r < rows) {
-        bounds(row0 + r, t.lo, t.hi);
-        t.token = t.s.first + (row0 + r) / a.group;
-        t.head_q = head * a.group + (row0 + r) % a.group;
+        t.row0 = (int)(j * R);
+        t.rows = n - t.row0 < R ? (int)(n - t.row0) : R;
     }
     return true;
+}
+
+// The places lo .. hi that a row of the sequence sees (none where hi < lo).
+__device__ __forceinline__ void row_sees(const KvAttnArgs &a, const KvSeq &s, int row, int32_t &lo, int32_t &hi)
+{
+    const int64_t end = (int64_t)a.b.cols * a.c.block;   // places that the table has
+    const int64_t place = (int64_t)s.len - s.n + row / a.group;
+    int64_t h = a.causal ? place : s.len - 1, l = a.window > 0 ? place - a.window + 1 : 0;
+    if (place < 0) h = -1;
+    if (h >= s.len) h = s.len - 1;
+    if (h >= end) h = end - 1;
+    lo = (int32_t)(l < 0 ? 0 : l);
+    hi = (int32_t)h;
+}
+
+// ... that one or another of rows row0 .. row0 + rows - 1 sees, and that all of them see.
+struct Span {
+    int32_t first, last, all_lo, all_hi;
+};
+__device__ __forceinline__ Span rows_see(const KvAttnArgs &a, const KvSeq &s, int row0, int rows)
+{
+    Span x;
+    row_sees(a, s, row0, x.first, x.all_hi);
+    row_sees(a, s, row0 + rows - 1, x.all_lo, x.last);
+    return Span{uniform(x.first), uniform(x.last), uniform(x.all_lo), uniform(x.all_hi)};
+}
+
+// A query row, of which the lane takes the D/4 elements from g D/4 on, as FP16 pairs of
+// the row scaled by a power of two; its scores' factor (log2 units, not negative: the
+// scale's sign goes to the row).  Rows that are not there (src null) are zeros.
+template <int D>
+__device__ __forceinline__ float load_query(const KvAttnArgs &a, const float *src, f16x8 *qh, f16x8 *ql)
+{
+    float x[D / 4], big = 0.0f;
+#pragma unroll
+    for (int i = 0; i < D / 4; i += 4) {
+        f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (src) v = load4(src + i, a.vec);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[i + e] = a.scale < 0.0f ? -v[e] : v[e];
+    }
+#pragma unroll
+    for (int i = 0; i < D / 4; ++i) big = __builtin_fmaxf(big, __builtin_fabsf(x[i]));
+    const int e = exponent(max_over_groups(big));
+    const int shift = e == kNoScale ? 0 : 14 - e;
+#pragma unroll
+    for (int i = 0; i < D / 4; ++i) x[i] = ldexpf(x[i], shift);
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) pairs8(x + 8 * k, qh[k], ql[k]);
+    return ldexpf(__builtin_fabsf(a.scale) * kLog2e, -shift);
 }
 
 // ln of the sum that the maximum m (log2 units) and the sum l stand for.
@@ -174,12 +201,6 @@ __device__ __forceinline__ void store4(float *p, f32x4 x, bool vec)
         p[2] = x[2];
         p[3] = x[3];
     }
-}
-
-__device__ __forceinline__ float4 load16(const float *p, bool vec)
-{
-    if (vec) return *reinterpret_cast<const float4 *>(p);
-    return float4{p[0], p[1], p[2], p[3]};
 }
 
 // The blocks of a wave's next tiles, one to a lane: a tile of 64 tokens has EPT of
@@ -241,16 +262,84 @@ struct Tile {
             coded = coded && blk[i] >= 0 && page[i] >= 0;
         }
     }
+    __device__ __forceinline__ int blk_of(int s) const { return pick(blk, s); }
+    __device__ __forceinline__ int page_of(int s) const { return pick(page, s); }
+    __device__ __forceinline__ float key_of(int s) const { return pick(k, s); }
+    __device__ __forceinline__ float value_of(int s) const { return pick(v, s); }
+    // of the block of group s, which need not be a constant
+    template <class X>
+    static __device__ __forceinline__ X pick(const X *x, int s)
+    {
+        X y = x[0];
+#pragma unroll
+        for (int i = 1; i < NB; ++i) y = s / GS == i ? x[i] : y;
+        return y;
+    }
+    // the factor of the scores with block i, but for the query's
+    __device__ __forceinline__ float key_factor(int i) const
+    {
+        if (blk[i] < 0) return 0.0f;
+        if (page[i] >= 0) return k[i] * (1.0f / 127.0f);
+        const int e = exponent(k[i]);
+        return ldexpf(1.0f, e == kNoScale ? 0 : e - 14);
+    }
     // place of the first token of group s
     __device__ __forceinline__ int64_t place(int s) const
     {
-        return (int64_t)blk[s / GS] * B + off + s % GS * 16;
+        return (int64_t)blk_of(s) * B + off + s % GS * 16;
     }
 };
 
-// Codes of a tile as they come from memory, in the registers of one lane: of keys, the
-// D/4 bytes of row r of each group that belong to lanes g; of values, of row 16 n + r
-// of V^T the four bytes of each group that do.
+// Codes as they come from memory, in the registers of one lane: of the keys of group
+// s, the D/4 bytes of row r that belong to lanes g; of row 16 n + r of V^T, the four
+// bytes of each group that do.  (The block's address is the wave's, the lane's part an
+// unsigned 32-bit offset: no 64-bit address per lane.)
+template <int D, int B>
+__device__ __forceinline__ void load_group_keys(const KvAttnArgs &a, const Tile<B> &t, int s, int head, int r, int g,
+                                                uint32_t *k)
+{
+    const int8_t *src = a.c.kc + ((int64_t)t.page_of(s) * a.c.heads + head) * (B * D) + (t.off + s % Tile<B>::GS * 16) * D;
+    const uint32_t at = r * D + g * (D / 4);
+    if constexpr (D % 64 == 0) {
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(src + 16 * i + at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) k[4 * i + e] = w[e];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            const u32x2 w = *reinterpret_cast<const u32x2 *>(src + 8 * i + at);
+            k[2 * i] = w[0];
+            k[2 * i + 1] = w[1];
+        }
+    }
+}
+
+template <int D, int B>
+__device__ __forceinline__ void load_column_values(const KvAttnArgs &a, const Tile<B> &t, int n, int head, int r, int g,
+                                                   uint32_t *v)
+{
+    const uint32_t at = r * B + g * (B / 4);
+#pragma unroll
+    for (int i = 0; i < Tile<B>::NB; ++i) {
+        const int8_t *src = a.c.vc + ((int64_t)t.page[i] * a.c.heads + head) * (B * D) + t.off / 4 + n * (16 * B);
+        if constexpr (B == 16) {
+            v[i] = *reinterpret_cast<const uint32_t *>(src + at);
+        } else if constexpr (B == 32) {
+            const u32x2 w = *reinterpret_cast<const u32x2 *>(src + at);
+            v[2 * i] = w[0];
+            v[2 * i + 1] = w[1];
+        } else {
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(src + at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = w[e];
+        }
+    }
+}
+
+// The codes of a whole tile.
 template <int D, int B>
 struct Codes {
     static constexpr int N = D / 16;
@@ -259,122 +348,205 @@ struct Codes {
     __device__ __forceinline__ void load_keys(const KvAttnArgs &a, const Tile<B> &t, int head, int r, int g)
     {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int8_t *src = a.c.kc + ((int64_t)t.page[s / Tile<B>::GS] * a.c.heads + head) * (B * D) +
-                                (t.off + s % Tile<B>::GS * 16) * D;
-            const uint32_t at = r * D + g * (D / 4);
-            if constexpr (D % 64 == 0) {
-#pragma unroll
-                for (int i = 0; i < D / 64; ++i) {
-                    const u32x4 w = *reinterpret_cast<const u32x4 *>(src + 16 * i + at);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) k[s][4 * i + e] = w[e];
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < D / 32; ++i) {
-                    const u32x2 w = *reinterpret_cast<const u32x2 *>(src + 8 * i + at);
-                    k[s][2 * i] = w[0];
-                    k[s][2 * i + 1] = w[1];
-                }
-            }
-        }
+        for (int s = 0; s < 4; ++s) load_group_keys<D, B>(a, t, s, head, r, g, k[s]);
     }
-
     __device__ __forceinline__ void load_values(const KvAttnArgs &a, const Tile<B> &t, int head, int r, int g)
     {
 #pragma unroll
-        for (int i = 0; i < Tile<B>::NB; ++i) {
-            const int8_t *src = a.c.vc + ((int64_t)t.page[i] * a.c.heads + head) * (B * D) + t.off / 4;
-            const uint32_t at = r * B + g * (B / 4);
-#pragma unroll
-            for (int n = 0; n < N; ++n, src += 16 * B) {
-                if constexpr (B == 16) {
-                    v[n][i] = *reinterpret_cast<const uint32_t *>(src + at);
-                } else if constexpr (B == 32) {
-                    const u32x2 w = *reinterpret_cast<const u32x2 *>(src + at);
-                    v[n][2 * i] = w[0];
-                    v[n][2 * i + 1] = w[1];
-                } else {
-                    const u32x4 w = *reinterpret_cast<const u32x4 *>(src + at);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[n][e] = w[e];
-                }
-            }
-        }
+        for (int n = 0; n < N; ++n) load_column_values<D, B>(a, t, n, head, r, g, v[n]);
     }
 };
 
-// Keys of group s of a tile that is not coded throughout, times the queries; fk becomes
-// the factor of the scores.
-template <int D, int B>
-__device__ __forceinline__ f32x4 scores_of_group(const KvAttnArgs &a, const Tile<B> &t, int s, int slot, int head,
-                                                 int64_t len, int r, int g, const f16x8 *qh, const f16x8 *ql, float fq,
-                                                 float &fk)
+// Keys of group s of a tile that is not coded throughout, as FP16 pairs: f(k, hi, lo)
+// for each chunk of 32 elements.
+template <int D, int B, class F>
+__device__ __forceinline__ void keys_of_group(const KvAttnArgs &a, const Tile<B> &t, int s, int slot, int head,
+                                              int64_t len, int r, int g, F f)
 {
-    f32x4 st = {0.0f, 0.0f, 0.0f, 0.0f};
-    const int i = s / Tile<B>::GS, off = t.off + s % Tile<B>::GS * 16;
-    fk = 0.0f;
-    if (t.blk[i] < 0) return st;
-    if (t.page[i] >= 0) {
-        const int8_t *src = a.c.kc + ((int64_t)t.page[i] * a.c.heads + head) * (B * D) + (off + r) * D + g * (D / 4);
+    const f16x8 zero = {};
+    const int blk = t.blk_of(s), page = t.page_of(s), off = t.off + s % Tile<B>::GS * 16;
+    if (blk < 0) {
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) f(k, zero, zero);
+    } else if (page >= 0) {
+        const int8_t *src = a.c.kc + ((int64_t)page * a.c.heads + head) * (B * D) + (off + r) * D + g * (D / 4);
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
             const u32x2 w = *reinterpret_cast<const u32x2 *>(src + 8 * k);
-            const f16x8 c = codes8(w[0], w[1]);
-            st = mfma16(c, qh[k], st);
-            st = mfma16(c, ql[k], st);
+            f(k, codes8(w[0], w[1]), zero);
         }
-        fk = t.k[i] * (1.0f / 127.0f) * fq;
-        return st;
-    }
-    // FP32 rows; what lies behind the last one may be anything
-    const float *src = a.c.kr + ((int64_t)slot * a.c.heads + head) * (2 * B * D) + ((t.blk[i] & 1) * B + off + r) * D + g * (D / 4);
-    const bool there = t.place(s) + r < len;
-    const int e = exponent(t.k[i]), shift = e == kNoScale ? 0 : 14 - e;
+    } else {
+        // FP32 rows; what lies behind the last one may be anything
+        const float *src = a.c.kr + ((int64_t)slot * a.c.heads + head) * (2 * B * D) + ((blk & 1) * B + off + r) * D + g * (D / 4);
+        const bool there = t.place(s) + r < len;
+        const int e = exponent(t.key_of(s)), shift = e == kNoScale ? 0 : 14 - e;
 #pragma unroll
-    for (int k = 0; k < D / 32; ++k) {
-        float x[8];
+        for (int k = 0; k < D / 32; ++k) {
+            float x[8];
 #pragma unroll
-        for (int j = 0; j < 8; j += 4) {
-            const f32x4 y = *reinterpret_cast<const f32x4 *>(src + 8 * k + j);
+            for (int j = 0; j < 8; j += 4) {
+                const f32x4 y = *reinterpret_cast<const f32x4 *>(src + 8 * k + j);
 #pragma unroll
-            for (int b = 0; b < 4; ++b) x[j + b] = there ? ldexpf(y[b], shift) : 0.0f;
+                for (int b = 0; b < 4; ++b) x[j + b] = there ? ldexpf(y[b], shift) : 0.0f;
+            }
+            f16x8 hi, lo;
+            pairs8(x, hi, lo);
+            f(k, hi, lo);
         }
-        f16x8 hi, lo;
-        pairs8(x, hi, lo);
-        st = mfma16(hi, qh[k], st);
-        st = mfma16(hi, ql[k], st);
-        st = mfma16(lo, qh[k], st);
     }
-    fk = ldexpf(fq, -shift);
-    return st;
 }
 
-// The lane's four values of group s in row 16 n + r of V^T as FP16 pairs.
+// The lane's values of groups 2 c and 2 c + 1 in row 16 n + r of V^T, as FP16 pairs.
 template <int D, int B>
-__device__ __forceinline__ void values_of_group(const KvAttnArgs &a, const Tile<B> &t, int s, int n, int slot, int head,
-                                                int64_t len, int r, int g, f16x2 &h0, f16x2 &h1, f16x2 &l0, f16x2 &l1)
+__device__ __forceinline__ void values_of_half(const KvAttnArgs &a, const Tile<B> &t, int c, int n, int slot, int head,
+                                               int64_t len, int r, int g, f16x8 &hi, f16x8 &lo)
 {
-    const int i = s / Tile<B>::GS, off = t.off + s % Tile<B>::GS * 16;
-    h0 = h1 = l0 = l1 = f16x2{(_Float16)0.0f, (_Float16)0.0f};
-    if (t.blk[i] < 0) return;
-    if (t.page[i] >= 0) {
-        const int8_t *src = a.c.vc + ((int64_t)t.page[i] * a.c.heads + head) * (B * D) + (16 * n + r) * B + g * (B / 4) + off / 4;
-        codes4(*reinterpret_cast<const uint32_t *>(src), h0, h1);
-        return;
-    }
-    const float *src = a.c.vr + ((int64_t)slot * a.c.heads + head) * (2 * B * D) + (int64_t)(16 * n + r) * (2 * B) + (t.blk[i] & 1) * B + off + 4 * g;
-    const int e = exponent(t.v[i]), shift = e == kNoScale ? 0 : 7 - e;
-    const int64_t rows = len - t.place(s);
-    const f32x4 y = *reinterpret_cast<const f32x4 *>(src);
-    float x[4];
+    float x[8];
+    hi = lo = f16x8{};
+    bool pairs = false;
 #pragma unroll
-    for (int b = 0; b < 4; ++b) x[b] = 4 * g + b < rows ? ldexpf(y[b], shift) : 0.0f;
-    h0 = __builtin_convertvector((f32x2{x[0], x[1]}), f16x2);
-    h1 = __builtin_convertvector((f32x2{x[2], x[3]}), f16x2);
-    l0 = __builtin_convertvector((f32x2{x[0] - (float)h0[0], x[1] - (float)h0[1]}), f16x2);
-    l1 = __builtin_convertvector((f32x2{x[2] - (float)h1[0], x[3] - (float)h1[1]}), f16x2);
+    for (int j = 0; j < 2; ++j) {
+        const int s = 2 * c + j, blk = t.blk_of(s), page = t.page_of(s), off = t.off + s % Tile<B>::GS * 16;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) x[4 * j + b] = 0.0f;
+        if (blk < 0) continue;
+        if (page >= 0) {
+            const int8_t *src = a.c.vc + ((int64_t)page * a.c.heads + head) * (B * D) + (16 * n + r) * B + g * (B / 4) + off / 4;
+            const uint32_t w = *reinterpret_cast<const uint32_t *>(src);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) x[4 * j + b] = (float)(int8_t)(w >> (8 * b));
+        } else {
+            const float *src = a.c.vr + ((int64_t)slot * a.c.heads + head) * (2 * B * D) + (int64_t)(16 * n + r) * (2 * B) + (blk & 1) * B + off + 4 * g;
+            const int e = exponent(t.value_of(s)), shift = e == kNoScale ? 0 : 7 - e;
+            const int64_t rows = len - t.place(s);
+            const f32x4 y = *reinterpret_cast<const f32x4 *>(src);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) x[4 * j + b] = 4 * g + b < rows ? ldexpf(y[b], shift) : 0.0f;
+        }
+        pairs = true;
+    }
+    if (pairs) pairs8(x, hi, lo);
+}
+
+// Where a row's result goes: its place in out, or in the workspace of its part.
+struct Place {
+    int64_t row;   // of lse
+    float *dst, *ml;
+
+    // maximum and sum
+    __device__ __forceinline__ void sums(const KvAttnArgs &a, float m, float l) const
+    {
+        if (a.parts > 1) {
+            ml[0] = m;
+            ml[1] = l;
+        } else if (a.lse) {
+            a.lse[row] = log_sum(m, l);
+        }
+    }
+    // columns c .. c + 3, to be divided by the sum l at the end
+    __device__ __forceinline__ void store(const KvAttnArgs &a, int c, f32x4 x, float l) const
+    {
+        if (a.parts == 1) x = l == 0.0f ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : x / l;
+        store4(dst + c, x, a.parts > 1 || a.vec);
+    }
+};
+
+__device__ __forceinline__ Place place_of(const KvAttnArgs &a, int64_t token, int head_q, int part)
+{
+    const int64_t heads = (int64_t)a.c.heads * a.group, rows = a.b.tokens * heads;
+    Place p;
+    p.row = token * heads + head_q;
+    const int64_t at = part * rows + p.row;
+    p.ml = a.ws_ml + at * 2;
+    p.dst = a.parts > 1 ? a.ws_o + at * a.c.dim : a.out + token * a.out_token + head_q * a.out_head;
+    return p;
+}
+
+// One row's running softmax: the maximum of its scores (log2 units), the lane's part of
+// the sum of exp2(score - m), and the units of its output, 2^(ref - 14) / 127.
+struct Soft {
+    float m, l;
+    int ref;
+};
+
+// A tile's scores become weights.  st: the lane's scores, of tokens 4 g + i of group s,
+// before their factors fk (one for each block).  Returns the weights times the
+// blocks' value factors as FP16 pairs, in the order of the values' operand, and
+// what the output so far is to be multiplied by.
+template <int B>
+__device__ __forceinline__ float soften(const Tile<B> &t, f32x4 *st, const float *fk, bool all, int32_t lo, int32_t hi,
+                                        int g, Soft &w, f16x8 *ph, f16x8 *pl)
+{
+    using T = Tile<B>;
+    float big = -__builtin_inff(), f[T::NB], vm[T::NB];
+    if (all) {
+#pragma unroll
+        for (int i = 0; i < T::NB; ++i) {
+            float top = -__builtin_inff();
+#pragma unroll
+            for (int s = i * T::GS; s < (i + 1) * T::GS; ++s)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top = __builtin_fmaxf(top, st[s][e]);
+            f[i] = fk[i];
+            vm[i] = t.v[i];
+            big = __builtin_fmaxf(big, top * f[i]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < T::NB; ++i) {
+            // (a row's units follow the blocks that it sees something of, and no others)
+            const int64_t p0 = t.place(i * T::GS);
+            const bool met = t.blk[i] >= 0 && p0 <= hi && p0 + T::GS * 16 - 1 >= lo;
+            vm[i] = met ? t.v[i] : 0.0f;
+            f[i] = 1.0f;
+#pragma unroll
+            for (int s = i * T::GS; s < (i + 1) * T::GS; ++s)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int64_t p = t.place(s) + 4 * g + e;
+                    st[s][e] = met && p >= lo && p <= hi ? st[s][e] * fk[i] : -__builtin_inff();
+                    big = __builtin_fmaxf(big, st[s][e]);
+                }
+        }
+    }
+    int ev = kNoScale;
+#pragma unroll
+    for (int i = 0; i < T::NB; ++i) ev = max(ev, exponent(vm[i]));
+    const float mn = __builtin_fmaxf(w.m, max_over_groups(big));
+    const float mz = mn == -__builtin_inff() ? 0.0f : mn;
+    const float alpha = __builtin_amdgcn_exp2f(w.m - mz);
+    const int rn = max(w.ref, ev);
+    // (before the first scale that is not 0, the output is 0)
+    const float turn = w.ref == kNoScale ? alpha : ldexpf(alpha, w.ref - rn);
+    float wv[T::NB];
+#pragma unroll
+    for (int i = 0; i < T::NB; ++i) {
+        const int e = exponent(vm[i]);
+        wv[i] = t.page[i] >= 0 ? ldexpf(vm[i], 14 - rn) : e == kNoScale ? 0.0f : ldexpf(127.0f, e + 7 - rn);
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int s = 2 * c + e / 4;
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(st[s][e % 4], f[s / T::GS], -mz));
+            sum += x;
+            p[e] = x * wv[s / T::GS];
+        }
+        pairs8(p, ph[c], pl[c]);
+    }
+    w.m = mn;
+    w.l = w.l * alpha + sum;
+    w.ref = rn;
+    return turn;
+}
+
+// The factor of a finished output.
+__device__ __forceinline__ float unit_of(int ref)
+{
+    return ref == kNoScale ? 0.0f : ldexpf(1.0f / 127.0f, ref - 14);
 }
 
 // Attention of 16 rows by the four waves of a workgroup, each on 64-token tiles of
@@ -396,14 +568,21 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
     const int part = (int)(wg % a.parts);
     const int head = (int)(wg / a.parts % a.c.heads);
     Rows t;
-    if (!find_rows<16>(a, by_token, wg / a.parts / a.c.heads, head, r, t)) return;
+    if (!find_rows<16>(a, by_token, wg / a.parts / a.c.heads, t)) return;
+    const Span span = rows_see(a, t.s, t.row0, t.rows);
+    // this lane's row
+    const int row = t.row0 + r;
+    const int64_t token = r < t.rows ? t.s.first + row / a.group : -1;
+    const int head_q = head * a.group + row % a.group;
+    int32_t lo = 0, hi = -1;
+    if (r < t.rows) row_sees(a, t.s, row, lo, hi);
 
     // tiles of this part: of the places from the tile of the first one seen, or of
     // the listed blocks
-    const int64_t listed = a.sel ? (int64_t)uniform(t.token) * a.c.heads + head : 0;
+    const int64_t listed = a.sel ? (int64_t)(t.s.first + t.row0 / a.group) * a.c.heads + head : 0;
     const int32_t *list = a.sel + listed * a.n_sel;
-    const int64_t base = a.sel ? 0 : t.first / 64;
-    const int64_t end = a.sel ? ((int64_t)a.n_sel * B + 63) / 64 : t.last < t.first ? 0 : (int64_t)t.last / 64 + 1;
+    const int64_t base = a.sel ? 0 : span.first / 64;
+    const int64_t end = a.sel ? ((int64_t)a.n_sel * B + 63) / 64 : (int64_t)span.last / 64 + 1;
     const int64_t from = base + (int64_t)part * a.part_tiles;
     const int64_t to = from + a.part_tiles < end ? from + a.part_tiles : end;
     const int slot = uniform(kv_slot(a.b, t.seq));
@@ -411,10 +590,9 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
     f32x4 o[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) o[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    float m = -__builtin_inff(), l = 0.0f;
-    int ref = kNoScale;   // this row's o is in units of 2^(ref - 14) / 127
+    Soft w = {-__builtin_inff(), 0.0f, kNoScale};
 
-    if (from + wave < to && t.last >= t.first) {
+    if (from + wave < to && span.last >= span.first) {
         Blocks<B> blocks;
         blocks.load(a, t.s, t.seq, slot, head, list, from + wave, to, W);
         T cur;
@@ -424,31 +602,8 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
             codes.load_keys(a, cur, head, r, g);
             codes.load_values(a, cur, head, r, g);
         }
-        // the query row: lane (r, g) holds elements g D/4 .. of row r
         f16x8 qh[KC], ql[KC];
-        float fq;
-        {
-            float x[D / 4];
-            const float *src = a.q + (int64_t)(t.token < 0 ? 0 : t.token) * a.q_token + t.head_q * a.q_head + g * (D / 4);
-            float big = 0.0f;
-#pragma unroll
-            for (int i = 0; i < D / 4; i += 4) {
-                const float4 v = t.token < 0 ? float4{0.0f, 0.0f, 0.0f, 0.0f} : load16(src + i, a.vec);
-                x[i] = v.x;
-                x[i + 1] = v.y;
-                x[i + 2] = v.z;
-                x[i + 3] = v.w;
-            }
-#pragma unroll
-            for (int i = 0; i < D / 4; ++i) big = __builtin_fmaxf(big, __builtin_fabsf(x[i]));
-            const int e = exponent(max_over_groups(big));
-            const int shift = e == kNoScale ? 0 : 14 - e;
-#pragma unroll
-            for (int i = 0; i < D / 4; ++i) x[i] = ldexpf(x[i], shift);
-#pragma unroll
-            for (int k = 0; k < KC; ++k) pairs8(x + 8 * k, qh[k], ql[k]);
-            fq = ldexpf(a.scale * kLog2e, -shift);
-        }
+        const float fq = load_query<D>(a, token < 0 ? nullptr : a.q + token * a.q_token + head_q * a.q_head + g * (D / 4), qh, ql);
 
         int at = 0;
         for (int64_t kt = from + wave; kt < to; kt += W) {
@@ -465,7 +620,7 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
 
             // scores
             f32x4 st[4];
-            float fk[4];
+            float fk[T::NB];
             if (cur.coded) {
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
@@ -477,88 +632,33 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
                         st[s] = mfma16(c, ql[k], st[s]);
                     }
                     if (s & 1) __builtin_amdgcn_sched_barrier(0);   // (two groups' keys as FP16 at a time)
-                    fk[s] = cur.k[s / T::GS] * (1.0f / 127.0f) * fq;
                 }
             } else {
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
-                    st[s] = scores_of_group<D, B>(a, cur, s, slot, head, t.s.len, r, g, qh, ql, fq, fk[s]);
+                    st[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                    keys_of_group<D, B>(a, cur, s, slot, head, t.s.len, r, g, [&](int k, f16x8 h, f16x8 x) {
+                        st[s] = mfma16(h, qh[k], st[s]);
+                        st[s] = mfma16(h, ql[k], st[s]);
+                        st[s] = mfma16(x, qh[k], st[s]);
+                    });
                     __builtin_amdgcn_sched_barrier(0);   // (rows of one group at a time in registers)
                 }
             }
+#pragma unroll
+            for (int i = 0; i < T::NB; ++i) fk[i] = cur.key_factor(i) * fq;
             if (ask) codes.load_keys(a, next, head, r, g);
 
-            // in log2 units, and without what a row does not see
-            float big = -__builtin_inff(), vm[T::NB];
-            int ev = kNoScale;
             bool all = cur.coded;
 #pragma unroll
-            for (int i = 0; i < T::NB; ++i) {
-                const int64_t p0 = cur.place(i * T::GS);
-                all = all && p0 >= t.all_lo && p0 + T::GS * 16 - 1 <= t.all_hi;
-                vm[i] = cur.v[i];
-            }
-            if (all) {
-#pragma unroll
-                for (int s = 0; s < 4; ++s)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        st[s][i] *= fk[s];
-                        big = __builtin_fmaxf(big, st[s][i]);
-                    }
-            } else {
-#pragma unroll
-                for (int i = 0; i < T::NB; ++i) {
-                    // (a row's units follow the blocks that it sees something of, and no others)
-                    const int64_t p0 = cur.place(i * T::GS);
-                    if (cur.blk[i] < 0 || p0 > t.hi || p0 + T::GS * 16 - 1 < t.lo) vm[i] = 0.0f;
-                }
-#pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const int64_t p0 = cur.place(s) + 4 * g;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const bool seen = cur.blk[s / T::GS] >= 0 && p0 + i >= t.lo && p0 + i <= t.hi;
-                        st[s][i] = seen ? st[s][i] * fk[s] : -__builtin_inff();
-                        big = __builtin_fmaxf(big, st[s][i]);
-                    }
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < T::NB; ++i) ev = max(ev, exponent(vm[i]));
-            const float mn = __builtin_fmaxf(m, max_over_groups(big));
-            const float mz = mn == -__builtin_inff() ? 0.0f : mn;
-            const float alpha = __builtin_amdgcn_exp2f(m - mz);
-            const int rn = max(ref, ev);
-            // (before the first scale that is not 0, o is 0)
-            const float turn = ref == kNoScale ? alpha : ldexpf(alpha, ref - rn);
-            m = mn;
-            ref = rn;
+            for (int i = 0; i < T::NB; ++i)
+                all = all && cur.place(i * T::GS) >= span.all_lo && cur.place(i * T::GS) + T::GS * 16 - 1 <= span.all_hi;
+            f16x8 ph[2], pl[2];
+            const float turn = soften<B>(cur, st, fk, all, lo, hi, g, w, ph, pl);
             if (__ballot(turn != 1.0f)) {
 #pragma unroll
                 for (int n = 0; n < N; ++n) o[n] *= turn;
             }
-            float wv[T::NB];   // the factor of a weight for the values of a block
-#pragma unroll
-            for (int i = 0; i < T::NB; ++i) {
-                const int e = exponent(vm[i]);
-                wv[i] = cur.page[i] >= 0 ? ldexpf(vm[i], 14 - rn) : e == kNoScale ? 0.0f : ldexpf(127.0f, e + 7 - rn);
-            }
-            float sum = 0.0f;
-            f16x8 ph[2], pl[2];
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                float p[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int s = 2 * c + i / 4;
-                    const float e = __builtin_amdgcn_exp2f(st[s][i % 4] - mz);
-                    sum += e;
-                    p[i] = e * wv[s / T::GS];
-                }
-                pairs8(p, ph[c], pl[c]);
-            }
-            l = l * alpha + sum;
 
             // values
             if (cur.coded) {
@@ -577,14 +677,11 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
                 for (int n = 0; n < N; ++n)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        f16x2 h[4], x[4];
-                        values_of_group<D, B>(a, cur, 2 * c, n, slot, head, t.s.len, r, g, h[0], h[1], x[0], x[1]);
-                        values_of_group<D, B>(a, cur, 2 * c + 1, n, slot, head, t.s.len, r, g, h[2], h[3], x[2], x[3]);
-                        const f16x8 vh = {h[0][0], h[0][1], h[1][0], h[1][1], h[2][0], h[2][1], h[3][0], h[3][1]};
-                        const f16x8 vl = {x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
-                        o[n] = mfma16(vh, ph[c], o[n]);
-                        o[n] = mfma16(vh, pl[c], o[n]);
-                        o[n] = mfma16(vl, ph[c], o[n]);
+                        f16x8 h, x;
+                        values_of_half<D, B>(a, cur, c, n, slot, head, t.s.len, r, g, h, x);
+                        o[n] = mfma16(h, ph[c], o[n]);
+                        o[n] = mfma16(h, pl[c], o[n]);
+                        o[n] = mfma16(x, ph[c], o[n]);
                         __builtin_amdgcn_sched_barrier(0);
                     }
             }
@@ -594,48 +691,232 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
     }
 
     // join the waves
-    l = sum_over_groups(l);
-    const float unit = ref == kNoScale ? 0.0f : ldexpf(1.0f / 127.0f, ref - 14);
+    const float sum = sum_over_groups(w.l), unit = unit_of(w.ref);
 #pragma unroll
     for (int n = 0; n < N; ++n) *reinterpret_cast<f32x4 *>(&part_o[wave][r][16 * n + 4 * g]) = o[n] * unit;
     if (g == 0) {
-        part_m[wave][r] = m;
-        part_l[wave][r] = l;
-        part_row[r] = t.token < 0 ? -1 : t.token;
-        part_head[r] = t.head_q;
+        part_m[wave][r] = w.m;
+        part_l[wave][r] = sum;
+        part_row[r] = (int)token;
+        part_head[r] = head_q;
     }
     __syncthreads();
     const int rr = threadIdx.x >> 4, c0 = threadIdx.x & 15;
-    const int64_t token = part_row[rr];
-    if (token < 0) return;
-    float top = -__builtin_inff(), total = 0.0f, w[W];
+    const int64_t to_token = part_row[rr];
+    if (to_token < 0) return;
+    float top = -__builtin_inff(), total = 0.0f, share[W];
 #pragma unroll
     for (int i = 0; i < W; ++i) top = __builtin_fmaxf(top, part_m[i][rr]);
     const float tz = top == -__builtin_inff() ? 0.0f : top;
 #pragma unroll
     for (int i = 0; i < W; ++i) {
-        w[i] = __builtin_amdgcn_exp2f(part_m[i][rr] - tz);
-        total += w[i] * part_l[i][rr];
+        share[i] = __builtin_amdgcn_exp2f(part_m[i][rr] - tz);
+        total += share[i] * part_l[i][rr];
     }
-    const int64_t row = token * a.c.heads * a.group + part_head[rr];
-    const int64_t rows = (int64_t)a.b.tokens * a.c.heads * a.group;
-    float *ml = a.ws_ml + ((int64_t)part * rows + row) * 2;
-    if (a.parts > 1 && c0 == 0) {
-        ml[0] = top;
-        ml[1] = total;
-    }
+    const Place to_row = place_of(a, to_token, part_head[rr], part);
+    if (c0 == 0) to_row.sums(a, top, total);
     if (a.parts > 1 && total == 0.0f) return;
-    float *dst = a.parts > 1 ? a.ws_o + ((int64_t)part * rows + row) * D
-                             : a.out + token * a.out_token + part_head[rr] * a.out_head;
-    const bool vec = a.parts > 1 || a.vec;
     for (int c = 4 * c0; c < D; c += 64) {
         f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < W; ++i) x += *reinterpret_cast<const f32x4 *>(&part_o[i][rr][c]) * w[i];
-        if (a.parts == 1) x = total == 0.0f ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : x / total;
-        store4(dst + c, x, vec);
+        for (int i = 0; i < W; ++i) x += *reinterpret_cast<const f32x4 *>(&part_o[i][rr][c]) * share[i];
+        to_row.store(a, c, x, total);
     }
-    if (a.parts == 1 && a.lse && c0 == 0) a.lse[row] = log_sum(top, total);
+}
+
+// Attention of 128 rows by a workgroup whose four waves have 32 rows each, for
+// prompts: keys and values are converted to FP16 once for all rows, a tile ahead, and
+// wait in LDS in the order of the matrix operands (lane by lane, no bank conflicts).
+// A key fragment feeds four matrix instructions (two groups of 16 rows, two parts of
+// the pair) and a value fragment likewise.
+template <int D, int B>
+__global__ void __launch_bounds__(256, 2)
+kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
+{
+    constexpr int KC = D / 32, N = D / 16, Q = 2, R = 128, NW = (N + 3) / 4;
+    using T = Tile<B>;
+    // fragments of 64 lanes x 16 bytes: keys of group s and chunk k at s KC + k, values of
+    // column tile n and token half c at 4 KC + 2 n + c
+    __shared__ f16x8 frag[2][4 * KC + 2 * N][64];
+    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int64_t wg = wg0 + blockIdx.x;
+    // heads side by side, so that with eight of them each XCD has its own head's keys in
+    // L2; the last rows of a sequence, which see most, first
+    const int head = (int)(wg % a.c.heads);
+    const int part = (int)(wg / a.c.heads % a.parts);
+    Rows t;
+    if (!find_rows<R>(a, false, tiles - 1 - wg / a.c.heads / a.parts, t)) return;
+    const Span span = rows_see(a, t.s, t.row0, t.rows);
+    const int slot = uniform(kv_slot(a.b, t.seq));
+    const int64_t base = span.first / 64, end = (int64_t)span.last / 64 + 1;
+    const int64_t from = base + (int64_t)part * a.part_tiles;
+    const int64_t to = from + a.part_tiles < end ? from + a.part_tiles : end;
+
+    // this wave's rows, and this lane's two
+    const int mine = t.rows - 32 * wave < 32 ? t.rows - 32 * wave : 32;   // (none: <= 0)
+    const Span wspan = mine > 0 ? rows_see(a, t.s, t.row0 + 32 * wave, mine) : Span{0, -1, 0, -1};
+    int64_t token[Q];
+    int head_q[Q];
+    int32_t lo[Q], hi[Q];
+    f16x8 qh[Q][KC], ql[Q][KC];
+    float fq[Q];
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+        const int at = 32 * wave + 16 * i + r, row = t.row0 + at;
+        const bool is = at < t.rows;
+        token[i] = is ? t.s.first + row / a.group : -1;
+        head_q[i] = head * a.group + row % a.group;
+        lo[i] = 0;
+        hi[i] = -1;
+        if (is) row_sees(a, t.s, row, lo[i], hi[i]);
+        fq[i] = load_query<D>(a, is ? a.q + token[i] * a.q_token + head_q[i] * a.q_head + g * (D / 4) : nullptr, qh[i], ql[i]);
+    }
+    f32x4 o[Q][N];
+    Soft w[Q];
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+        w[i] = Soft{-__builtin_inff(), 0.0f, kNoScale};
+#pragma unroll
+        for (int n = 0; n < N; ++n) o[i][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    if (from < to && span.last >= span.first) {
+        // staging: wave w takes the keys of group w and the values of column tiles w, w + 4
+        uint32_t ks[D / 16], vs[NW][4];
+        auto ask = [&](const T &x) {
+            load_group_keys<D, B>(a, x, wave, head, r, g, ks);
+#pragma unroll
+            for (int j = 0; j < NW; ++j)
+                if (wave + 4 * j < N) load_column_values<D, B>(a, x, wave + 4 * j, head, r, g, vs[j]);
+        };
+        auto keep = [&](int b) {
+#pragma unroll
+            for (int k = 0; k < KC; ++k) frag[b][wave * KC + k][lane] = codes8(ks[2 * k], ks[2 * k + 1]);
+#pragma unroll
+            for (int j = 0; j < NW; ++j)
+                if (wave + 4 * j < N) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+                        frag[b][4 * KC + 2 * (wave + 4 * j) + c][lane] = codes8(vs[j][2 * c], vs[j][2 * c + 1]);
+                }
+        };
+        // a tile with FP32 rows (or without some of its blocks): both parts of the pairs
+        auto keep_pairs = [&](const T &x, int b) {
+            keys_of_group<D, B>(a, x, wave, slot, head, t.s.len, r, g, [&](int k, f16x8 h, f16x8 l) {
+                frag[b][wave * KC + k][lane] = h;
+                frag[b ^ 1][wave * KC + k][lane] = l;
+            });
+#pragma unroll 1
+            for (int n = wave; n < N; n += 4)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    f16x8 h, l;
+                    values_of_half<D, B>(a, x, c, n, slot, head, t.s.len, r, g, h, l);
+                    frag[b][4 * KC + 2 * n + c][lane] = h;
+                    frag[b ^ 1][4 * KC + 2 * n + c][lane] = l;
+                }
+        };
+
+        Blocks<B> blocks;
+        blocks.load(a, t.s, t.seq, slot, head, nullptr, from, to, 1);
+        T cur;
+        cur.take(blocks, 0, from);
+        int buf = 0, at = 0;
+        if (cur.coded) {
+            ask(cur);
+            keep(0);
+        } else {
+            keep_pairs(cur, 0);
+        }
+        __syncthreads();
+        for (int64_t kt = from; kt < to; ++kt) {
+            T next = cur;
+            const bool more = kt + 1 < to;
+            if (more) {
+                if (++at == Blocks<B>::TILES) {
+                    at = 0;
+                    blocks.load(a, t.s, t.seq, slot, head, nullptr, kt + 1, to, 1);
+                }
+                next.take(blocks, at, kt + 1);
+                if (next.coded) ask(next);
+            }
+            // (a wave whose rows see nothing of the tile only helps to stage)
+            if (kt * 64 <= wspan.last && kt * 64 + 63 >= wspan.first) {
+                f32x4 st[Q][4];
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+#pragma unroll
+                    for (int i = 0; i < Q; ++i) st[i][s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int k = 0; k < KC; ++k) {
+                        const f16x8 c = frag[buf][s * KC + k][lane];
+#pragma unroll
+                        for (int i = 0; i < Q; ++i) st[i][s] = mfma16(c, qh[i][k], st[i][s]);
+#pragma unroll
+                        for (int i = 0; i < Q; ++i) st[i][s] = mfma16(c, ql[i][k], st[i][s]);
+                        if (!cur.coded) {
+                            const f16x8 d = frag[buf ^ 1][s * KC + k][lane];
+#pragma unroll
+                            for (int i = 0; i < Q; ++i) st[i][s] = mfma16(d, qh[i][k], st[i][s]);
+                        }
+                    }
+                }
+                bool all = cur.coded;
+#pragma unroll
+                for (int i = 0; i < T::NB; ++i)
+                    all = all && cur.place(i * T::GS) >= wspan.all_lo && cur.place(i * T::GS) + T::GS * 16 - 1 <= wspan.all_hi;
+                f16x8 ph[Q][2], pl[Q][2];
+#pragma unroll
+                for (int i = 0; i < Q; ++i) {
+                    float fk[T::NB];
+#pragma unroll
+                    for (int b = 0; b < T::NB; ++b) fk[b] = cur.key_factor(b) * fq[i];
+                    const float turn = soften<B>(cur, st[i], fk, all, lo[i], hi[i], g, w[i], ph[i], pl[i]);
+                    if (__ballot(turn != 1.0f)) {
+#pragma unroll
+                        for (int n = 0; n < N; ++n) o[i][n] *= turn;
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const f16x8 v = frag[buf][4 * KC + 2 * n + c][lane];
+#pragma unroll
+                        for (int i = 0; i < Q; ++i) o[i][n] = mfma16(v, ph[i][c], o[i][n]);
+#pragma unroll
+                        for (int i = 0; i < Q; ++i) o[i][n] = mfma16(v, pl[i][c], o[i][n]);
+                        if (!cur.coded) {
+                            const f16x8 d = frag[buf ^ 1][4 * KC + 2 * n + c][lane];
+#pragma unroll
+                            for (int i = 0; i < Q; ++i) o[i][n] = mfma16(d, ph[i][c], o[i][n]);
+                        }
+                    }
+            }
+            if (more) {
+                // both buffers are in use where a tile has residuals
+                if (!cur.coded || !next.coded) __syncthreads();
+                if (next.coded)
+                    keep(buf ^ 1);
+                else
+                    keep_pairs(next, buf ^ 1);
+                __syncthreads();
+                buf ^= 1;
+                cur = next;
+            }
+        }
+    }
+
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+        const float sum = sum_over_groups(w[i].l), unit = unit_of(w[i].ref);
+        if (token[i] < 0) continue;
+        const Place to_row = place_of(a, token[i], head_q[i], part);
+        if (g == 0) to_row.sums(a, w[i].m, sum);
+        if (a.parts > 1 && sum == 0.0f) continue;
+#pragma unroll
+        for (int n = 0; n < N; ++n) to_row.store(a, 16 * n + 4 * g, o[i][n] * unit, sum);
+    }
 }
 
 // The parts of a row joined in ascending order, one wave to a row.  A lane holds the
@@ -700,7 +981,10 @@ hipError_t attention_sized(KvAttnArgs &a, const KvPlan &plan, hipStream_t stream
 {
     const int64_t n = plan.tiles * a.c.heads * plan.parts;
     hipError_t err = in_parts(n, [&](int64_t at, unsigned m) {
-        hipLaunchKernelGGL((kv_attention_kernel<D, B>), dim3(m), dim3(256), 0, stream, a, plan.by_token, at);
+        if (plan.wide)
+            hipLaunchKernelGGL((kv_prompt_kernel<D, B>), dim3(m), dim3(256), 0, stream, a, plan.tiles, at);
+        else
+            hipLaunchKernelGGL((kv_attention_kernel<D, B>), dim3(m), dim3(256), 0, stream, a, plan.by_token, at);
     });
     if (err != hipSuccess || plan.parts == 1) return err;
     const int64_t rows = (int64_t)a.b.tokens * a.c.heads * a.group;
@@ -716,10 +1000,13 @@ KvPlan kv_plan(int64_t tokens, int64_t seqs, bool ragged, int heads, int group, 
 {
     KvPlan p = {};
     p.by_token = n_sel > 0 || !ragged;
-    p.tiles = p.by_token ? tokens * ((group + 15) / 16) : kv_tiles(tokens, seqs, group, 16);
-    // 64-token tiles that a row tile can have to read (its rows' windows begin at up to 16 places)
+    // (a chunk of the caller's asks for sums that do not depend on the call's sizes)
+    p.wide = !p.by_token && chunk == 0 && tokens * group >= kWideRows * seqs;
+    const int R = p.wide ? 128 : 16;
+    p.tiles = p.by_token ? tokens * ((group + 15) / 16) : kv_tiles(tokens, seqs, group, R);
+    // 64-token tiles that a row tile can have to read (its rows' windows begin at up to R places)
     int64_t places = n_sel > 0 ? n_sel * block : cols * block;
-    if (n_sel == 0 && window > 0 && window + 16 + 63 < places) places = window + 16 + 63;
+    if (n_sel == 0 && window > 0 && window + R + 63 < places) places = window + R + 63;
     const int64_t span = (places + 63) / 64 > 0 ? (places + 63) / 64 : 1;
     int64_t part_tiles;
     if (chunk > 0) {
