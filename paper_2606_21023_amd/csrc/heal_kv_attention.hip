@@ -284,9 +284,9 @@ struct Tile {
         return ldexpf(1.0f, e == kNoScale ? 0 : e - 14);
     }
     // place of the first token of group s
-    __device__ __forceinline__ int64_t place(int s) const
+    __device__ __forceinline__ int32_t place(int s) const
     {
-        return (int64_t)blk_of(s) * B + off + s % GS * 16;
+        return blk_of(s) * B + off + s % GS * 16;
     }
 };
 
@@ -378,7 +378,7 @@ __device__ __forceinline__ void keys_of_group(const KvAttnArgs &a, const Tile<B>
     } else {
         // FP32 rows; what lies behind the last one may be anything
         const float *src = a.c.kr + ((int64_t)slot * a.c.heads + head) * (2 * B * D) + ((blk & 1) * B + off + r) * D + g * (D / 4);
-        const bool there = t.place(s) + r < len;
+        const bool there = (int64_t)t.place(s) + r < len;
         const int e = exponent(t.key_of(s)), shift = e == kNoScale ? 0 : 14 - e;
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
@@ -479,7 +479,7 @@ __device__ __forceinline__ float soften(const Tile<B> &t, f32x4 *st, const float
 {
     using T = Tile<B>;
     float big = -__builtin_inff(), f[T::NB], vm[T::NB];
-    if (all) {
+    if (__builtin_expect(all, true)) {
 #pragma unroll
         for (int i = 0; i < T::NB; ++i) {
             float top = -__builtin_inff();
@@ -495,16 +495,18 @@ __device__ __forceinline__ float soften(const Tile<B> &t, f32x4 *st, const float
 #pragma unroll
         for (int i = 0; i < T::NB; ++i) {
             // (a row's units follow the blocks that it sees something of, and no others)
-            const int64_t p0 = t.place(i * T::GS);
-            const bool met = t.blk[i] >= 0 && p0 <= hi && p0 + T::GS * 16 - 1 >= lo;
+            const int32_t p0 = t.place(i * T::GS);
+            const bool met = t.blk[i] >= 0 && p0 <= hi && p0 + (T::GS * 16 - 1) >= lo;
             vm[i] = met ? t.v[i] : 0.0f;
             f[i] = 1.0f;
+            // what the row sees, counted from the lane's first token of the block
+            const int32_t from = lo - p0 - 4 * g, to = met ? hi - p0 - 4 * g : -1;
 #pragma unroll
             for (int s = i * T::GS; s < (i + 1) * T::GS; ++s)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int64_t p = t.place(s) + 4 * g + e;
-                    st[s][e] = met && p >= lo && p <= hi ? st[s][e] * fk[i] : -__builtin_inff();
+                    const int at = (s - i * T::GS) * 16 + e;
+                    st[s][e] = at >= from && at <= to ? st[s][e] * fk[i] : -__builtin_inff();
                     big = __builtin_fmaxf(big, st[s][e]);
                 }
         }
@@ -822,6 +824,60 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
         T cur;
         cur.take(blocks, 0, from);
         int buf = 0, at = 0;
+        // the tile in LDS; residuals: with FP32 rows, whose residuals the other buffer has
+        auto compute = [&](auto residuals) {
+            constexpr bool X = decltype(residuals)::value;
+            f32x4 st[Q][4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+#pragma unroll
+                for (int i = 0; i < Q; ++i) st[i][s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int k = 0; k < KC; ++k) {
+                    const f16x8 c = frag[buf][s * KC + k][lane];
+#pragma unroll
+                    for (int i = 0; i < Q; ++i) st[i][s] = mfma16(c, qh[i][k], st[i][s]);
+#pragma unroll
+                    for (int i = 0; i < Q; ++i) st[i][s] = mfma16(c, ql[i][k], st[i][s]);
+                    if (X) {
+                        const f16x8 d = frag[buf ^ 1][s * KC + k][lane];
+#pragma unroll
+                        for (int i = 0; i < Q; ++i) st[i][s] = mfma16(d, qh[i][k], st[i][s]);
+                    }
+                }
+            }
+            bool all = !X;
+#pragma unroll
+            for (int i = 0; i < T::NB; ++i)
+                all = all && cur.place(i * T::GS) >= wspan.all_lo && cur.place(i * T::GS) + T::GS * 16 - 1 <= wspan.all_hi;
+            f16x8 ph[Q][2], pl[Q][2];
+#pragma unroll
+            for (int i = 0; i < Q; ++i) {
+                float fk[T::NB];
+#pragma unroll
+                for (int b = 0; b < T::NB; ++b) fk[b] = cur.key_factor(b) * fq[i];
+                const float turn = soften<B>(cur, st[i], fk, all, lo[i], hi[i], g, w[i], ph[i], pl[i]);
+                if (__ballot(turn != 1.0f)) {
+#pragma unroll
+                    for (int n = 0; n < N; ++n) o[i][n] *= turn;
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const f16x8 v = frag[buf][4 * KC + 2 * n + c][lane];
+#pragma unroll
+                    for (int i = 0; i < Q; ++i) o[i][n] = mfma16(v, ph[i][c], o[i][n]);
+#pragma unroll
+                    for (int i = 0; i < Q; ++i) o[i][n] = mfma16(v, pl[i][c], o[i][n]);
+                    if (X) {
+                        const f16x8 d = frag[buf ^ 1][4 * KC + 2 * n + c][lane];
+#pragma unroll
+                        for (int i = 0; i < Q; ++i) o[i][n] = mfma16(d, ph[i][c], o[i][n]);
+                    }
+                }
+        };
         if (cur.coded) {
             ask(cur);
             keep(0);
@@ -842,56 +898,10 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
             }
             // (a wave whose rows see nothing of the tile only helps to stage)
             if (kt * 64 <= wspan.last && kt * 64 + 63 >= wspan.first) {
-                f32x4 st[Q][4];
-#pragma unroll
-                for (int s = 0; s < 4; ++s) {
-#pragma unroll
-                    for (int i = 0; i < Q; ++i) st[i][s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int k = 0; k < KC; ++k) {
-                        const f16x8 c = frag[buf][s * KC + k][lane];
-#pragma unroll
-                        for (int i = 0; i < Q; ++i) st[i][s] = mfma16(c, qh[i][k], st[i][s]);
-#pragma unroll
-                        for (int i = 0; i < Q; ++i) st[i][s] = mfma16(c, ql[i][k], st[i][s]);
-                        if (!cur.coded) {
-                            const f16x8 d = frag[buf ^ 1][s * KC + k][lane];
-#pragma unroll
-                            for (int i = 0; i < Q; ++i) st[i][s] = mfma16(d, qh[i][k], st[i][s]);
-                        }
-                    }
-                }
-                bool all = cur.coded;
-#pragma unroll
-                for (int i = 0; i < T::NB; ++i)
-                    all = all && cur.place(i * T::GS) >= wspan.all_lo && cur.place(i * T::GS) + T::GS * 16 - 1 <= wspan.all_hi;
-                f16x8 ph[Q][2], pl[Q][2];
-#pragma unroll
-                for (int i = 0; i < Q; ++i) {
-                    float fk[T::NB];
-#pragma unroll
-                    for (int b = 0; b < T::NB; ++b) fk[b] = cur.key_factor(b) * fq[i];
-                    const float turn = soften<B>(cur, st[i], fk, all, lo[i], hi[i], g, w[i], ph[i], pl[i]);
-                    if (__ballot(turn != 1.0f)) {
-#pragma unroll
-                        for (int n = 0; n < N; ++n) o[i][n] *= turn;
-                    }
-                }
-#pragma unroll
-                for (int n = 0; n < N; ++n)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const f16x8 v = frag[buf][4 * KC + 2 * n + c][lane];
-#pragma unroll
-                        for (int i = 0; i < Q; ++i) o[i][n] = mfma16(v, ph[i][c], o[i][n]);
-#pragma unroll
-                        for (int i = 0; i < Q; ++i) o[i][n] = mfma16(v, pl[i][c], o[i][n]);
-                        if (!cur.coded) {
-                            const f16x8 d = frag[buf ^ 1][4 * KC + 2 * n + c][lane];
-#pragma unroll
-                            for (int i = 0; i < Q; ++i) o[i][n] = mfma16(d, ph[i][c], o[i][n]);
-                        }
-                    }
+                if (__builtin_expect(cur.coded, true))
+                    compute(std::false_type());
+                else
+                    compute(std::true_type());
             }
             if (more) {
                 // both buffers are in use where a tile has residuals
@@ -1012,8 +1022,11 @@ KvPlan kv_plan(int64_t tokens, int64_t seqs, bool ragged, int heads, int group, 
     if (chunk > 0) {
         part_tiles = chunk / 64;
     } else {
-        // enough workgroups to fill the chip, each with a tile for every wave at least
-        const int64_t wanted = (kWantedWorkgroups + p.tiles * heads - 1) / (p.tiles * heads > 0 ? p.tiles * heads : 1);
+        // enough workgroups to fill the chip, each with a tile for every wave at least; of the
+        // prompts' kernel two to a compute unit, which take equal parts (the bound on their
+        // row tiles counts one too many for each sequence)
+        const int64_t wgs = (p.wide ? p.tiles - seqs : p.tiles) * heads;
+        const int64_t wanted = wgs <= 0 ? 1 : p.wide ? 512 / wgs : (kWantedWorkgroups + wgs - 1) / wgs;
         int64_t parts = wanted < (span + 3) / 4 ? wanted : (span + 3) / 4;
         parts = parts < 1 ? 1 : parts > 64 ? 64 : parts;
         part_tiles = ((span + parts - 1) / parts + 3) / 4 * 4;
