@@ -79,6 +79,15 @@ __device__ __forceinline__ int exponent(float x)
 // it depends on has to be known as such.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
+// x, as a value that the compiler knows nothing of: what is computed from it on a path
+// that is seldom taken is computed there, and not before the loop, where its results
+// would take registers from the path that is.
+__device__ __forceinline__ int hidden(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 __device__ __forceinline__ KvSeq uniform_seq(const KvSeqs &b, int i)
 {
     const KvSeq s = kv_seq(b, i);
@@ -474,8 +483,8 @@ struct Soft {
 // blocks' value factors as FP16 pairs, in the order of the values' operand, and
 // what the output so far is to be multiplied by.
 template <int B>
-__device__ __forceinline__ float soften(const Tile<B> &t, f32x4 *st, const float *fk, bool all, int32_t lo, int32_t hi,
-                                        int g, Soft &w, f16x8 *ph, f16x8 *pl)
+__device__ __forceinline__ float soften(const Tile<B> &t, f32x4 *st, const float *fk, bool all, const int32_t *row_lo,
+                                        const int32_t *row_hi, int g, Soft &w, f16x8 *ph, f16x8 *pl)
 {
     using T = Tile<B>;
     float big = -__builtin_inff(), f[T::NB], vm[T::NB];
@@ -492,6 +501,7 @@ __device__ __forceinline__ float soften(const Tile<B> &t, f32x4 *st, const float
             big = __builtin_fmaxf(big, top * f[i]);
         }
     } else {
+        const int32_t lo = *row_lo, hi = *row_hi;
 #pragma unroll
         for (int i = 0; i < T::NB; ++i) {
             // (a row's units follow the blocks that it sees something of, and no others)
@@ -639,7 +649,7 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
                     st[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                    keys_of_group<D, B>(a, cur, s, slot, head, t.s.len, r, g, [&](int k, f16x8 h, f16x8 x) {
+                    keys_of_group<D, B>(a, cur, s, slot, head, t.s.len, hidden(r), hidden(g), [&](int k, f16x8 h, f16x8 x) {
                         st[s] = mfma16(h, qh[k], st[s]);
                         st[s] = mfma16(h, ql[k], st[s]);
                         st[s] = mfma16(x, qh[k], st[s]);
@@ -656,7 +666,7 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
             for (int i = 0; i < T::NB; ++i)
                 all = all && cur.place(i * T::GS) >= span.all_lo && cur.place(i * T::GS) + T::GS * 16 - 1 <= span.all_hi;
             f16x8 ph[2], pl[2];
-            const float turn = soften<B>(cur, st, fk, all, lo, hi, g, w, ph, pl);
+            const float turn = soften<B>(cur, st, fk, all, &lo, &hi, g, w, ph, pl);
             if (__ballot(turn != 1.0f)) {
 #pragma unroll
                 for (int n = 0; n < N; ++n) o[n] *= turn;
@@ -680,7 +690,7 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         f16x8 h, x;
-                        values_of_half<D, B>(a, cur, c, n, slot, head, t.s.len, r, g, h, x);
+                        values_of_half<D, B>(a, cur, c, n, slot, head, t.s.len, hidden(r), hidden(g), h, x);
                         o[n] = mfma16(h, ph[c], o[n]);
                         o[n] = mfma16(h, pl[c], o[n]);
                         o[n] = mfma16(x, ph[c], o[n]);
@@ -740,6 +750,9 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
     // fragments of 64 lanes x 16 bytes: keys of group s and chunk k at s KC + k, values of
     // column tile n and token half c at 4 KC + 2 n + c
     __shared__ f16x8 frag[2][4 * KC + 2 * N][64];
+    // what a row needs once a tile, or seldom: kept out of the registers, which are full
+    __shared__ float row_factor[R];
+    __shared__ int32_t row_lo[R], row_hi[R];
     const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int64_t wg = wg0 + blockIdx.x;
     // heads side by side, so that with eight of them each XCD has its own head's keys in
@@ -757,21 +770,20 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
     // this wave's rows, and this lane's two
     const int mine = t.rows - 32 * wave < 32 ? t.rows - 32 * wave : 32;   // (none: <= 0)
     const Span wspan = mine > 0 ? rows_see(a, t.s, t.row0 + 32 * wave, mine) : Span{0, -1, 0, -1};
-    int64_t token[Q];
-    int head_q[Q];
-    int32_t lo[Q], hi[Q];
     f16x8 qh[Q][KC], ql[Q][KC];
-    float fq[Q];
 #pragma unroll
     for (int i = 0; i < Q; ++i) {
         const int at = 32 * wave + 16 * i + r, row = t.row0 + at;
         const bool is = at < t.rows;
-        token[i] = is ? t.s.first + row / a.group : -1;
-        head_q[i] = head * a.group + row % a.group;
-        lo[i] = 0;
-        hi[i] = -1;
-        if (is) row_sees(a, t.s, row, lo[i], hi[i]);
-        fq[i] = load_query<D>(a, is ? a.q + token[i] * a.q_token + head_q[i] * a.q_head + g * (D / 4) : nullptr, qh[i], ql[i]);
+        const int64_t token = t.s.first + row / a.group, head_q = head * a.group + row % a.group;
+        int32_t lo = 0, hi = -1;
+        if (is) row_sees(a, t.s, row, lo, hi);
+        const float fq = load_query<D>(a, is ? a.q + token * a.q_token + head_q * a.q_head + g * (D / 4) : nullptr, qh[i], ql[i]);
+        if (g == 0) {   // (read by this wave only)
+            row_factor[at] = fq;
+            row_lo[at] = lo;
+            row_hi[at] = hi;
+        }
     }
     f32x4 o[Q][N];
     Soft w[Q];
@@ -804,7 +816,8 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
         };
         // a tile with FP32 rows (or without some of its blocks): both parts of the pairs
         auto keep_pairs = [&](const T &x, int b) {
-            keys_of_group<D, B>(a, x, wave, slot, head, t.s.len, r, g, [&](int k, f16x8 h, f16x8 l) {
+            const int r2 = hidden(r), g2 = hidden(g);
+            keys_of_group<D, B>(a, x, wave, slot, head, t.s.len, r2, g2, [&](int k, f16x8 h, f16x8 l) {
                 frag[b][wave * KC + k][lane] = h;
                 frag[b ^ 1][wave * KC + k][lane] = l;
             });
@@ -813,7 +826,7 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     f16x8 h, l;
-                    values_of_half<D, B>(a, x, c, n, slot, head, t.s.len, r, g, h, l);
+                    values_of_half<D, B>(a, x, c, n, slot, head, t.s.len, r2, g2, h, l);
                     frag[b][4 * KC + 2 * n + c][lane] = h;
                     frag[b ^ 1][4 * KC + 2 * n + c][lane] = l;
                 }
@@ -853,10 +866,12 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
             f16x8 ph[Q][2], pl[Q][2];
 #pragma unroll
             for (int i = 0; i < Q; ++i) {
+                const int at = 32 * wave + 16 * i + r;
+                const float fq = row_factor[at];
                 float fk[T::NB];
 #pragma unroll
-                for (int b = 0; b < T::NB; ++b) fk[b] = cur.key_factor(b) * fq[i];
-                const float turn = soften<B>(cur, st[i], fk, all, lo[i], hi[i], g, w[i], ph[i], pl[i]);
+                for (int b = 0; b < T::NB; ++b) fk[b] = cur.key_factor(b) * fq;
+                const float turn = soften<B>(cur, st[i], fk, all, row_lo + at, row_hi + at, g, w[i], ph[i], pl[i]);
                 if (__ballot(turn != 1.0f)) {
 #pragma unroll
                     for (int n = 0; n < N; ++n) o[i][n] *= turn;
@@ -920,8 +935,9 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
 #pragma unroll
     for (int i = 0; i < Q; ++i) {
         const float sum = sum_over_groups(w[i].l), unit = unit_of(w[i].ref);
-        if (token[i] < 0) continue;
-        const Place to_row = place_of(a, token[i], head_q[i], part);
+        const int at = 32 * wave + 16 * i + hidden(r), row = t.row0 + at;
+        if (at >= t.rows) continue;
+        const Place to_row = place_of(a, t.s.first + row / a.group, head * a.group + row % a.group, part);
         if (g == 0) to_row.sums(a, w[i].m, sum);
         if (a.parts > 1 && sum == 0.0f) continue;
 #pragma unroll
