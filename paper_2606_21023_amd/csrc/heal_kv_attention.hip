@@ -840,25 +840,38 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
         // the tile in LDS; residuals: with FP32 rows, whose residuals the other buffer has
         auto compute = [&](auto residuals) {
             constexpr bool X = decltype(residuals)::value;
+            // fragments are read from LDS a step ahead of the matrix instructions: keys of the
+            // next group, values of the next two column tiles
+            const f16x8(*hi)[64] = frag[buf], (*res)[64] = frag[buf ^ 1];
             f32x4 st[Q][4];
+            f16x8 kf[2][KC];
+#pragma unroll
+            for (int k = 0; k < KC; ++k) kf[0][k] = hi[k][lane];
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
+                if (s < 3) {
+#pragma unroll
+                    for (int k = 0; k < KC; ++k) kf[(s + 1) & 1][k] = hi[(s + 1) * KC + k][lane];
+                }
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int i = 0; i < Q; ++i) st[i][s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int k = 0; k < KC; ++k) {
-                    const f16x8 c = frag[buf][s * KC + k][lane];
 #pragma unroll
-                    for (int i = 0; i < Q; ++i) st[i][s] = mfma16(c, qh[i][k], st[i][s]);
+                    for (int i = 0; i < Q; ++i) st[i][s] = mfma16(kf[s & 1][k], qh[i][k], st[i][s]);
 #pragma unroll
-                    for (int i = 0; i < Q; ++i) st[i][s] = mfma16(c, ql[i][k], st[i][s]);
+                    for (int i = 0; i < Q; ++i) st[i][s] = mfma16(kf[s & 1][k], ql[i][k], st[i][s]);
                     if (X) {
-                        const f16x8 d = frag[buf ^ 1][s * KC + k][lane];
+                        const f16x8 d = res[s * KC + k][lane];
 #pragma unroll
                         for (int i = 0; i < Q; ++i) st[i][s] = mfma16(d, qh[i][k], st[i][s]);
                     }
                 }
             }
+            f16x8 vf[2][4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) vf[0][c] = hi[4 * KC + c][lane];
             bool all = !X;
 #pragma unroll
             for (int i = 0; i < T::NB; ++i)
@@ -878,20 +891,28 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
                 }
             }
 #pragma unroll
-            for (int n = 0; n < N; ++n)
+            for (int n = 0; n < N; n += 2) {
+                if (n + 2 < N) {
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const f16x8 v = frag[buf][4 * KC + 2 * n + c][lane];
-#pragma unroll
-                    for (int i = 0; i < Q; ++i) o[i][n] = mfma16(v, ph[i][c], o[i][n]);
-#pragma unroll
-                    for (int i = 0; i < Q; ++i) o[i][n] = mfma16(v, pl[i][c], o[i][n]);
-                    if (X) {
-                        const f16x8 d = frag[buf ^ 1][4 * KC + 2 * n + c][lane];
-#pragma unroll
-                        for (int i = 0; i < Q; ++i) o[i][n] = mfma16(d, ph[i][c], o[i][n]);
-                    }
+                    for (int c = 0; c < 4; ++c) vf[(n / 2 + 1) & 1][c] = hi[4 * KC + 2 * (n + 2) + c][lane];
                 }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int m = n; m < n + 2; ++m) {
+                        const f16x8 v = vf[(n / 2) & 1][2 * (m - n) + c];
+#pragma unroll
+                        for (int i = 0; i < Q; ++i) o[i][m] = mfma16(v, ph[i][c], o[i][m]);
+#pragma unroll
+                        for (int i = 0; i < Q; ++i) o[i][m] = mfma16(v, pl[i][c], o[i][m]);
+                        if (X) {
+                            const f16x8 d = res[4 * KC + 2 * m + c][lane];
+#pragma unroll
+                            for (int i = 0; i < Q; ++i) o[i][m] = mfma16(d, ph[i][c], o[i][m]);
+                        }
+                    }
+            }
         };
         if (cur.coded) {
             ask(cur);
