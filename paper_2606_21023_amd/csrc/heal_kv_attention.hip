@@ -219,7 +219,7 @@ template <int B>
 struct Blocks {
     static constexpr int EPT = B < 64 ? 64 / B : 1, TILES = 64 / EPT, STEP = B < 64 ? B : 64;
     int blk;     // block of the sequence, or -1 where the cache holds nothing of it
-    int page;    // its page, or -1 - page where it is read from the ring
+    int page;    // its page (0 where there is none), or -1 - page where it is read from the ring
     float k, v;  // m of its keys and values
 
     __device__ __forceinline__ void load(const KvAttnArgs &a, const KvSeq &s, int seq, int slot, int head,
@@ -233,7 +233,10 @@ struct Blocks {
         if (tile < to) blk = !a.sel ? (int)entry : entry < a.n_sel ? list[entry] : -1;
         if (blk >= 0) page = kv_page(a.b, seq, blk);
         const bool full = (int64_t)blk * B + B <= s.len;
-        if (page < 0 || (!full && slot < 0)) blk = -1;
+        if (page < 0 || (!full && slot < 0)) {
+            blk = -1;
+            page = 0;   // (its codes may be read: their weights are zeros)
+        }
         if (blk >= 0) {
             const float *sc = a.c.scales + ((int64_t)page * a.c.heads + head) * 2;
             k = sc[0];
@@ -256,7 +259,7 @@ struct Tile {
     int blk[NB], page[NB];
     float k[NB], v[NB];
     int off;      // of its first token within the block (B > 64)
-    bool coded;   // every group lies in a complete block
+    bool coded;   // no group is read from the ring
 
     __device__ __forceinline__ void take(const Blocks<B> &b, int at, int64_t kt)
     {
@@ -268,7 +271,7 @@ struct Tile {
             page[i] = from_lane(b.page, at * NB + i);
             k[i] = from_lane(b.k, at * NB + i);
             v[i] = from_lane(b.v, at * NB + i);
-            coded = coded && blk[i] >= 0 && page[i] >= 0;
+            coded = coded && page[i] >= 0;
         }
     }
     __device__ __forceinline__ int blk_of(int s) const { return pick(blk, s); }
@@ -302,13 +305,14 @@ struct Tile {
 // Codes as they come from memory, in the registers of one lane: of the keys of group
 // s, the D/4 bytes of row r that belong to lanes g; of row 16 n + r of V^T, the four
 // bytes of each group that do.  (The block's address is the wave's, the lane's part an
-// unsigned 32-bit offset: no 64-bit address per lane.)
+// unsigned 32-bit offset, hidden so that the two are not added outside the loop: no
+// 64-bit address per lane.)
 template <int D, int B>
 __device__ __forceinline__ void load_group_keys(const KvAttnArgs &a, const Tile<B> &t, int s, int head, int r, int g,
                                                 uint32_t *k)
 {
     const int8_t *src = a.c.kc + ((int64_t)t.page_of(s) * a.c.heads + head) * (B * D) + (t.off + s % Tile<B>::GS * 16) * D;
-    const uint32_t at = r * D + g * (D / 4);
+    const uint32_t at = hidden(r * D + g * (D / 4));
     if constexpr (D % 64 == 0) {
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) {
@@ -330,7 +334,7 @@ template <int D, int B>
 __device__ __forceinline__ void load_column_values(const KvAttnArgs &a, const Tile<B> &t, int n, int head, int r, int g,
                                                    uint32_t *v)
 {
-    const uint32_t at = r * B + g * (B / 4);
+    const uint32_t at = hidden(r * B + g * (B / 4));
 #pragma unroll
     for (int i = 0; i < Tile<B>::NB; ++i) {
         const int8_t *src = a.c.vc + ((int64_t)t.page[i] * a.c.heads + head) * (B * D) + t.off / 4 + n * (16 * B);
@@ -801,14 +805,14 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
             load_group_keys<D, B>(a, x, wave, head, r, g, ks);
 #pragma unroll
             for (int j = 0; j < NW; ++j)
-                if (wave + 4 * j < N) load_column_values<D, B>(a, x, wave + 4 * j, head, r, g, vs[j]);
+                if (N % 4 == 0 || wave + 4 * j < N) load_column_values<D, B>(a, x, wave + 4 * j, head, r, g, vs[j]);
         };
         auto keep = [&](int b) {
 #pragma unroll
             for (int k = 0; k < KC; ++k) frag[b][wave * KC + k][lane] = codes8(ks[2 * k], ks[2 * k + 1]);
 #pragma unroll
             for (int j = 0; j < NW; ++j)
-                if (wave + 4 * j < N) {
+                if (N % 4 == 0 || wave + 4 * j < N) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
                         frag[b][4 * KC + 2 * (wave + 4 * j) + c][lane] = codes8(vs[j][2 * c], vs[j][2 * c + 1]);
@@ -832,46 +836,44 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
                 }
         };
 
+        // the ring's block can only be in a sequence's last tile, which comes after the loop
+        const bool ring = t.s.len % B != 0 && t.s.len / B * B / 64 == to - 1;
+        const int64_t coded_to = ring ? to - 1 : to;
         Blocks<B> blocks;
-        blocks.load(a, t.s, t.seq, slot, head, nullptr, from, to, 1);
         T cur;
-        cur.take(blocks, 0, from);
         int buf = 0, at = 0;
         // the tile in LDS; residuals: with FP32 rows, whose residuals the other buffer has
         auto compute = [&](auto residuals) {
             constexpr bool X = decltype(residuals)::value;
-            // fragments are read from LDS a step ahead of the matrix instructions: keys of the
-            // next group, values of the next two column tiles
+            // fragments are read from LDS three steps (of four matrix instructions) ahead
             const f16x8(*hi)[64] = frag[buf], (*res)[64] = frag[buf ^ 1];
+            constexpr int A = 3;
             f32x4 st[Q][4];
-            f16x8 kf[2][KC];
+            f16x8 f[A + 1];
 #pragma unroll
-            for (int k = 0; k < KC; ++k) kf[0][k] = hi[k][lane];
+            for (int u = 0; u < A; ++u) f[u] = hi[u][lane];
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                if (s < 3) {
-#pragma unroll
-                    for (int k = 0; k < KC; ++k) kf[(s + 1) & 1][k] = hi[(s + 1) * KC + k][lane];
-                }
-                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int i = 0; i < Q; ++i) st[i][s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int k = 0; k < KC; ++k) {
+                    const int u = s * KC + k;
+                    if (u + A < 4 * KC) f[(u + A) % (A + 1)] = hi[u + A][lane];
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int i = 0; i < Q; ++i) st[i][s] = mfma16(kf[s & 1][k], qh[i][k], st[i][s]);
+                    for (int i = 0; i < Q; ++i) st[i][s] = mfma16(f[u % (A + 1)], qh[i][k], st[i][s]);
 #pragma unroll
-                    for (int i = 0; i < Q; ++i) st[i][s] = mfma16(kf[s & 1][k], ql[i][k], st[i][s]);
+                    for (int i = 0; i < Q; ++i) st[i][s] = mfma16(f[u % (A + 1)], ql[i][k], st[i][s]);
                     if (X) {
-                        const f16x8 d = res[s * KC + k][lane];
+                        const f16x8 d = res[u][lane];
 #pragma unroll
                         for (int i = 0; i < Q; ++i) st[i][s] = mfma16(d, qh[i][k], st[i][s]);
                     }
                 }
             }
-            f16x8 vf[2][4];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) vf[0][c] = hi[4 * KC + c][lane];
+            for (int u = 0; u < A; ++u) f[u] = hi[4 * KC + u][lane];
             bool all = !X;
 #pragma unroll
             for (int i = 0; i < T::NB; ++i)
@@ -891,65 +893,57 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
                 }
             }
 #pragma unroll
-            for (int n = 0; n < N; n += 2) {
-                if (n + 2 < N) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) vf[(n / 2 + 1) & 1][c] = hi[4 * KC + 2 * (n + 2) + c][lane];
-                }
+            for (int u = 0; u < 2 * N; ++u) {
+                const int n = u / 2, c = u % 2;
+                if (u + A < 2 * N) f[(u + A) % (A + 1)] = hi[4 * KC + u + A][lane];
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
+                for (int i = 0; i < Q; ++i) o[i][n] = mfma16(f[u % (A + 1)], ph[i][c], o[i][n]);
 #pragma unroll
-                    for (int m = n; m < n + 2; ++m) {
-                        const f16x8 v = vf[(n / 2) & 1][2 * (m - n) + c];
+                for (int i = 0; i < Q; ++i) o[i][n] = mfma16(f[u % (A + 1)], pl[i][c], o[i][n]);
+                if (X) {
+                    const f16x8 d = res[4 * KC + u][lane];
 #pragma unroll
-                        for (int i = 0; i < Q; ++i) o[i][m] = mfma16(v, ph[i][c], o[i][m]);
-#pragma unroll
-                        for (int i = 0; i < Q; ++i) o[i][m] = mfma16(v, pl[i][c], o[i][m]);
-                        if (X) {
-                            const f16x8 d = res[4 * KC + 2 * m + c][lane];
-#pragma unroll
-                            for (int i = 0; i < Q; ++i) o[i][m] = mfma16(d, ph[i][c], o[i][m]);
-                        }
-                    }
+                    for (int i = 0; i < Q; ++i) o[i][n] = mfma16(d, ph[i][c], o[i][n]);
+                }
             }
         };
-        if (cur.coded) {
+        // (a wave whose rows see nothing of a tile only helps to stage it)
+        auto sees = [&](int64_t kt) { return kt * 64 <= wspan.last && kt * 64 + 63 >= wspan.first; };
+        if (from < coded_to) {
+            blocks.load(a, t.s, t.seq, slot, head, nullptr, from, coded_to, 1);
+            cur.take(blocks, 0, from);
             ask(cur);
             keep(0);
-        } else {
-            keep_pairs(cur, 0);
+            __syncthreads();
         }
-        __syncthreads();
-        for (int64_t kt = from; kt < to; ++kt) {
+        for (int64_t kt = from; kt < coded_to; ++kt) {
             T next = cur;
-            const bool more = kt + 1 < to;
+            const bool more = kt + 1 < coded_to;
             if (more) {
                 if (++at == Blocks<B>::TILES) {
                     at = 0;
-                    blocks.load(a, t.s, t.seq, slot, head, nullptr, kt + 1, to, 1);
+                    blocks.load(a, t.s, t.seq, slot, head, nullptr, kt + 1, coded_to, 1);
                 }
                 next.take(blocks, at, kt + 1);
-                if (next.coded) ask(next);
+                ask(next);
             }
-            // (a wave whose rows see nothing of the tile only helps to stage)
-            if (kt * 64 <= wspan.last && kt * 64 + 63 >= wspan.first) {
-                if (__builtin_expect(cur.coded, true))
-                    compute(std::false_type());
-                else
-                    compute(std::true_type());
-            }
+            if (sees(kt)) compute(std::false_type());
             if (more) {
-                // both buffers are in use where a tile has residuals
-                if (!cur.coded || !next.coded) __syncthreads();
-                if (next.coded)
-                    keep(buf ^ 1);
-                else
-                    keep_pairs(next, buf ^ 1);
+                keep(buf ^ 1);
                 __syncthreads();
                 buf ^= 1;
                 cur = next;
             }
+        }
+        if (ring) {
+            __syncthreads();   // both buffers are written
+            blocks.load(a, t.s, t.seq, slot, head, nullptr, to - 1, to, 1);
+            cur.take(blocks, 0, to - 1);
+            buf = 0;
+            keep_pairs(cur, 0);
+            __syncthreads();
+            if (sees(to - 1)) compute(std::true_type());
         }
     }
 
