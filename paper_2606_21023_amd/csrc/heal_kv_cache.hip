@@ -50,55 +50,153 @@ __device__ __forceinline__ void rotate(float &a, float &b, float co, float si)
     b = (float)(y * c + x * s);
 }
 
-// One block of one head, keys or values: rows staged in LDS as FP32, one more
-// element per row than dim so that columns spread over the banks.
-template <int D, int B>
-struct Stage {
-    float x[B][D + 1];
-    double sum[kThreads / D][D];
-    uint32_t part[kThreads / 64];
+// A row's columns c .. c + 3 as they lie in memory, and the rotation of rows whose
+// columns are taken four pairs at a time: the first elements of the pairs and the second
+// ones lie rot / 2 apart, or alternate.
+struct Turn {
+    int pairs;   // rot / 2
+    bool interleaved;
+    const float *cos, *sin;
+    int64_t places;
 };
 
-// New rows (place >= start) of block blk into the stage; keys are rotated.
-template <int D, int B, bool KEYS>
-__device__ __forceinline__ void stage_new(Stage<D, B> &st, const KvAppendArgs &a, const KvSeq &s,
-                                          int start, int head, int64_t blk)
+// Whether rows at this address and stride can be read (written) in 16-byte units.
+__device__ __forceinline__ bool units16(const float *p, int64_t token, int64_t head)
 {
-    const float *src = KEYS ? a.k : a.v;
+    return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)((token | head) * 4)) & 15u) == 0;
+}
+
+__device__ __forceinline__ void store4(float *p, f32x4 x, bool vec)
+{
+    if (vec) {
+        *reinterpret_cast<f32x4 *>(p) = x;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = x[e];
+    }
+}
+
+// One row's elements, rotated if its place is in the table, four at a time: unit u of
+// D / 4.  The units of the rotated part come in pairs that hold each other's partners,
+// and unit u < rot / 8 does both; f(column, four elements) takes what comes out.
+// Needs rot % 8 == 0.
+template <class F>
+__device__ __forceinline__ void turn_unit(const Turn &t, const float *src, bool vec, int u, bool turn, int64_t p, F f)
+{
+    const int two = t.pairs / 4;   // units that do two
+    if (u >= two) {                // behind the rotated part
+        const int c = 2 * t.pairs + 4 * (u - two);
+        f(c, load4(src + c, vec));
+        return;
+    }
+    const int c0 = t.interleaved ? 8 * u : 4 * u, c1 = t.interleaved ? c0 + 4 : c0 + t.pairs;
+    f32x4 x = load4(src + c0, vec), y = load4(src + c1, vec);
+    if (turn) {
+        const float *co = t.cos + p * t.pairs + 4 * u, *si = t.sin + p * t.pairs + 4 * u;
+        float a[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = t.interleaved ? 2 * e : e, j = t.interleaved ? 2 * e + 1 : e + 4;
+            rotate(a[i], a[j], co[e], si[e]);
+        }
+        x = f32x4{a[0], a[1], a[2], a[3]};
+        y = f32x4{a[4], a[5], a[6], a[7]};
+    }
+    f(c0, x);
+    f(c1, y);
+}
+
+// ... one element, or one pair, at a time, for any even rot: unit u of D - rot / 2.
+template <class F>
+__device__ __forceinline__ void turn_pair(const Turn &t, const float *src, int u, bool turn, int64_t p, F f)
+{
+    if (u >= t.pairs) {
+        f(t.pairs + u, src[t.pairs + u]);
+        return;
+    }
+    const int c0 = t.interleaved ? 2 * u : u, c1 = t.interleaved ? c0 + 1 : c0 + t.pairs;
+    float x = src[c0], y = src[c1];
+    if (turn) rotate(x, y, t.cos[p * t.pairs + u], t.sin[p * t.pairs + u]);
+    f(c0, x);
+    f(c1, y);
+}
+
+// One block of one head, keys or values: rows staged in LDS as FP32.  Keys go in and
+// out by rows, in 16-byte units; values come out by columns, four rows apart, which an
+// odd row length spreads over the banks.
+template <int D, int B>
+struct Stage {
+    union {
+        float k[B][D + 4];
+        float v[B][D + 1];
+    };
+    double sum[kThreads / D][D];
+    uint32_t part[kThreads / 64];
+
+    template <bool KEYS>
+    __device__ __forceinline__ void put(int r, int c, f32x4 x)
+    {
+        if (KEYS) {
+            *reinterpret_cast<f32x4 *>(&k[r][c]) = x;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[r][c + e] = x[e];
+        }
+    }
+    template <bool KEYS>
+    __device__ __forceinline__ float &at(int r, int c)
+    {
+        return KEYS ? k[r][c] : v[r][c];
+    }
+};
+
+__device__ __forceinline__ uint32_t max_bits(uint32_t m, f32x4 x)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float y = x[e];
+        m = max(m, __builtin_bit_cast(uint32_t, y) & 0x7fffffffu);
+    }
+    return m;
+}
+
+// New rows (place >= start) of block blk into the stage, rotated if they are keys, and
+// the largest of m and their elements.
+template <int D, int B, bool KEYS>
+__device__ __forceinline__ uint32_t stage_new(Stage<D, B> &st, const KvAppendArgs &a, const KvSeq &s,
+                                              int start, int head, int64_t blk, uint32_t m)
+{
+    const float *src = (KEYS ? a.k : a.v) + head * (KEYS ? a.k_head : a.v_head);
     const int64_t ts = KEYS ? a.k_token : a.v_token;
-    src += head * (KEYS ? a.k_head : a.v_head);
-    const bool vec = ((reinterpret_cast<uintptr_t>(src) | (uintptr_t)(ts * 4)) & 15u) == 0;
+    const bool vec = units16(src, ts, 0);
     const int64_t p0 = blk * B;
     const int lo = p0 < start ? (int)(start - p0) : 0;
     const int hi = s.len - p0 < B ? (int)(s.len - p0) : B;
     const int64_t tok0 = (int64_t)s.first + (p0 - (s.len - s.n));
-    for (int i = threadIdx.x; i < (hi - lo) * (D / 4); i += kThreads) {
-        const int r = lo + i / (D / 4), c = i % (D / 4) * 4;
-        const f32x4 v = load4(src + (tok0 + r) * ts + c, vec);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) st.x[r][c + e] = v[e];
+    const Turn t = {KEYS ? a.rot / 2 : 0, a.interleaved != 0, a.cos, a.sin, a.places};
+    if (t.pairs % 4 == 0) {
+        // threads stay in their columns: one division for all rows
+        const int units = D / 4 - t.pairs / 4, step = kThreads / units, u = threadIdx.x % units;
+        for (int r = lo + threadIdx.x / units; r < hi && (int)threadIdx.x < step * units; r += step)
+            turn_unit(t, src + (tok0 + r) * ts, vec, u, p0 + r < t.places, p0 + r, [&](int c, f32x4 x) {
+                st.template put<KEYS>(r, c, x);
+                m = max_bits(m, x);
+            });
+    } else {
+        const int units = D - t.pairs, step = kThreads / units, u = threadIdx.x % units;
+        for (int r = lo + threadIdx.x / units; r < hi && (int)threadIdx.x < step * units; r += step)
+            turn_pair(t, src + (tok0 + r) * ts, u, p0 + r < t.places, p0 + r, [&](int c, float x) {
+                st.template at<KEYS>(r, c) = x;
+                m = max(m, __builtin_bit_cast(uint32_t, x) & 0x7fffffffu);
+            });
     }
-    __syncthreads();
-    if (KEYS && a.rot > 0) {
-        const int half = a.rot / 2;
-        for (int i = threadIdx.x; i < (hi - lo) * half; i += kThreads) {
-            const int r = lo + i / half, j = i % half;
-            const int64_t p = p0 + r;
-            if (p >= a.places) continue;
-            const int ja = a.interleaved ? 2 * j : j, jb = a.interleaved ? 2 * j + 1 : j + half;
-            float x = st.x[r][ja], y = st.x[r][jb];
-            rotate(x, y, a.cos[p * half + j], a.sin[p * half + j]);
-            st.x[r][ja] = x;
-            st.x[r][jb] = y;
-        }
-        __syncthreads();
-    }
+    return m;
 }
 
 // The staged new rows of block blk into the sequence's ring.
 template <int D, int B, bool KEYS>
-__device__ __forceinline__ void store_ring(const Stage<D, B> &st, const KvAppendArgs &a,
-                                           const KvSeq &s, int start, int head, int64_t blk, int slot)
+__device__ __forceinline__ void store_ring(Stage<D, B> &st, const KvAppendArgs &a, const KvSeq &s, int start,
+                                           int head, int64_t blk, int slot)
 {
     const int64_t p0 = blk * B;
     const int lo = p0 < start ? (int)(start - p0) : 0;
@@ -106,14 +204,16 @@ __device__ __forceinline__ void store_ring(const Stage<D, B> &st, const KvAppend
     const int half = (int)(blk & 1) * B;
     const int64_t base = ((int64_t)slot * a.c.heads + head) * (2 * B * D);
     if (KEYS) {
-        for (int i = threadIdx.x; i < (hi - lo) * D; i += kThreads) {
-            const int r = lo + i / D, c = i % D;
-            a.c.kr[base + (int64_t)(half + r) * D + c] = st.x[r][c];
+        for (int i = lo * (D / 4) + threadIdx.x; i < hi * (D / 4); i += kThreads) {
+            const int r = i / (D / 4), c = i % (D / 4) * 4;
+            *reinterpret_cast<f32x4 *>(a.c.kr + base + (half + r) * D + c) = *reinterpret_cast<const f32x4 *>(&st.k[r][c]);
         }
+    } else if (hi - lo == 1) {   // one token: a thread to a column
+        for (int c = threadIdx.x; c < D; c += kThreads) a.c.vr[base + c * (2 * B) + half + lo] = st.v[lo][c];
     } else {
-        for (int i = threadIdx.x; i < (hi - lo) * D; i += kThreads) {
-            const int c = i / (hi - lo), r = lo + i % (hi - lo);
-            a.c.vr[base + (int64_t)c * (2 * B) + half + r] = st.x[r][c];
+        for (int i = threadIdx.x; i < B * D; i += kThreads) {
+            const int c = i / B, r = i % B;
+            if (r >= lo && r < hi) a.c.vr[base + c * (2 * B) + half + r] = st.v[r][c];
         }
     }
 }
@@ -132,42 +232,74 @@ __device__ __forceinline__ void append_block(Stage<D, B> &st, const KvAppendArgs
     const int64_t p0 = blk * B;
     const int old = p0 < t.start ? (int)(t.start - p0) : 0;   // rows from the ring
     const int rows = s.len - p0 < B ? (int)(s.len - p0) : B;
+    const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    uint32_t m = 0u;
 
-    // rows of the ring (zeros without one), and zeros behind the last row
+    // rows of the ring (zeros without one); keys by rows, values by columns
     const int64_t base = ((int64_t)slot * a.c.heads + head) * (2 * B * D);
     const int half = (int)(blk & 1) * B;
-    for (int i = threadIdx.x; i < old * D; i += kThreads) {
-        if (KEYS) {
-            const int r = i / D, c = i % D;
-            st.x[r][c] = slot >= 0 ? a.c.kr[base + (int64_t)(half + r) * D + c] : 0.0f;
-        } else {
-            const int c = i / old, r = i % old;
-            st.x[r][c] = slot >= 0 ? a.c.vr[base + (int64_t)c * (2 * B) + half + r] : 0.0f;
+    if (KEYS) {
+        for (int i = threadIdx.x; i < old * (D / 4); i += kThreads) {
+            const int r = i / (D / 4), c = i % (D / 4) * 4;
+            const f32x4 x = slot >= 0 ? *reinterpret_cast<const f32x4 *>(a.c.kr + base + (half + r) * D + c) : zero;
+            st.template put<KEYS>(r, c, x);
+            m = max_bits(m, x);
+        }
+        // (zeros behind the last row add nothing to the mean)
+        for (int i = rows * (D / 4) + threadIdx.x; i < B * (D / 4); i += kThreads)
+            st.template put<KEYS>(i / (D / 4), i % (D / 4) * 4, zero);
+    } else if (old > 0) {
+        for (int i = threadIdx.x; i < D * (B / 4); i += kThreads) {
+            const int c = i / (B / 4), r = i % (B / 4) * 4;
+            if (r >= old) continue;
+            const f32x4 x = slot >= 0 ? *reinterpret_cast<const f32x4 *>(a.c.vr + base + c * (2 * B) + half + r) : zero;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (r + e < old) {
+                    const float y = x[e];
+                    st.v[r + e][c] = y;
+                    m = max(m, __builtin_bit_cast(uint32_t, y) & 0x7fffffffu);
+                }
         }
     }
-    for (int i = threadIdx.x; i < (B - rows) * D; i += kThreads) st.x[rows + i / D][i % D] = 0.0f;
-    stage_new<D, B, KEYS>(st, a, s, t.start, head, blk);
+    m = stage_new<D, B, KEYS>(st, a, s, t.start, head, blk, m);
+    m = max_over_workgroup(m, st.part);   // (and the rows are there for all)
 
     const int conflict = kv_ring_conflict(t);
     if (slot >= 0 && blk >= t.last - 1 && blk != conflict)
         store_ring<D, B, KEYS>(st, a, s, t.start, head, blk, slot);
 
     if (page >= 0) {
-        uint32_t m = 0u;
-        for (int i = threadIdx.x; i < rows * D; i += kThreads)
-            m = max(m, __builtin_bit_cast(uint32_t, st.x[i / D][i % D]) & 0x7fffffffu);
-        m = max_over_workgroup(m, st.part);
         const float mf = __builtin_bit_cast(float, m);
         const int64_t ph = (int64_t)page * a.c.heads + head;
         if (threadIdx.x == 0) a.c.scales[2 * ph + (KEYS ? 0 : 1)] = mf;
+        if (rows == B) {
+            const bool none = !(mf > 0.0f);
+            const double md = none ? 1.0 : (double)mf, inv = 1.0 / md;
+            uint32_t *out = reinterpret_cast<uint32_t *>(KEYS ? a.c.kc : a.c.vc) + ph * (B * D / 4);
+            for (int i = threadIdx.x; i < B * D / 4; i += kThreads) {
+                f32x4 x;
+                if (KEYS) {
+                    x = *reinterpret_cast<const f32x4 *>(&st.k[i / (D / 4)][i % (D / 4) * 4]);
+                } else {
+                    // dword i of [D][B]: value places 4 q .. 4 q + 3 of column i / (B / 4)
+                    const int q = i % (B / 4), r = 16 * (q % (B / 16)) + 4 * (q / (B / 16));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = st.v[r + e][i / (B / 4)];
+                }
+                uint32_t w = 0u;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w |= (uint32_t)(none ? 0 : code_i8(x[e], md, inv) & 0xff) << (8 * e);
+                out[i] = w;
+            }
+        }
         if (KEYS) {
-            // the mean: FP64 sums over whole parts of the block (zeros behind the last
-            // row add nothing), joined in their order
+            // the mean: FP64 sums over whole parts of the block, joined in their order
             constexpr int P = kThreads / D;
             const int c = threadIdx.x % D, w = threadIdx.x / D;
             if (w < P) {
                 double sum = 0.0;
-                for (int r = w * (B / P); r < (w + 1) * (B / P); ++r) sum += (double)st.x[r][c];
+                for (int r = w * (B / P); r < (w + 1) * (B / P); ++r) sum += (double)st.k[r][c];
                 st.sum[w][c] = sum;
             }
             __syncthreads();
@@ -178,33 +310,13 @@ __device__ __forceinline__ void append_block(Stage<D, B> &st, const KvAppendArgs
                 a.c.mean[ph * D + threadIdx.x] = (float)(sum / (double)rows);
             }
         }
-        if (rows == B) {
-            const bool zero = !(mf > 0.0f);
-            const double md = zero ? 1.0 : (double)mf, inv = 1.0 / md;
-            uint32_t *out = reinterpret_cast<uint32_t *>(KEYS ? a.c.kc : a.c.vc) + ph * (B * D / 4);
-            for (int i = threadIdx.x; i < B * D / 4; i += kThreads) {
-                uint32_t w = 0u;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float x;
-                    if (KEYS) {
-                        x = st.x[i / (D / 4)][i % (D / 4) * 4 + e];
-                    } else {
-                        // dword i of [D][B]: value places 4 q .. 4 q + 3 of column i / (B / 4)
-                        const int q = i % (B / 4), g = q / (B / 16), sb = q % (B / 16);
-                        x = st.x[16 * sb + 4 * g + e][i / (B / 4)];
-                    }
-                    w |= (uint32_t)(zero ? 0 : code_i8(x, md, inv) & 0xff) << (8 * e);
-                }
-                out[i] = w;
-            }
-        }
     }
 
     // ring rows of a later block where unit 0's old rows were
     if (unit == 0 && conflict >= 0 && conflict < a.b.cols && slot >= 0) {
         __syncthreads();
-        stage_new<D, B, KEYS>(st, a, s, t.start, head, conflict);
+        stage_new<D, B, KEYS>(st, a, s, t.start, head, conflict, 0u);
+        __syncthreads();
         store_ring<D, B, KEYS>(st, a, s, t.start, head, conflict, slot);
     }
 }
@@ -212,25 +324,26 @@ __device__ __forceinline__ void append_block(Stage<D, B> &st, const KvAppendArgs
 // Queries of one token, rotated.
 __device__ __forceinline__ void rotate_queries(const KvAppendArgs &a, int64_t token)
 {
-    const int seq = kv_last_at_most(a.b.seqs, token, [&](int i) { return (int64_t)kv_first(a.b, i); });
+    const int seq = a.b.cu ? kv_last_at_most(a.b.seqs, token, [&](int i) { return (int64_t)kv_first(a.b, i); })
+                           : (int)token;
     const KvSeq s = kv_seq(a.b, seq);
     if (token < s.first || token >= (int64_t)s.first + s.n) return;
     const int64_t p = (int64_t)s.len - s.n + (token - s.first);
     const bool turn = p >= 0 && p < a.places;
-    const int half = a.rot / 2, D = a.c.dim, rest = D - a.rot;
+    const Turn t = {a.rot / 2, a.interleaved != 0, a.cos, a.sin, a.places};
     const float *src = a.q + token * a.q_token;
     float *dst = a.q_out + token * a.qo_token;
-    for (int i = threadIdx.x; i < a.heads_q * half; i += kThreads) {
-        const int h = i / half, j = i % half;
-        const int ja = a.interleaved ? 2 * j : j, jb = a.interleaved ? 2 * j + 1 : j + half;
-        float x = src[h * a.q_head + ja], y = src[h * a.q_head + jb];
-        if (turn) rotate(x, y, a.cos[p * half + j], a.sin[p * half + j]);
-        dst[h * a.qo_head + ja] = x;
-        dst[h * a.qo_head + jb] = y;
-    }
-    for (int i = threadIdx.x; i < a.heads_q * rest; i += kThreads) {
-        const int h = i / rest, j = a.rot + i % rest;
-        dst[h * a.qo_head + j] = src[h * a.q_head + j];
+    const int D = a.c.dim;
+    if (t.pairs % 4 == 0) {
+        const bool in = units16(src, 0, a.q_head), out = units16(dst, 0, a.qo_head);
+        const int units = D / 4 - t.pairs / 4, step = kThreads / units, u = threadIdx.x % units;
+        for (int h = threadIdx.x / units; h < a.heads_q && (int)threadIdx.x < step * units; h += step)
+            turn_unit(t, src + h * a.q_head, in, u, turn, p,
+                      [&](int c, f32x4 x) { store4(dst + h * a.qo_head + c, x, out); });
+    } else {
+        const int units = D - t.pairs, step = kThreads / units, u = threadIdx.x % units;
+        for (int h = threadIdx.x / units; h < a.heads_q && (int)threadIdx.x < step * units; h += step)
+            turn_pair(t, src + h * a.q_head, u, turn, p, [&](int c, float x) { dst[h * a.qo_head + c] = x; });
     }
 }
 
@@ -247,7 +360,7 @@ kv_append_kernel(KvAppendArgs a, int64_t wg0, int64_t blocks_wg)
     }
     const int64_t u = wg / (2 * a.c.heads);
     const int role = (int)(wg % (2 * a.c.heads));
-    const int seq = kv_last_at_most(a.b.seqs, u, [&](int i) { return kv_unit(a.b, B, i); });
+    const int seq = a.b.cu ? kv_last_at_most(a.b.seqs, u, [&](int i) { return kv_unit(a.b, B, i); }) : (int)u;
     const int64_t j = u - kv_unit(a.b, B, seq);
     if (j < 0) return;
     if (role < a.c.heads)
@@ -256,12 +369,16 @@ kv_append_kernel(KvAppendArgs a, int64_t wg0, int64_t blocks_wg)
         append_block<D, B, false>(st, a, seq, (int)j, role - a.c.heads);
 }
 
-// One block of one head back as FP32 rows.
+// One block of one head back as FP32 rows.  Values are turned in LDS: codes with four
+// bytes, FP32 rows with one element more to a column.
 template <int D, int B>
 __global__ void __launch_bounds__(kThreads)
 kv_read_kernel(KvSeqs b, KvCache c, float *k, float *v, int64_t wg0)
 {
-    __shared__ uint32_t codes[B * D / 4];
+    __shared__ union {
+        uint32_t codes[D][B / 4 + 1];
+        float rows[D][B + 1];
+    } x;
     const int64_t wg = wg0 + blockIdx.x;
     const int64_t u = wg / (2 * c.heads);
     const int role = (int)(wg % (2 * c.heads));
@@ -269,12 +386,14 @@ kv_read_kernel(KvSeqs b, KvCache c, float *k, float *v, int64_t wg0)
     const int head = keys ? role : role - c.heads;
     float *out = keys ? k : v;
     if (!out) return;
-    const int seq = kv_last_at_most(b.seqs, u, [&](int i) { return kv_unit(b, B, i); });
+    const int seq = b.cu ? kv_last_at_most(b.seqs, u, [&](int i) { return kv_unit(b, B, i); }) : (int)u;
     const int64_t j = u - kv_unit(b, B, seq);
     if (j < 0) return;
     const KvSeq s = kv_seq(b, seq);
     const KvTouched t = kv_touched(s, B);
     const int64_t ld = (int64_t)c.heads * D;
+    const bool vec = (reinterpret_cast<uintptr_t>(out) & 15u) == 0;
+    const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
     out += head * D;
     if (j == 0)   // tokens before place 0 are nowhere
         for (int64_t i = threadIdx.x; i < (int64_t)(s.n - s.len) * D; i += kThreads)
@@ -288,29 +407,50 @@ kv_read_kernel(KvSeqs b, KvCache c, float *k, float *v, int64_t wg0)
     const int page = blk < b.cols ? kv_page(b, seq, (int)blk) : -1;
     const int slot = kv_slot(b, seq);
     const bool full = p0 + B <= s.len;
-    if (page < 0 || (!full && slot < 0)) {
-        for (int i = threadIdx.x; i < (hi - lo) * D; i += kThreads)
-            out[(int64_t)(lo + i / D) * ld + i % D] = 0.0f;
-    } else if (full) {
-        const int64_t ph = (int64_t)page * c.heads + head;
-        const uint32_t *src = reinterpret_cast<const uint32_t *>(keys ? c.kc : c.vc) + ph * (B * D / 4);
-        const float step = c.scales[2 * ph + (keys ? 0 : 1)] / 127.0f;
-        for (int i = threadIdx.x; i < B * D / 4; i += kThreads) codes[i] = src[i];
+    const bool held = page >= 0 && (full || slot >= 0);
+    const int64_t ph = (int64_t)page * c.heads + head;
+    const int64_t ring = ((int64_t)slot * c.heads + head) * (2 * B * D);
+    const int half = (int)(blk & 1) * B;
+    if (held && !keys) {
+        if (full) {
+            const uint32_t *src = reinterpret_cast<const uint32_t *>(c.vc) + ph * (B * D / 4);
+            for (int i = threadIdx.x; i < B * D / 4; i += kThreads) x.codes[i / (B / 4)][i % (B / 4)] = src[i];
+        } else {
+            for (int i = threadIdx.x; i < B * D / 4; i += kThreads) {
+                const int col = i / (B / 4), r = i % (B / 4) * 4;
+                if (r >= hi) continue;
+                const f32x4 y = *reinterpret_cast<const f32x4 *>(c.vr + ring + col * (2 * B) + half + r);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x.rows[col][r + e] = y[e];
+            }
+        }
         __syncthreads();
-        const int8_t *x = reinterpret_cast<const int8_t *>(codes);
-        for (int i = threadIdx.x; i < (hi - lo) * D; i += kThreads) {
-            const int r = lo + i / D, col = i % D;
-            const int8_t q = keys ? x[r * D + col] : x[col * B + kv_value_place(B, r)];
-            out[(int64_t)r * ld + col] = (float)q * step;
+    }
+    const float step = held && full ? c.scales[2 * ph + (keys ? 0 : 1)] / 127.0f : 0.0f;
+    for (int i = lo * (D / 4) + threadIdx.x; i < hi * (D / 4); i += kThreads) {
+        const int r = i / (D / 4), col = i % (D / 4) * 4;
+        f32x4 y = zero;
+        if (held && full) {
+            uint32_t w;
+            if (keys) {
+                w = reinterpret_cast<const uint32_t *>(c.kc)[ph * (B * D / 4) + i];
+            } else {
+                const int at = kv_value_place(B, r);
+                w = 0u;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w |= (x.codes[col + e][at / 4] >> (at % 4 * 8) & 0xffu) << (8 * e);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = (float)(int8_t)(w >> (8 * e)) * step;
+        } else if (held) {
+            if (keys) {
+                y = *reinterpret_cast<const f32x4 *>(c.kr + ring + (half + r) * D + col);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = x.rows[col + e][r];
+            }
         }
-    } else {
-        const int64_t base = ((int64_t)slot * c.heads + head) * (2 * B * D);
-        const int half = (int)(blk & 1) * B;
-        for (int i = threadIdx.x; i < (hi - lo) * D; i += kThreads) {
-            const int r = lo + i / D, col = i % D;
-            out[(int64_t)r * ld + col] = keys ? c.kr[base + (int64_t)(half + r) * D + col]
-                                              : c.vr[base + (int64_t)col * (2 * B) + half + r];
-        }
+        store4(out + (int64_t)r * ld + col, y, vec);
     }
 }
 
