@@ -370,14 +370,14 @@ kv_append_kernel(KvAppendArgs a, int64_t wg0, int64_t blocks_wg)
 }
 
 // One block of one head back as FP32 rows.  Values are turned in LDS: codes with four
-// bytes, FP32 rows with one element more to a column.
+// bytes, FP32 rows (32 columns at a time) with one element more to a column.
 template <int D, int B>
 __global__ void __launch_bounds__(kThreads)
 kv_read_kernel(KvSeqs b, KvCache c, float *k, float *v, int64_t wg0)
 {
     __shared__ union {
         uint32_t codes[D][B / 4 + 1];
-        float rows[D][B + 1];
+        float rows[32][B + 1];
     } x;
     const int64_t wg = wg0 + blockIdx.x;
     const int64_t u = wg / (2 * c.heads);
@@ -411,19 +411,30 @@ kv_read_kernel(KvSeqs b, KvCache c, float *k, float *v, int64_t wg0)
     const int64_t ph = (int64_t)page * c.heads + head;
     const int64_t ring = ((int64_t)slot * c.heads + head) * (2 * B * D);
     const int half = (int)(blk & 1) * B;
-    if (held && !keys) {
-        if (full) {
-            const uint32_t *src = reinterpret_cast<const uint32_t *>(c.vc) + ph * (B * D / 4);
-            for (int i = threadIdx.x; i < B * D / 4; i += kThreads) x.codes[i / (B / 4)][i % (B / 4)] = src[i];
-        } else {
-            for (int i = threadIdx.x; i < B * D / 4; i += kThreads) {
+    if (held && !keys && !full) {
+        for (int c0 = 0; c0 < D; c0 += 32) {
+            for (int i = threadIdx.x; i < 32 * (B / 4); i += kThreads) {
                 const int col = i / (B / 4), r = i % (B / 4) * 4;
                 if (r >= hi) continue;
-                const f32x4 y = *reinterpret_cast<const f32x4 *>(c.vr + ring + col * (2 * B) + half + r);
+                const f32x4 y = *reinterpret_cast<const f32x4 *>(c.vr + ring + (c0 + col) * (2 * B) + half + r);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x.rows[col][r + e] = y[e];
             }
+            __syncthreads();
+            for (int i = lo * 8 + threadIdx.x; i < hi * 8; i += kThreads) {
+                const int r = i / 8, col = i % 8 * 4;
+                f32x4 y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = x.rows[col + e][r];
+                store4(out + (int64_t)r * ld + c0 + col, y, vec);
+            }
+            __syncthreads();
         }
+        return;
+    }
+    if (held && !keys) {
+        const uint32_t *src = reinterpret_cast<const uint32_t *>(c.vc) + ph * (B * D / 4);
+        for (int i = threadIdx.x; i < B * D / 4; i += kThreads) x.codes[i / (B / 4)][i % (B / 4)] = src[i];
         __syncthreads();
     }
     const float step = held && full ? c.scales[2 * ph + (keys ? 0 : 1)] / 127.0f : 0.0f;
@@ -443,12 +454,7 @@ kv_read_kernel(KvSeqs b, KvCache c, float *k, float *v, int64_t wg0)
 #pragma unroll
             for (int e = 0; e < 4; ++e) y[e] = (float)(int8_t)(w >> (8 * e)) * step;
         } else if (held) {
-            if (keys) {
-                y = *reinterpret_cast<const f32x4 *>(c.kr + ring + (half + r) * D + col);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = x.rows[col + e][r];
-            }
+            y = *reinterpret_cast<const f32x4 *>(c.kr + ring + (half + r) * D + col);
         }
         store4(out + (int64_t)r * ld + col, y, vec);
     }
