@@ -24,7 +24,11 @@ namespace heal {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int64_t kWantedWorkgroups = 1024;
+// Two workgroups of either kernel fit on a compute unit.  Parts are cut until there are
+// as many (a decode step of 64 sequences 157 us; 162 with 768 or 1024, 188 with 2048; 48
+// of 512 blocks of 32 sequences 54, 67, 70 and 85).
+constexpr int64_t kWantedWorkgroups = 512;
+// Rows of a sequence, on average, from which 128-row tiles are taken.
 constexpr int64_t kWideRows = 64;
 constexpr int kNoScale = -100000;   // no value block with a scale seen yet
 
@@ -306,8 +310,16 @@ struct Tile {
 // s, the D/4 bytes of row r that belong to lanes g; of row 16 n + r of V^T, the four
 // bytes of each group that do.  (The block's address is the wave's, the lane's part an
 // unsigned 32-bit offset, hidden so that the two are not added outside the loop: no
-// 64-bit address per lane.)
-template <int D, int B>
+// 64-bit address per lane.)  ONCE: nobody else reads them, so they pass the caches by
+// (a decode step of 64 sequences 162 us, 179 with ordinary loads).
+template <bool ONCE, class X>
+__device__ __forceinline__ X load_codes(const int8_t *p)
+{
+    const X *x = reinterpret_cast<const X *>(p);
+    return ONCE ? __builtin_nontemporal_load(x) : *x;
+}
+
+template <int D, int B, bool ONCE>
 __device__ __forceinline__ void load_group_keys(const KvAttnArgs &a, const Tile<B> &t, int s, int head, int r, int g,
                                                 uint32_t *k)
 {
@@ -316,21 +328,21 @@ __device__ __forceinline__ void load_group_keys(const KvAttnArgs &a, const Tile<
     if constexpr (D % 64 == 0) {
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) {
-            const u32x4 w = *reinterpret_cast<const u32x4 *>(src + 16 * i + at);
+            const u32x4 w = load_codes<ONCE, u32x4>(src + 16 * i + at);
 #pragma unroll
             for (int e = 0; e < 4; ++e) k[4 * i + e] = w[e];
         }
     } else {
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
-            const u32x2 w = *reinterpret_cast<const u32x2 *>(src + 8 * i + at);
+            const u32x2 w = load_codes<ONCE, u32x2>(src + 8 * i + at);
             k[2 * i] = w[0];
             k[2 * i + 1] = w[1];
         }
     }
 }
 
-template <int D, int B>
+template <int D, int B, bool ONCE>
 __device__ __forceinline__ void load_column_values(const KvAttnArgs &a, const Tile<B> &t, int n, int head, int r, int g,
                                                    uint32_t *v)
 {
@@ -339,13 +351,13 @@ __device__ __forceinline__ void load_column_values(const KvAttnArgs &a, const Ti
     for (int i = 0; i < Tile<B>::NB; ++i) {
         const int8_t *src = a.c.vc + ((int64_t)t.page[i] * a.c.heads + head) * (B * D) + t.off / 4 + n * (16 * B);
         if constexpr (B == 16) {
-            v[i] = *reinterpret_cast<const uint32_t *>(src + at);
+            v[i] = load_codes<ONCE, uint32_t>(src + at);
         } else if constexpr (B == 32) {
-            const u32x2 w = *reinterpret_cast<const u32x2 *>(src + at);
+            const u32x2 w = load_codes<ONCE, u32x2>(src + at);
             v[2 * i] = w[0];
             v[2 * i + 1] = w[1];
         } else {
-            const u32x4 w = *reinterpret_cast<const u32x4 *>(src + at);
+            const u32x4 w = load_codes<ONCE, u32x4>(src + at);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = w[e];
         }
@@ -353,7 +365,7 @@ __device__ __forceinline__ void load_column_values(const KvAttnArgs &a, const Ti
 }
 
 // The codes of a whole tile.
-template <int D, int B>
+template <int D, int B, bool ONCE>
 struct Codes {
     static constexpr int N = D / 16;
     uint32_t k[4][D / 16], v[N][4];
@@ -361,12 +373,12 @@ struct Codes {
     __device__ __forceinline__ void load_keys(const KvAttnArgs &a, const Tile<B> &t, int head, int r, int g)
     {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) load_group_keys<D, B>(a, t, s, head, r, g, k[s]);
+        for (int s = 0; s < 4; ++s) load_group_keys<D, B, ONCE>(a, t, s, head, r, g, k[s]);
     }
     __device__ __forceinline__ void load_values(const KvAttnArgs &a, const Tile<B> &t, int head, int r, int g)
     {
 #pragma unroll
-        for (int n = 0; n < N; ++n) load_column_values<D, B>(a, t, n, head, r, g, v[n]);
+        for (int n = 0; n < N; ++n) load_column_values<D, B, ONCE>(a, t, n, head, r, g, v[n]);
     }
 };
 
@@ -570,7 +582,7 @@ __device__ __forceinline__ float unit_of(int ref)
 // LDS, and the waves' results are joined at the end.  The next tile's keys are asked
 // for as soon as this one's are in the matrix units, its values likewise, so that a
 // wave has 16 KiB on the way while it computes.
-template <int D, int B>
+template <int D, int B, bool ONCE>
 __global__ void __launch_bounds__(256, 2)
 kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
 {
@@ -578,7 +590,9 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
     using T = Tile<B>;
     __shared__ float part_o[W][16][D + 4];
     __shared__ float part_m[W][16], part_l[W][16];
+    // (every wave writes what it reads of these, the same values: registers are full)
     __shared__ int part_row[16], part_head[16];
+    __shared__ int32_t row_lo[16], row_hi[16];
     const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int64_t wg = wg0 + blockIdx.x;
     const int part = (int)(wg % a.parts);
@@ -590,8 +604,14 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
     const int row = t.row0 + r;
     const int64_t token = r < t.rows ? t.s.first + row / a.group : -1;
     const int head_q = head * a.group + row % a.group;
-    int32_t lo = 0, hi = -1;
-    if (r < t.rows) row_sees(a, t.s, row, lo, hi);
+    {
+        int32_t lo = 0, hi = -1;
+        if (r < t.rows) row_sees(a, t.s, row, lo, hi);
+        row_lo[r] = lo;
+        row_hi[r] = hi;
+        part_row[r] = (int)token;
+        part_head[r] = head_q;
+    }
 
     // tiles of this part: of the places from the tile of the first one seen, or of
     // the listed blocks
@@ -612,7 +632,7 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
         Blocks<B> blocks;
         blocks.load(a, t.s, t.seq, slot, head, list, from + wave, to, W);
         T cur;
-        Codes<D, B> codes;
+        Codes<D, B, ONCE> codes;
         cur.take(blocks, 0, from + wave);
         if (cur.coded) {
             codes.load_keys(a, cur, head, r, g);
@@ -670,7 +690,7 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
             for (int i = 0; i < T::NB; ++i)
                 all = all && cur.place(i * T::GS) >= span.all_lo && cur.place(i * T::GS) + T::GS * 16 - 1 <= span.all_hi;
             f16x8 ph[2], pl[2];
-            const float turn = soften<B>(cur, st, fk, all, &lo, &hi, g, w, ph, pl);
+            const float turn = soften<B>(cur, st, fk, all, row_lo + r, row_hi + r, g, w, ph, pl);
             if (__ballot(turn != 1.0f)) {
 #pragma unroll
                 for (int n = 0; n < N; ++n) o[n] *= turn;
@@ -713,8 +733,6 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
     if (g == 0) {
         part_m[wave][r] = w.m;
         part_l[wave][r] = sum;
-        part_row[r] = (int)token;
-        part_head[r] = head_q;
     }
     __syncthreads();
     const int rr = threadIdx.x >> 4, c0 = threadIdx.x & 15;
@@ -802,10 +820,10 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
         // staging: wave w takes the keys of group w and the values of column tiles w, w + 4
         uint32_t ks[D / 16], vs[NW][4];
         auto ask = [&](const T &x) {
-            load_group_keys<D, B>(a, x, wave, head, r, g, ks);
+            load_group_keys<D, B, false>(a, x, wave, head, r, g, ks);
 #pragma unroll
             for (int j = 0; j < NW; ++j)
-                if (N % 4 == 0 || wave + 4 * j < N) load_column_values<D, B>(a, x, wave + 4 * j, head, r, g, vs[j]);
+                if (N % 4 == 0 || wave + 4 * j < N) load_column_values<D, B, false>(a, x, wave + 4 * j, head, r, g, vs[j]);
         };
         auto keep = [&](int b) {
 #pragma unroll
@@ -1024,8 +1042,10 @@ hipError_t attention_sized(KvAttnArgs &a, const KvPlan &plan, hipStream_t stream
     hipError_t err = in_parts(n, [&](int64_t at, unsigned m) {
         if (plan.wide)
             hipLaunchKernelGGL((kv_prompt_kernel<D, B>), dim3(m), dim3(256), 0, stream, a, plan.tiles, at);
+        else if (plan.by_token && a.group <= 16)
+            hipLaunchKernelGGL((kv_attention_kernel<D, B, true>), dim3(m), dim3(256), 0, stream, a, true, at);
         else
-            hipLaunchKernelGGL((kv_attention_kernel<D, B>), dim3(m), dim3(256), 0, stream, a, plan.by_token, at);
+            hipLaunchKernelGGL((kv_attention_kernel<D, B, false>), dim3(m), dim3(256), 0, stream, a, plan.by_token, at);
     });
     if (err != hipSuccess || plan.parts == 1) return err;
     const int64_t rows = (int64_t)a.b.tokens * a.c.heads * a.group;
@@ -1057,7 +1077,7 @@ KvPlan kv_plan(int64_t tokens, int64_t seqs, bool ragged, int heads, int group, 
         // prompts' kernel two to a compute unit, which take equal parts (the bound on their
         // row tiles counts one too many for each sequence)
         const int64_t wgs = (p.wide ? p.tiles - seqs : p.tiles) * heads;
-        const int64_t wanted = wgs <= 0 ? 1 : p.wide ? 512 / wgs : (kWantedWorkgroups + wgs - 1) / wgs;
+        const int64_t wanted = wgs <= 0 ? 1 : p.wide ? kWantedWorkgroups / wgs : (kWantedWorkgroups + wgs - 1) / wgs;
         int64_t parts = wanted < (span + 3) / 4 ? wanted : (span + 3) / 4;
         parts = parts < 1 ? 1 : parts > 64 ? 64 : parts;
         part_tiles = ((span + parts - 1) / parts + 3) / 4 * 4;
