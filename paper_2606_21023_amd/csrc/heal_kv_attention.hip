@@ -237,7 +237,7 @@ struct Blocks {
         if (tile < to) blk = !a.sel ? (int)entry : entry < a.n_sel ? list[entry] : -1;
         if (blk >= 0) page = kv_page(a.b, seq, blk);
         const bool full = (int64_t)blk * B + B <= s.len;
-        if (page < 0 || (!full && slot < 0)) {
+        if (page < 0 || (!full && (slot < 0 || (int64_t)blk * B >= s.len))) {
             blk = -1;
             page = 0;   // (its codes may be read: their weights are zeros)
         }
@@ -291,12 +291,14 @@ struct Tile {
         for (int i = 1; i < NB; ++i) y = s / GS == i ? x[i] : y;
         return y;
     }
-    // the factor of the scores with block i, but for the query's
-    __device__ __forceinline__ float key_factor(int i) const
+    // the factor of the scores with block i (of group s), but for the query's
+    __device__ __forceinline__ float key_factor(int i) const { return factor(blk[i], page[i], k[i]); }
+    __device__ __forceinline__ float key_factor_of(int s) const { return factor(blk_of(s), page_of(s), key_of(s)); }
+    static __device__ __forceinline__ float factor(int blk, int page, float k)
     {
-        if (blk[i] < 0) return 0.0f;
-        if (page[i] >= 0) return k[i] * (1.0f / 127.0f);
-        const int e = exponent(k[i]);
+        if (blk < 0) return 0.0f;
+        if (page >= 0) return k * (1.0f / 127.0f);
+        const int e = exponent(k);
         return ldexpf(1.0f, e == kNoScale ? 0 : e - 14);
     }
     // place of the first token of group s
@@ -421,36 +423,44 @@ __device__ __forceinline__ void keys_of_group(const KvAttnArgs &a, const Tile<B>
     }
 }
 
-// The lane's values of groups 2 c and 2 c + 1 in row 16 n + r of V^T, as FP16 pairs.
+// The lane's four values of group s in row 16 n + r of V^T: codes as they are, FP32
+// rows scaled by a power of two.
+template <int D, int B>
+__device__ __forceinline__ f32x4 values_of_group(const KvAttnArgs &a, const Tile<B> &t, int s, int n, int slot, int head,
+                                                 int64_t len, int r, int g)
+{
+    const int blk = t.blk_of(s), page = t.page_of(s), off = t.off + s % Tile<B>::GS * 16;
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (blk < 0) return x;
+    if (page >= 0) {
+        const int8_t *src = a.c.vc + ((int64_t)page * a.c.heads + head) * (B * D) + (16 * n + r) * B + g * (B / 4) + off / 4;
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(src);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) x[b] = (float)(int8_t)(w >> (8 * b));
+        return x;
+    }
+    const float *src = a.c.vr + ((int64_t)slot * a.c.heads + head) * (2 * B * D) + (int64_t)(16 * n + r) * (2 * B) + (blk & 1) * B + off + 4 * g;
+    const int e = exponent(t.value_of(s)), shift = e == kNoScale ? 0 : 7 - e;
+    const int64_t rows = len - t.place(s);
+    const f32x4 y = *reinterpret_cast<const f32x4 *>(src);
+#pragma unroll
+    for (int b = 0; b < 4; ++b) x[b] = 4 * g + b < rows ? ldexpf(y[b], shift) : 0.0f;
+    return x;
+}
+
+// ... of groups 2 c and 2 c + 1, as FP16 pairs.
 template <int D, int B>
 __device__ __forceinline__ void values_of_half(const KvAttnArgs &a, const Tile<B> &t, int c, int n, int slot, int head,
                                                int64_t len, int r, int g, f16x8 &hi, f16x8 &lo)
 {
     float x[8];
-    hi = lo = f16x8{};
-    bool pairs = false;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const int s = 2 * c + j, blk = t.blk_of(s), page = t.page_of(s), off = t.off + s % Tile<B>::GS * 16;
+        const f32x4 y = values_of_group<D, B>(a, t, 2 * c + j, n, slot, head, len, r, g);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) x[4 * j + b] = 0.0f;
-        if (blk < 0) continue;
-        if (page >= 0) {
-            const int8_t *src = a.c.vc + ((int64_t)page * a.c.heads + head) * (B * D) + (16 * n + r) * B + g * (B / 4) + off / 4;
-            const uint32_t w = *reinterpret_cast<const uint32_t *>(src);
-#pragma unroll
-            for (int b = 0; b < 4; ++b) x[4 * j + b] = (float)(int8_t)(w >> (8 * b));
-        } else {
-            const float *src = a.c.vr + ((int64_t)slot * a.c.heads + head) * (2 * B * D) + (int64_t)(16 * n + r) * (2 * B) + (blk & 1) * B + off + 4 * g;
-            const int e = exponent(t.value_of(s)), shift = e == kNoScale ? 0 : 7 - e;
-            const int64_t rows = len - t.place(s);
-            const f32x4 y = *reinterpret_cast<const f32x4 *>(src);
-#pragma unroll
-            for (int b = 0; b < 4; ++b) x[4 * j + b] = 4 * g + b < rows ? ldexpf(y[b], shift) : 0.0f;
-        }
-        pairs = true;
+        for (int b = 0; b < 4; ++b) x[4 * j + b] = y[b];
     }
-    if (pairs) pairs8(x, hi, lo);
+    pairs8(x, hi, lo);
 }
 
 // Where a row's result goes: its place in out, or in the workspace of its part.
@@ -571,6 +581,41 @@ __device__ __forceinline__ float soften(const Tile<B> &t, f32x4 *st, const float
     return turn;
 }
 
+// ... of one group s, four scores to a lane; the other half of the operand is zeros.
+template <int B>
+__device__ __forceinline__ float soften_group(const Tile<B> &t, int s, f32x4 st, float fk, int32_t lo, int32_t hi, int g,
+                                              Soft &w, f16x8 &ph, f16x8 &pl)
+{
+    const int32_t p0 = t.place(s);
+    const bool met = t.blk_of(s) >= 0 && p0 <= hi && p0 + 15 >= lo;
+    const float vm = met ? t.value_of(s) : 0.0f;
+    float big = -__builtin_inff();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int32_t p = p0 + 4 * g + e;
+        st[e] = met && p >= lo && p <= hi ? st[e] * fk : -__builtin_inff();
+        big = __builtin_fmaxf(big, st[e]);
+    }
+    const float mn = __builtin_fmaxf(w.m, max_over_groups(big));
+    const float mz = mn == -__builtin_inff() ? 0.0f : mn;
+    const float alpha = __builtin_amdgcn_exp2f(w.m - mz);
+    const int ev = exponent(vm), rn = max(w.ref, ev);
+    const float turn = w.ref == kNoScale ? alpha : ldexpf(alpha, w.ref - rn);
+    const float wv = t.page_of(s) >= 0 ? ldexpf(vm, 14 - rn) : ev == kNoScale ? 0.0f : ldexpf(127.0f, ev + 7 - rn);
+    float p[8] = {}, sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float x = __builtin_amdgcn_exp2f(st[e] - mz);
+        sum += x;
+        p[e] = x * wv;
+    }
+    pairs8(p, ph, pl);
+    w.m = mn;
+    w.l = w.l * alpha + sum;
+    w.ref = rn;
+    return turn;
+}
+
 // The factor of a finished output.
 __device__ __forceinline__ float unit_of(int ref)
 {
@@ -654,10 +699,9 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
             }
             const bool ask = more && next.coded;
 
-            // scores
-            f32x4 st[4];
-            float fk[T::NB];
             if (cur.coded) {
+                f32x4 st[4];
+                float fk[T::NB];
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
                     st[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -669,35 +713,20 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
                     }
                     if (s & 1) __builtin_amdgcn_sched_barrier(0);   // (two groups' keys as FP16 at a time)
                 }
-            } else {
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    st[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                    keys_of_group<D, B>(a, cur, s, slot, head, t.s.len, hidden(r), hidden(g), [&](int k, f16x8 h, f16x8 x) {
-                        st[s] = mfma16(h, qh[k], st[s]);
-                        st[s] = mfma16(h, ql[k], st[s]);
-                        st[s] = mfma16(x, qh[k], st[s]);
-                    });
-                    __builtin_amdgcn_sched_barrier(0);   // (rows of one group at a time in registers)
+                for (int i = 0; i < T::NB; ++i) fk[i] = cur.key_factor(i) * fq;
+                if (ask) codes.load_keys(a, next, head, r, g);
+
+                bool all = true;
+#pragma unroll
+                for (int i = 0; i < T::NB; ++i)
+                    all = all && cur.place(i * T::GS) >= span.all_lo && cur.place(i * T::GS) + T::GS * 16 - 1 <= span.all_hi;
+                f16x8 ph[2], pl[2];
+                const float turn = soften<B>(cur, st, fk, all, row_lo + r, row_hi + r, g, w, ph, pl);
+                if (__ballot(turn != 1.0f)) {
+#pragma unroll
+                    for (int n = 0; n < N; ++n) o[n] *= turn;
                 }
-            }
-#pragma unroll
-            for (int i = 0; i < T::NB; ++i) fk[i] = cur.key_factor(i) * fq;
-            if (ask) codes.load_keys(a, next, head, r, g);
-
-            bool all = cur.coded;
-#pragma unroll
-            for (int i = 0; i < T::NB; ++i)
-                all = all && cur.place(i * T::GS) >= span.all_lo && cur.place(i * T::GS) + T::GS * 16 - 1 <= span.all_hi;
-            f16x8 ph[2], pl[2];
-            const float turn = soften<B>(cur, st, fk, all, row_lo + r, row_hi + r, g, w, ph, pl);
-            if (__ballot(turn != 1.0f)) {
-#pragma unroll
-                for (int n = 0; n < N; ++n) o[n] *= turn;
-            }
-
-            // values
-            if (cur.coded) {
 #pragma unroll
                 for (int n = 0; n < N; ++n) {
 #pragma unroll
@@ -708,21 +737,75 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
                     }
                     if (n & 1) __builtin_amdgcn_sched_barrier(0);
                 }
-            } else {
-#pragma unroll
-                for (int n = 0; n < N; ++n)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        f16x8 h, x;
-                        values_of_half<D, B>(a, cur, c, n, slot, head, t.s.len, hidden(r), hidden(g), h, x);
-                        o[n] = mfma16(h, ph[c], o[n]);
-                        o[n] = mfma16(h, pl[c], o[n]);
-                        o[n] = mfma16(x, ph[c], o[n]);
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
+                if (ask) codes.load_values(a, next, head, r, g);
+            } else if (ask) {
+                codes.load_keys(a, next, head, r, g);
+                codes.load_values(a, next, head, r, g);
             }
-            if (ask) codes.load_values(a, next, head, r, g);
             cur = next;
+        }
+    }
+
+    // Tiles with FP32 rows, a group of 16 tokens to each wave: all that a wave needs of
+    // one is asked for at once, where one wave with the whole tile would have four times
+    // the bytes of a coded tile to wait for (8191 tokens of one sequence: 17.7 us, 12.5 so).
+    auto ring_tile = [&](int64_t kt) {
+        Blocks<B> blocks;
+        T tile;
+        blocks.load(a, t.s, t.seq, slot, head, list, kt, to, 1);
+        tile.take(blocks, 0, kt);
+        if (tile.coded || tile.blk_of(wave) < 0) return;
+        f16x8 qh[KC], ql[KC], kh[KC], kl[KC];
+        f32x4 v[N];
+        const float fq = load_query<D>(a, token < 0 ? nullptr : a.q + token * a.q_token + head_q * a.q_head + g * (D / 4), qh, ql);
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] = values_of_group<D, B>(a, tile, wave, n, slot, head, t.s.len, r, g);
+        keys_of_group<D, B>(a, tile, wave, slot, head, t.s.len, r, g, [&](int k, f16x8 h, f16x8 x) {
+            kh[k] = h;
+            kl[k] = x;
+        });
+        f32x4 st = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+            st = mfma16(kh[k], qh[k], st);
+            st = mfma16(kh[k], ql[k], st);
+            st = mfma16(kl[k], qh[k], st);
+        }
+        f16x8 ph, pl;
+        const float turn = soften_group<B>(tile, wave, st, tile.key_factor_of(wave) * fq, row_lo[r], row_hi[r], g, w, ph, pl);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const float x[8] = {v[n][0], v[n][1], v[n][2], v[n][3]};
+            f16x8 vh, vl;
+            pairs8(x, vh, vl);
+            o[n] *= turn;
+            o[n] = mfma16(vh, ph, o[n]);
+            o[n] = mfma16(vh, pl, o[n]);
+            o[n] = mfma16(vl, ph, o[n]);
+        }
+    };
+    if (t.s.len % B != 0 && span.last >= span.first) {
+        const int32_t rb = t.s.len / B;   // the block that is not complete
+        if (!a.sel) {
+            const int64_t kt = (int64_t)rb * B / 64 + (B > 64 ? t.s.len % B / 64 : 0);
+            for (int64_t x = (int64_t)rb * B / 64; x <= kt; ++x)
+                if (x >= from && x < to) ring_tile(x);
+        } else {
+            // wherever the lists have it, 64 entries at a time
+            constexpr int E = B < 64 ? 64 / B : 1, P = B > 64 ? B / 64 : 1;   // entries of a tile, tiles of an entry
+            for (int64_t e0 = from * E / P; e0 * P < to * E; e0 += 64) {
+                const int64_t e = e0 + lane;
+                uint64_t found = __ballot(e < a.n_sel && e * P < to * E && list[e] == rb);
+                while (found) {
+                    const int64_t at = e0 + __builtin_ctzll(found);
+                    const int64_t kt = at * P / E;
+                    for (int64_t x = kt; x < kt + P; ++x)
+                        if (x >= from && x < to) ring_tile(x);
+                    // (the other entries of that tile are done with it)
+                    found &= found - 1;
+                    while (found && (e0 + __builtin_ctzll(found)) * P / E == kt && P == 1) found &= found - 1;
+                }
+            }
         }
     }
 
