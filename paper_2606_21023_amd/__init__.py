@@ -465,6 +465,7 @@ class KVCache:
         self.blocks, self.slots, self.heads, self.dim, self.block = blocks, slots, heads, dim, block
         self.device = k_codes.device
         self._index = k_codes.get_device()
+        self._f32, self._i32 = torch.float32, torch.int32
         self._c = _CCache(blocks, slots, heads, dim, block, *(t.data_ptr() for t in arrays.values()))
         self._ref = ctypes.byref(self._c)
 
@@ -480,6 +481,10 @@ class KVCache:
                    f(blocks, heads, dim), f(slots, heads, 2 * block, dim), f(slots, heads, dim, 2 * block))
 
 
+# The checks of a decode step's tensors cost as much of the host's time as its launches
+# do, so what is right is recognised by its attributes first (0.3 us a tensor, 0.6 by the
+# checks that tell what is wrong), and only the rest is asked what is wrong with it.
+
 def _kv_on(cache, t, name):
     if t.get_device() != cache._index:
         raise HealError("%s is on %s, the cache on %s" % (name, t.device, cache.device))
@@ -493,8 +498,28 @@ def _kv_ints(cache, t, name, ndim, size=None):
     return shape, stride
 
 
+def _kv_list(cache, t, name, size):
+    """A dense int32 vector of that size on the cache's device; its address."""
+    try:
+        if (t.dtype is cache._i32 and t.get_device() == cache._index and t.shape == (size,)
+                and (size <= 1 or t.stride(0) == 1)):
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _kv_ints(cache, t, name, 1, size)
+    return t.data_ptr()
+
+
 def _kv_rows(cache, t, name, tokens=None, heads=None):
     """A (tokens, heads, dim) float32 tensor; returns shape, token and head strides."""
+    try:
+        shape, stride = t.shape, t.stride()
+        if (t.dtype is cache._f32 and t.get_device() == cache._index and len(shape) == 3
+                and shape[2] == cache.dim and stride[2] == 1 and (tokens is None or shape[0] == tokens)
+                and (heads is None or shape[1] == heads)):
+            return shape, stride[0], stride[1]
+    except AttributeError:
+        pass
     shape, stride = _tensor(t, name, torch.float32, 3)
     _kv_on(cache, t, name)
     if shape[2] != cache.dim or (tokens is not None and shape[0] != tokens) or (
@@ -510,20 +535,33 @@ def _kv_batch(cache, tokens, table, lens, cu, slots):
         raise HealError("cache must be a KVCache")
     if _device() != cache._index:
         raise HealError("the cache is on %s, the current device is another" % cache.device)
-    shape, stride = _kv_ints(cache, table, "table", 2)
-    seqs = shape[0]
-    _kv_ints(cache, lens, "lens", 1, seqs)
+    try:
+        shape, stride = table.shape, table.stride()
+        if not (table.dtype is cache._i32 and table.get_device() == cache._index and len(shape) == 2
+                and (stride[1] == 1 or shape[1] <= 1)):
+            shape = None
+    except AttributeError:
+        shape = None
+    if shape is None:
+        shape, stride = _kv_ints(cache, table, "table", 2)
+    seqs, cols = shape
     if cu is not None:
-        _kv_ints(cache, cu, "cu", 1, seqs + 1)
+        cu = _kv_list(cache, cu, "cu", seqs + 1)
     elif tokens != seqs:
         raise HealError("%d tokens of %d sequences need cu" % (tokens, seqs))
     if slots is not None:
-        _kv_ints(cache, slots, "slots", 1, seqs)
+        slots = _kv_list(cache, slots, "slots", seqs)
     elif seqs > cache.slots:
         raise HealError("%d sequences, the cache has %d slots" % (seqs, cache.slots))
-    return _CBatch(seqs, tokens, cu.data_ptr() if cu is not None else None, lens.data_ptr(),
-                   table.data_ptr(), _ld(shape, stride), shape[1],
-                   slots.data_ptr() if slots is not None else None)
+    return _CBatch(seqs, tokens, cu, _kv_list(cache, lens, "lens", seqs), table.data_ptr(),
+                   stride[0] if seqs > 1 else cols or 1, cols, slots)
+
+
+def _kv_new(cache, shape):
+    """A new float32 tensor beside the cache."""
+    like = cache.scales
+    return (like.new_empty(shape) if type(like) is torch.Tensor
+            else torch.empty(shape, dtype=torch.float32, device=cache.device))
 
 
 def _device():
@@ -536,6 +574,19 @@ def _device():
 def _kv_group(cache, heads_q):
     if heads_q < 1 or heads_q % cache.heads:
         raise HealError("%d query heads for %d key/value heads" % (heads_q, cache.heads))
+
+
+def _kv_angles(cache, t, name, like):
+    try:
+        shape = t.shape
+        if (t.dtype is cache._f32 and t.get_device() == cache._index and len(shape) == 2 and t.is_contiguous()
+                and (like is None or shape == like)):
+            return shape
+    except AttributeError:
+        pass
+    _tensor(t, name, torch.float32, 2)
+    _kv_on(cache, t, name)
+    raise HealError("cos and sin must be contiguous and of one shape")
 
 
 def heal_kv_append(cache, k, v, table, lens, cu=None, slots=None, cos=None, sin=None,
@@ -557,19 +608,18 @@ def heal_kv_append(cache, k, v, table, lens, cu=None, slots=None, cos=None, sin=
     if (cos is None) != (sin is None):
         raise HealError("cos and sin come together")
     if cos is not None:
-        for t, name in ((cos, "cos"), (sin, "sin")):
-            _tensor(t, name, torch.float32, 2)
-            _kv_on(cache, t, name)
-            if not t.is_contiguous() or t.shape != cos.shape:
-                raise HealError("cos and sin must be contiguous and of one shape")
-        places, rot = cos.shape[0], 2 * cos.shape[1]
+        shape = _kv_angles(cache, cos, "cos", None)
+        _kv_angles(cache, sin, "sin", shape)
+        places, rot = shape[0], 2 * shape[1]
     heads_q = q_token = q_head = qo_token = qo_head = 0
     if q is not None:
         shape, q_token, q_head = _kv_rows(cache, q, "q", tokens)
         heads_q = shape[1]
         if q_out is None:
-            q_out = torch.empty(tuple(shape), dtype=torch.float32, device=q.device)
-        _, qo_token, qo_head = _kv_rows(cache, q_out, "q_out", tokens, heads_q)
+            q_out = _kv_new(cache, shape)
+            qo_token, qo_head = heads_q * cache.dim, cache.dim
+        else:
+            _, qo_token, qo_head = _kv_rows(cache, q_out, "q_out", tokens, heads_q)
     elif q_out is not None:
         raise HealError("q_out without q")
     with_q = q is not None and q.numel() > 0
@@ -586,8 +636,8 @@ def heal_kv_read(cache, tokens, table, lens, cu=None, slots=None):
     sequence's last tokens (cu says how many).  Rows it does not hold are zeros;
     rows of no sequence are not written."""
     batch = _kv_batch(cache, tokens, table, lens, cu, slots)
-    k = torch.empty((tokens, cache.heads, cache.dim), dtype=torch.float32, device=cache.device)
-    v = torch.empty((tokens, cache.heads, cache.dim), dtype=torch.float32, device=cache.device)
+    shape = (tokens, cache.heads, cache.dim)
+    k, v = _kv_new(cache, shape), _kv_new(cache, shape)
     _check((_lib or lib()).heal_kv_read(cache._ref, ctypes.byref(batch), k.data_ptr(), v.data_ptr(),
                                         _stream()), "heal_kv_read")
     return k, v
@@ -644,21 +694,23 @@ def heal_kv_attention(cache, q, table, lens, cu=None, slots=None, scale=None, ca
     batch = _kv_batch(cache, tokens, table, lens, cu, slots)
     n_sel = _kv_sel(cache, sel, "sel", tokens) if sel is not None else 0
     if out is None:
-        out = torch.empty(tuple(shape), dtype=torch.float32, device=q.device)
-    _, out_token, out_head = _kv_rows(cache, out, "out", tokens, heads_q)
+        out = _kv_new(cache, shape)
+        out_token, out_head = heads_q * cache.dim, cache.dim
+    else:
+        _, out_token, out_head = _kv_rows(cache, out, "out", tokens, heads_q)
     if lse is not None:
         _tensor(lse, "lse", torch.float32, 2)
         _kv_on(cache, lse, "lse")
-        if tuple(lse.shape) != (tokens, heads_q) or not lse.is_contiguous():
+        if lse.shape != (tokens, heads_q) or not lse.is_contiguous():
             raise HealError("lse must be a contiguous (%d, %d) tensor" % (tokens, heads_q))
-    scale = cache.dim ** -0.5 if scale is None else scale
+    scale = cache.dim ** -0.5 if scale is None else float(scale)
     if tokens == 0:
         return out
     L, ref = _lib or lib(), ctypes.byref(batch)
     size = L.heal_kv_attention_workspace(cache._ref, ref, heads_q, window, n_sel, chunk)
-    space = torch.empty(size, dtype=torch.uint8, device=q.device) if size > 0 else None
+    space = _kv_new(cache, size // 4) if size > 0 else None
     _check(L.heal_kv_attention(
-        cache._ref, ref, q.data_ptr(), q_token, q_head, heads_q, ctypes.c_float(scale), 1 if causal else 0,
+        cache._ref, ref, q.data_ptr(), q_token, q_head, heads_q, scale, 1 if causal else 0,
         window, sel.data_ptr() if n_sel else None, n_sel, out.data_ptr(), out_token, out_head,
         lse.data_ptr() if lse is not None else None, chunk, space.data_ptr() if size > 0 else None,
         max(size, 0), _stream()), "heal_kv_attention")
