@@ -471,80 +471,90 @@ constexpr uint64_t kLowest = 0x000fffffffffffffull;   // the key of -infinity
 
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kSelectThreads = 512;
-
-// Key `i` of a lane: candidates lie 64 apart.  Up to kHeld of them are held in registers.
-constexpr int kHeld = 16;
-
-// How many candidates (n of them, in LDS at `key`) have a key of at least x.
-__device__ __forceinline__ int keys_from(const uint64_t *key, const uint64_t *held, int n, uint64_t x)
+// x, as a value that the compiler knows nothing of.
+__device__ __forceinline__ float hidden(float x)
 {
-    int c = 0;
-    if (n <= 64 * kHeld) {
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-            if (i * 64 < n) c += __popcll(__ballot(held[i] >= x));
-        }
-    } else {
-        const int lane = threadIdx.x & 63;
-        for (int i = 0; i < n; i += 64) c += __popcll(__ballot(i + lane < n && key[i + lane] >= x));
-    }
-    return c;
+    asm volatile("" : "+v"(x));
+    return x;
 }
 
-// The blocks of one token: the forced ones, and the r best of the n candidates whose
-// keys are in LDS.  One wave: the r-th largest key is found bit by bit from the first
-// bit in which the keys differ, ending where a threshold parts exactly r from the rest;
-// then the blocks above it, and the lowest of those equal to it, are written in order.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x)
+{
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+    return (uint64_t)hi << 32 | lo;
+}
+
+// The blocks of one token: the first lo, those from lo + n on, and the r best of the n
+// candidates between them, whose keys are in LDS.  One wave: the r-th largest key is found
+// bit by bit from the first bit in which the keys differ, ending where a threshold parts
+// exactly r from the rest; then the blocks above it, and the lowest of those equal to
+// it, are written in order.  A lane has candidates 64 apart, up to H of them in
+// registers (H = 0: any number, read from LDS each time).
+template <int H>
 __device__ __forceinline__ void pick_blocks(const uint64_t *key, int lo, int n, int nb, int r, int32_t *sel)
 {
     const int lane = threadIdx.x & 63;
-    uint64_t held[kHeld], top = 0u;
+    uint64_t held[H > 0 ? H : 1];
+#pragma unroll
+    for (int i = 0; i < H; ++i) held[i] = i * 64 + lane < n ? key[i * 64 + lane] : 0u;   // (no threshold is 0)
+    // f(the lane's key, its candidate, whether there is one) for all of them in order
+    auto each = [&](auto f) {
+        if (H > 0) {
+#pragma unroll
+            for (int i = 0; i < H; ++i) f(held[i], i * 64 + lane, i * 64 + lane < n);
+        } else {
+            for (int i = lane; i - lane < n; i += 64) f(i < n ? key[i] : 0u, i, i < n);
+        }
+    };
+    uint64_t top = 0u;
     int left = 0;
     if (r > 0) {
+        auto keys_from = [&](uint64_t x) {
+            int c = 0;
+            each([&](uint64_t k, int, bool) { c += __popcll(__ballot(k >= x)); });
+            return c;
+        };
         uint64_t most = 0u, least = ~0ull;
-        if (n <= 64 * kHeld) {
-#pragma unroll
-            for (int i = 0; i < kHeld; ++i) held[i] = i * 64 + lane < n ? key[i * 64 + lane] : 0u;
-        }
-        for (int i = lane; i < n; i += 64) {
-            const uint64_t k = key[i];
+        each([&](uint64_t k, int, bool is) {
             most = k > most ? k : most;
-            least = k < least ? k : least;
-        }
+            least = is && k < least ? k : least;
+        });
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) {
             const uint64_t x = __shfl_xor(most, off), y = __shfl_xor(least, off);
             most = x > most ? x : most;
             least = y < least ? y : least;
         }
+        most = uniform(most);
+        least = uniform(least);
         top = most;
         if (most != least) {
             int bit = 63 - __builtin_clzll(most ^ least);
             top = bit == 63 ? 0u : most >> (bit + 1) << (bit + 1);
             for (; bit >= 0; --bit) {
                 const uint64_t x = top | 1ull << bit;
-                const int c = keys_from(key, held, n, x);
+                const int c = keys_from(x);
                 if (c >= r) top = x;
                 if (c == r) break;
             }
         }
-        left = r - (top == ~0ull ? 0 : keys_from(key, held, n, top + 1));
+        left = r - (top == ~0ull ? 0 : keys_from(top + 1));
     }
-    int at = 0, equals = 0;
-    const uint64_t before = (1ull << lane) - 1;
-    for (int b0 = 0; b0 < nb; b0 += 64) {
-        const int b = b0 + lane;
-        const bool forced = b < nb && (b < lo || b >= lo + n);
-        const bool cand = r > 0 && b >= lo && b < lo + n;
-        const uint64_t x = cand ? key[b - lo] : 0u;
-        const uint64_t same = __ballot(cand && x == top);
-        const bool take = forced || (cand && (x > top || (x == top && equals + __popcll(same & before) < left)));
-        const uint64_t taken = __ballot(take);
-        if (take) sel[at + __popcll(taken & before)] = b;
-        at += __popcll(taken);
-        equals += __popcll(same);
+    for (int b = lane; b < lo; b += 64) sel[b] = b;
+    int at = lo, equals = 0;
+    if (r > 0) {
+        const uint64_t before = (1ull << lane) - 1;
+        each([&](uint64_t k, int i, bool is) {
+            const uint64_t same = __ballot(is && k == top);
+            const bool take = is && (k > top || (k == top && equals + __popcll(same & before) < left));
+            const uint64_t taken = __ballot(take);
+            if (take) sel[at + __popcll(taken & before)] = lo + i;
+            at += __popcll(taken);
+            equals += __popcll(same);
+        });
     }
+    for (int b = lo + n + lane; b < nb; b += 64) sel[at + b - (lo + n)] = b;
 }
 
 // One workgroup per key/value head and `slots` tokens of one sequence (1 or 4).
@@ -556,13 +566,14 @@ __device__ __forceinline__ void pick_blocks(const uint64_t *key, int lo, int n, 
 // it), so the maximum over a token's queries is taken within the lane; with one
 // token the 16 rows are its queries.  The order of the sum is the same for every block,
 // so equal blocks score equally.
-template <int D>
-__global__ void __launch_bounds__(kSelectThreads)
-kv_select_kernel(KvSelectArgs a, int B, int slots, int64_t wg0)
+template <int D, int SLOTS>
+__global__ void __launch_bounds__(SLOTS == 1 ? 512 : 256, 4)
+kv_select_kernel(KvSelectArgs a, int B, int64_t wg0)
 {
+    constexpr int slots = SLOTS, kSelectThreads = SLOTS == 1 ? 512 : 256;
     extern __shared__ char lds[];
     uint64_t *key = reinterpret_cast<uint64_t *>(lds);   // [slots][cols]
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, kk = lane >> 4;
+    const int wave = uniform((int)threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, kk = lane >> 4;
     const int64_t wg = wg0 + blockIdx.x;
     const int64_t u = wg / a.c.heads;
     const int head = (int)(wg % a.c.heads);
@@ -570,12 +581,14 @@ kv_select_kernel(KvSelectArgs a, int B, int slots, int64_t wg0)
     int64_t first;   // token of slot 0
     if (slots == 1) {
         first = u;
-        seq = kv_last_at_most(a.b.seqs, u, [&](int i) { return (int64_t)kv_first(a.b, i); });
+        seq = a.b.cu ? kv_last_at_most(a.b.seqs, u, [&](int i) { return (int64_t)kv_first(a.b, i); }) : (int)u;
     } else {
         seq = kv_last_at_most(a.b.seqs, u, [&](int i) { return kv_tile(a.b, 1, 4, i); });
         first = kv_first(a.b, seq) + (u - kv_tile(a.b, 1, 4, seq)) * 4;
     }
-    const KvSeq s = kv_seq(a.b, seq);
+    seq = uniform(seq);
+    KvSeq s = kv_seq(a.b, seq);
+    s = KvSeq{uniform(s.first), uniform(s.n), uniform(s.len)};
     if (first < s.first || first >= (int64_t)s.first + s.n) return;
     const int tokens = (int)((int64_t)s.first + s.n - first < slots ? s.first + s.n - first : slots);
     // blocks up to a token's own
@@ -592,9 +605,9 @@ kv_select_kernel(KvSelectArgs a, int B, int slots, int64_t wg0)
             const int slot = slots == 1 ? 0 : col % 4, g = g0 + (slots == 1 ? col : col / 4);
             const int64_t token = first + (slot < tokens ? slot : tokens - 1);
             const float *qs = a.q + token * a.q_token + ((int64_t)head * a.group + (g < a.group ? g : a.group - 1)) * a.q_head + kk * (D / 4);
-            double q[D / 4];
+            float q[D / 4];
 #pragma unroll
-            for (int i = 0; i < D / 4; ++i) q[i] = (double)qs[i];
+            for (int i = 0; i < D / 4; ++i) q[i] = qs[i];
             auto page_of = [&](int b0) { return b0 + col < hi ? kv_page(a.b, seq, b0 + col) : -1; };
             auto mean_of = [&](int page, f32x4 *m) {
                 const f32x4 *src = reinterpret_cast<const f32x4 *>(a.c.mean + ((int64_t)page * a.c.heads + head) * D + kk * (D / 4));
@@ -614,7 +627,8 @@ kv_select_kernel(KvSelectArgs a, int B, int slots, int64_t wg0)
                 f64x4 sum = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll
                 for (int i = 0; i < D / 4; ++i)
-                    sum = __builtin_amdgcn_mfma_f64_16x16x4f64(q[i], (double)m[i / 4][i % 4], sum, 0, 0, 0);
+                    // (q is converted here: as FP64 it would take the registers of a second wave)
+                    sum = __builtin_amdgcn_mfma_f64_16x16x4f64((double)hidden(q[i]), (double)m[i / 4][i % 4], sum, 0, 0, 0);
                 uint64_t best = kLowest;
                 if (page >= 0) {
 #pragma unroll
@@ -644,13 +658,20 @@ kv_select_kernel(KvSelectArgs a, int B, int slots, int64_t wg0)
     }
     __syncthreads();
     if (wave >= tokens) return;
-    const int nb = blocks_of(wave);
+    const int nb = uniform(blocks_of(wave));
     int32_t *sel = a.sel + ((first + wave) * a.c.heads + head) * a.n_sel;
     if (nb <= a.n_sel) {   // all of them
         for (int i = lane; i < a.n_sel; i += 64) sel[i] = i < nb ? i : -1;
         return;
     }
-    pick_blocks(key + (int64_t)wave * a.b.cols, lo, nb - a.keep_last - lo, nb, r, sel);
+    const int n = nb - a.keep_last - lo;
+    key += (int64_t)wave * a.b.cols;
+    if (n <= 128)
+        pick_blocks<2>(key, lo, n, nb, r, sel);
+    else if (n <= 512)
+        pick_blocks<8>(key, lo, n, nb, r, sel);
+    else
+        pick_blocks<0>(key, lo, n, nb, r, sel);
 }
 
 template <int D, int B>
@@ -668,6 +689,23 @@ hipError_t read_sized(const KvSeqs &b, const KvCache &c, float *k, float *v, hip
     const int64_t n = kv_units(b.cu != nullptr, b.tokens, b.seqs, B) * 2 * c.heads;
     return in_parts(n, [&](int64_t at, unsigned m) {
         hipLaunchKernelGGL((kv_read_kernel<D, B>), dim3(m), dim3(kThreads), 0, stream, b, c, k, v, at);
+    });
+}
+
+template <int SLOTS>
+hipError_t select_slots(const KvSelectArgs &a, int64_t n, size_t lds, hipStream_t stream)
+{
+    auto kernel = a.c.dim == 64   ? kv_select_kernel<64, SLOTS>
+                  : a.c.dim == 96 ? kv_select_kernel<96, SLOTS>
+                                  : kv_select_kernel<128, SLOTS>;
+    if (lds > 32768) {   // beyond what a kernel may ask for by itself
+        const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                                   hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                   (int)(kMaxSelectBlocks * sizeof(uint64_t)));
+        if (err != hipSuccess) return err;
+    }
+    return in_parts(n, [&](int64_t at, unsigned m) {
+        hipLaunchKernelGGL(kernel, dim3(m), dim3(SLOTS == 1 ? 512 : 256), lds, stream, a, a.c.block, at);
     });
 }
 
@@ -689,23 +727,7 @@ hipError_t launch_kv_select(const KvSelectArgs &a, hipStream_t stream)
     const int slots = a.b.cu && a.b.cols * 4 <= kMaxSelectBlocks ? 4 : 1;
     const int64_t n = (slots == 4 ? kv_tiles(a.b.tokens, a.b.seqs, 1, 4) : a.b.tokens) * a.c.heads;
     const size_t lds = (size_t)a.b.cols * slots * sizeof(uint64_t);
-    if (lds > 32768) {   // beyond what a kernel may ask for by itself
-        const void *f = a.c.dim == 64   ? reinterpret_cast<const void *>(kv_select_kernel<64>)
-                        : a.c.dim == 96 ? reinterpret_cast<const void *>(kv_select_kernel<96>)
-                                        : reinterpret_cast<const void *>(kv_select_kernel<128>);
-        const hipError_t err = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                   (int)(kMaxSelectBlocks * sizeof(uint64_t)));
-        if (err != hipSuccess) return err;
-    }
-    return in_parts(n, [&](int64_t at, unsigned m) {
-        const dim3 grid(m), block(kSelectThreads);
-        if (a.c.dim == 64)
-            hipLaunchKernelGGL(kv_select_kernel<64>, grid, block, lds, stream, a, a.c.block, slots, at);
-        else if (a.c.dim == 96)
-            hipLaunchKernelGGL(kv_select_kernel<96>, grid, block, lds, stream, a, a.c.block, slots, at);
-        else
-            hipLaunchKernelGGL(kv_select_kernel<128>, grid, block, lds, stream, a, a.c.block, slots, at);
-    });
+    return slots == 4 ? select_slots<4>(a, n, lds, stream) : select_slots<1>(a, n, lds, stream);
 }
 
 }  // namespace heal
