@@ -23,6 +23,11 @@ namespace heal {
 
 namespace {
 
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+
+// Lambdas that are inlined at once: what they take by reference stays in registers.
+#define HEAL_INLINE __attribute__((always_inline))
+
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // Two workgroups of either kernel fit on a compute unit.  Parts are cut until there are
 // as many (a decode step of 64 sequences 157 us; 162 with 768 or 1024, 188 with 2048; 48
@@ -260,10 +265,25 @@ __device__ __forceinline__ float from_lane(float x, int lane)
 template <int B>
 struct Tile {
     static constexpr int NB = Blocks<B>::EPT, GS = 4 / NB;
-    int blk[NB], page[NB];
-    float k[NB], v[NB];
+    // (vectors, of which NB elements are used: arrays would end up in memory)
+    i32x4 blk, page;
+    f32x4 k, v;
     int off;      // of its first token within the block (B > 64)
     bool coded;   // no group is read from the ring
+
+    // member by member: a copy of the whole struct takes its padding along, in memory
+    Tile() = default;
+    __device__ __forceinline__ Tile(const Tile &t) { *this = t; }
+    __device__ __forceinline__ Tile &operator=(const Tile &t)
+    {
+        blk = t.blk;
+        page = t.page;
+        k = t.k;
+        v = t.v;
+        off = t.off;
+        coded = t.coded;
+        return *this;
+    }
 
     __device__ __forceinline__ void take(const Blocks<B> &b, int at, int64_t kt)
     {
@@ -278,19 +298,11 @@ struct Tile {
             coded = coded && page[i] >= 0;
         }
     }
-    __device__ __forceinline__ int blk_of(int s) const { return pick(blk, s); }
-    __device__ __forceinline__ int page_of(int s) const { return pick(page, s); }
-    __device__ __forceinline__ float key_of(int s) const { return pick(k, s); }
-    __device__ __forceinline__ float value_of(int s) const { return pick(v, s); }
     // of the block of group s, which need not be a constant
-    template <class X>
-    static __device__ __forceinline__ X pick(const X *x, int s)
-    {
-        X y = x[0];
-#pragma unroll
-        for (int i = 1; i < NB; ++i) y = s / GS == i ? x[i] : y;
-        return y;
-    }
+    __device__ __forceinline__ int blk_of(int s) const { return blk[NB == 1 ? 0 : s / GS]; }
+    __device__ __forceinline__ int page_of(int s) const { return page[NB == 1 ? 0 : s / GS]; }
+    __device__ __forceinline__ float key_of(int s) const { return k[NB == 1 ? 0 : s / GS]; }
+    __device__ __forceinline__ float value_of(int s) const { return v[NB == 1 ? 0 : s / GS]; }
     // the factor of the scores with block i (of group s), but for the query's
     __device__ __forceinline__ float key_factor(int i) const { return factor(blk[i], page[i], k[i]); }
     __device__ __forceinline__ float key_factor_of(int s) const { return factor(blk_of(s), page_of(s), key_of(s)); }
@@ -749,7 +761,7 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
     // Tiles with FP32 rows, a group of 16 tokens to each wave: all that a wave needs of
     // one is asked for at once, where one wave with the whole tile would have four times
     // the bytes of a coded tile to wait for (8191 tokens of one sequence: 17.7 us, 12.5 so).
-    auto ring_tile = [&](int64_t kt) {
+    auto ring_tile = [&](int64_t kt) HEAL_INLINE {
         Blocks<B> blocks;
         T tile;
         blocks.load(a, t.s, t.seq, slot, head, list, kt, to, 1);
@@ -902,13 +914,13 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
     if (from < to && span.last >= span.first) {
         // staging: wave w takes the keys of group w and the values of column tiles w, w + 4
         uint32_t ks[D / 16], vs[NW][4];
-        auto ask = [&](const T &x) {
+        auto ask = [&](const T &x) HEAL_INLINE {
             load_group_keys<D, B, false>(a, x, wave, head, r, g, ks);
 #pragma unroll
             for (int j = 0; j < NW; ++j)
                 if (N % 4 == 0 || wave + 4 * j < N) load_column_values<D, B, false>(a, x, wave + 4 * j, head, r, g, vs[j]);
         };
-        auto keep = [&](int b) {
+        auto keep = [&](int b) HEAL_INLINE {
 #pragma unroll
             for (int k = 0; k < KC; ++k) frag[b][wave * KC + k][lane] = codes8(ks[2 * k], ks[2 * k + 1]);
 #pragma unroll
@@ -920,7 +932,7 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
                 }
         };
         // a tile with FP32 rows (or without some of its blocks): both parts of the pairs
-        auto keep_pairs = [&](const T &x, int b) {
+        auto keep_pairs = [&](const T &x, int b) HEAL_INLINE {
             const int r2 = hidden(r), g2 = hidden(g);
             keys_of_group<D, B>(a, x, wave, slot, head, t.s.len, r2, g2, [&](int k, f16x8 h, f16x8 l) {
                 frag[b][wave * KC + k][lane] = h;
@@ -944,7 +956,7 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
         T cur;
         int buf = 0, at = 0;
         // the tile in LDS; residuals: with FP32 rows, whose residuals the other buffer has
-        auto compute = [&](auto residuals) {
+        auto compute = [&](auto residuals) HEAL_INLINE {
             constexpr bool X = decltype(residuals)::value;
             // fragments are read from LDS three steps (of four matrix instructions) ahead
             const f16x8(*hi)[64] = frag[buf], (*res)[64] = frag[buf ^ 1];
@@ -1010,7 +1022,7 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
             }
         };
         // (a wave whose rows see nothing of a tile only helps to stage it)
-        auto sees = [&](int64_t kt) { return kt * 64 <= wspan.last && kt * 64 + 63 >= wspan.first; };
+        auto sees = [&](int64_t kt) HEAL_INLINE { return kt * 64 <= wspan.last && kt * 64 + 63 >= wspan.first; };
         if (from < coded_to) {
             blocks.load(a, t.s, t.seq, slot, head, nullptr, from, coded_to, 1);
             cur.take(blocks, 0, from);
