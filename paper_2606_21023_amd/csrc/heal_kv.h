@@ -187,6 +187,7 @@ struct KvPlan {
     bool by_token;               // a row tile holds one token's queries
     bool wide;                   // 128-row tiles
     int64_t tiles;               // row tiles of the grid
+    int64_t wgs;                 // workgroups for each part, about
     int32_t parts, part_tiles;
     int64_t bytes;               // of workspace
 };

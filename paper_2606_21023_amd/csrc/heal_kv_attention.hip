@@ -33,8 +33,8 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // as many (a decode step of 64 sequences 157 us; 162 with 768 or 1024, 188 with 2048; 48
 // of 512 blocks of 32 sequences 54, 67, 70 and 85).
 constexpr int64_t kWantedWorkgroups = 512;
-// Rows of a sequence, on average, from which 128-row tiles are taken.
-constexpr int64_t kWideRows = 64;
+// Up to so many sequences the tiles of a ragged call are counted one after another.
+constexpr int64_t kCountedSeqs = 256;
 constexpr int kNoScale = -100000;   // no value block with a scale seen yet
 
 __device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c)
@@ -142,9 +142,42 @@ __device__ __forceinline__ bool find_rows(const KvAttnArgs &a, bool by_token, in
         t.rows = a.group - t.row0 < R ? a.group - t.row0 : R;
         t.row0 += (int)(token - t.s.first) * a.group;
     } else {
-        t.seq = uniform(kv_last_at_most(a.b.seqs, u, [&](int i) { return kv_tile(a.b, a.group, R, i); }));
-        t.s = uniform_seq(a.b, t.seq);
-        const int64_t j = u - kv_tile(a.b, a.group, R, t.seq);
+        int64_t j;
+        if (a.b.seqs <= kCountedSeqs) {
+            // The tiles of each sequence are counted, so that those of the grid that are nobody's
+            // come last.  Where they lie between the others, they can take every second
+            // place in the order in which workgroups are dealt out, and half of the compute
+            // units get nothing else (32 sequences of 128 rows over 2048 tokens: 155 us, 99 so).
+            const int lane = threadIdx.x & 63;
+            int64_t before = 0;
+            t.seq = -1;
+            for (int i0 = 0; i0 < a.b.seqs; i0 += 64) {
+                const int first = i0 + lane < a.b.seqs ? kv_first(a.b, i0 + lane) : 0;
+                const int next = i0 + lane < a.b.seqs ? kv_first(a.b, i0 + lane + 1) : 0;
+                const int64_t own = next > first ? ((int64_t)(next - first) * a.group + R - 1) / R : 0;
+                int64_t sum = own;
+#pragma unroll
+                for (int off = 1; off < 64; off <<= 1) {
+                    const int64_t x = __shfl_up(sum, off);
+                    sum += lane >= off ? x : 0;
+                }
+                const uint64_t past = __ballot(before + sum > u);
+                if (past) {
+                    const int at = __builtin_ctzll(past);
+                    t.seq = uniform(i0 + at);
+                    j = u - before - (__shfl(sum, at) - __shfl(own, at));
+                    break;
+                }
+                before += __shfl(sum, 63);
+            }
+            if (t.seq < 0) return false;
+            t.s = uniform_seq(a.b, t.seq);
+        } else {
+            t.seq = uniform(kv_last_at_most(a.b.seqs, u, [&](int i) { return kv_tile(a.b, a.group, R, i); }));
+            t.s = uniform_seq(a.b, t.seq);
+            j = u - kv_tile(a.b, a.group, R, t.seq);
+        }
+        j = (int64_t)uniform((int)j);
         const int64_t n = (int64_t)t.s.n * a.group;
         if (j < 0 || j * R >= n) return false;
         t.row0 = (int)(j * R);
@@ -1151,15 +1184,18 @@ hipError_t attention_sized(KvAttnArgs &a, const KvPlan &plan, hipStream_t stream
 
 }  // namespace
 
-KvPlan kv_plan(int64_t tokens, int64_t seqs, bool ragged, int heads, int group, int dim, int block,
-               int64_t cols, int64_t window, int64_t n_sel, int64_t chunk)
+namespace {
+
+// Row tiles of a plan's kernel and the parts that each of them is cut into.
+void cut(KvPlan &p, int64_t tokens, int64_t seqs, int heads, int group, int block, int64_t cols, int64_t window,
+         int64_t n_sel, int64_t chunk)
 {
-    KvPlan p = {};
-    p.by_token = n_sel > 0 || !ragged;
-    // (a chunk of the caller's asks for sums that do not depend on the call's sizes)
-    p.wide = !p.by_token && chunk == 0 && tokens * group >= kWideRows * seqs;
     const int R = p.wide ? 128 : 16;
     p.tiles = p.by_token ? tokens * ((group + 15) / 16) : kv_tiles(tokens, seqs, group, R);
+    // workgroups, if the sequences have equally many rows
+    const int64_t each = seqs > 0 ? (tokens * group + seqs * R - 1) / (seqs * R) : 0;
+    const int64_t real = p.by_token || seqs * each > p.tiles ? p.tiles : seqs * each;
+    p.wgs = real * heads > 0 ? real * heads : 1;
     // 64-token tiles that a row tile can have to read (its rows' windows begin at up to R places)
     int64_t places = n_sel > 0 ? n_sel * block : cols * block;
     if (n_sel == 0 && window > 0 && window + R + 63 < places) places = window + R + 63;
@@ -1168,11 +1204,9 @@ KvPlan kv_plan(int64_t tokens, int64_t seqs, bool ragged, int heads, int group, 
     if (chunk > 0) {
         part_tiles = chunk / 64;
     } else {
-        // enough workgroups to fill the chip, each with a tile for every wave at least; of the
-        // prompts' kernel two to a compute unit, which take equal parts (the bound on their
-        // row tiles counts one too many for each sequence)
-        const int64_t wgs = (p.wide ? p.tiles - seqs : p.tiles) * heads;
-        const int64_t wanted = wgs <= 0 ? 1 : p.wide ? kWantedWorkgroups / wgs : (kWantedWorkgroups + wgs - 1) / wgs;
+        // enough workgroups to fill the chip (of the prompts' kernel, whose workgroups take
+        // equally long, no more than that), each with a tile for every wave at least
+        const int64_t wanted = p.wide ? kWantedWorkgroups / p.wgs : (kWantedWorkgroups + p.wgs - 1) / p.wgs;
         int64_t parts = wanted < (span + 3) / 4 ? wanted : (span + 3) / 4;
         parts = parts < 1 ? 1 : parts > 64 ? 64 : parts;
         part_tiles = ((span + parts - 1) / parts + 3) / 4 * 4;
@@ -1180,6 +1214,40 @@ KvPlan kv_plan(int64_t tokens, int64_t seqs, bool ragged, int heads, int group, 
     if (part_tiles > span) part_tiles = span;
     p.part_tiles = (int32_t)part_tiles;
     p.parts = (int32_t)((span + part_tiles - 1) / part_tiles);
+}
+
+// About how many us a plan takes: rounds of 512 workgroups, each with a fixed cost and a
+// cost for each of its tiles (of the kernel for few rows: for each four), and what
+// the parts' results cost.  Fitted to calls of 16 to 2048 rows of 1 to 32
+// sequences over up to 8192 tokens, measured with both kernels: of 77 of them the
+// faster one is found for 73, and the other four lose 11 to 29% (2048 rows of 32
+// sequences over 2048 tokens: 927 us with 128-row tiles, 1807 with 16-row ones; 64 rows
+// 83 and 72).
+double estimate(const KvPlan &p, int64_t tokens, int heads, int group, int dim)
+{
+    const double rounds = (double)p.wgs * p.parts / (double)kWantedWorkgroups, d = dim / 128.0;
+    const double one = p.wide ? 9.0 + p.part_tiles * (1.4 + 1.9 * d) : 6.0 + (p.part_tiles + 3) / 4 * (0.2 + 2.5 * d);
+    const double join = p.parts > 1 ? 3.0 + (double)tokens * heads * group * p.parts * (dim + 2) * 2e-6 : 0.0;
+    return (rounds > 1.0 ? rounds : 1.0) * one + join;
+}
+
+}  // namespace
+
+KvPlan kv_plan(int64_t tokens, int64_t seqs, bool ragged, int heads, int group, int dim, int block,
+               int64_t cols, int64_t window, int64_t n_sel, int64_t chunk)
+{
+    KvPlan p = {};
+    p.by_token = n_sel > 0 || !ragged;
+    // (a chunk of the caller's asks for sums that do not depend on the call's sizes)
+    const bool either = !p.by_token && chunk == 0 && seqs > 0 && tokens > 0;
+    p.wide = false;
+    cut(p, tokens, seqs, heads, group, block, cols, window, n_sel, chunk);
+    if (either) {
+        KvPlan w = p;
+        w.wide = true;
+        cut(w, tokens, seqs, heads, group, block, cols, window, n_sel, chunk);
+        if (estimate(w, tokens, heads, group, dim) < estimate(p, tokens, heads, group, dim)) p = w;
+    }
     const double rows = (double)tokens * heads * group;
     p.bytes = p.parts == 1 ? 0 : rows * p.parts > 0x1p44 ? -1 : tokens * heads * group * p.parts * (dim + 2) * 4;
     return p;
