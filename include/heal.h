@@ -447,6 +447,7 @@ heal_status_t heal_kv_select(const heal_kv_cache_t *cache, const heal_kv_batch_t
  *   sel  : NULL, or [tokens][heads][n_sel] int32, dense: only these blocks of the
  *          sequence are read for a token and head (a block listed twice counts
  *          twice; numbers outside the table hold nothing);
+ *   tokens * heads_q / heads < 2^31;
  *   out  : [tokens][heads_q][dim], written; must not overlap q;
  *   lse  : [tokens][heads_q] dense, or NULL;
  *   chunk: 0, or a multiple of 64: each row's tokens are summed in chunks of so many
@@ -472,6 +473,12 @@ heal_status_t heal_kv_attention(const heal_kv_cache_t *cache, const heal_kv_batc
  * (no HIP call). */
 int64_t heal_kv_attention_workspace(const heal_kv_cache_t *cache, const heal_kv_batch_t *batch,
                                     int64_t heads_q, int64_t window, int64_t n_sel, int64_t chunk);
+
+/* The rows (token, query of a head) of a tile that the call's kernel takes: 16, each
+ * tile read by four waves side by side, or 128 for prompts; 0 where the call would be
+ * refused (no HIP call).  For the labels of measurements. */
+int heal_kv_attention_tile(const heal_kv_cache_t *cache, const heal_kv_batch_t *batch,
+                           int64_t heads_q, int64_t window, int64_t n_sel, int64_t chunk);
 
 #ifdef __cplusplus
 }

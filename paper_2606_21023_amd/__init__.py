@@ -128,6 +128,8 @@ def lib():
     L.heal_kv_attention.restype = _c
     L.heal_kv_attention_workspace.argtypes = [_vp, _vp, _i64, _i64, _i64, _i64]
     L.heal_kv_attention_workspace.restype = _i64
+    L.heal_kv_attention_tile.argtypes = L.heal_kv_attention_workspace.argtypes
+    L.heal_kv_attention_tile.restype = _c
     _lib = L
     return L
 

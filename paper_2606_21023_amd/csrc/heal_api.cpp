@@ -249,6 +249,7 @@ bool kv_attention_sizes(const heal_kv_cache_t *c, const heal_kv_batch_t *b, int6
     if (window < 0 || window > lim || n_sel < 0 || n_sel * c->block > lim || chunk < 0 || chunk % 64 != 0 ||
         chunk > lim)
         return false;
+    if (b->tokens * (heads_q / c->heads) > lim - 128) return false;   // rows are counted in 32 bits
     *plan = heal::kv_plan(b->tokens, b->seqs, b->cu != nullptr, (int)c->heads, (int)(heads_q / c->heads),
                           (int)c->dim, (int)c->block, b->table_cols, window, n_sel, chunk);
     return plan->bytes >= 0;
@@ -618,6 +619,14 @@ int64_t heal_kv_attention_workspace(const heal_kv_cache_t *cache, const heal_kv_
 {
     heal::KvPlan plan;
     return kv_attention_sizes(cache, batch, heads_q, window, n_sel, chunk, &plan) ? plan.bytes : -1;
+}
+
+int heal_kv_attention_tile(const heal_kv_cache_t *cache, const heal_kv_batch_t *batch, int64_t heads_q,
+                           int64_t window, int64_t n_sel, int64_t chunk)
+{
+    heal::KvPlan plan;
+    if (!kv_attention_sizes(cache, batch, heads_q, window, n_sel, chunk, &plan)) return 0;
+    return plan.wide ? 128 : 16;
 }
 
 heal_status_t heal_kv_attention(const heal_kv_cache_t *cache, const heal_kv_batch_t *batch, const float *q,

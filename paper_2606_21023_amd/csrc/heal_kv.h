@@ -100,6 +100,12 @@ HEAL_HD KvTouched kv_touched(const KvSeq &s, int B)
     return t;
 }
 
+// The first 64-token tile of a sequence that has a block which is not complete, and the
+// tile behind its last one (blocks of 128 tokens are two tiles, of which the second
+// may have rows too); both behind every tile where the last block is complete.
+HEAL_HD int64_t kv_ring_first(int32_t len, int B) { return len % B ? (int64_t)(len / B) * B / 64 : (int64_t)1 << 40; }
+HEAL_HD int64_t kv_ring_end(int32_t len, int B) { return len % B ? ((int64_t)len - 1) / 64 + 1 : (int64_t)1 << 40; }
+
 // Unit j of a sequence handles block first + j when it appends, except that the
 // ring rows of a later block, which take the place of rows that unit 0 still has
 // to read, are unit 0's too: the block of {last - 1, last} that lies an even

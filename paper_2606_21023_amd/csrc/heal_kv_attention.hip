@@ -830,12 +830,11 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
         }
     };
     if (t.s.len % B != 0 && span.last >= span.first) {
-        const int32_t rb = t.s.len / B;   // the block that is not complete
         if (!a.sel) {
-            const int64_t kt = (int64_t)rb * B / 64 + (B > 64 ? t.s.len % B / 64 : 0);
-            for (int64_t x = (int64_t)rb * B / 64; x <= kt; ++x)
+            for (int64_t x = kv_ring_first(t.s.len, B); x < kv_ring_end(t.s.len, B); ++x)
                 if (x >= from && x < to) ring_tile(x);
         } else {
+            const int32_t rb = t.s.len / B;   // the block that is not complete
             // wherever the lists have it, 64 entries at a time
             constexpr int E = B < 64 ? 64 / B : 1, P = B > 64 ? B / 64 : 1;   // entries of a tile, tiles of an entry
             for (int64_t e0 = from * E / P; e0 * P < to * E; e0 += 64) {
@@ -982,9 +981,8 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
                 }
         };
 
-        // the ring's block can only be in a sequence's last tile, which comes after the loop
-        const bool ring = t.s.len % B != 0 && t.s.len / B * B / 64 == to - 1;
-        const int64_t coded_to = ring ? to - 1 : to;
+        // the tiles of the ring's block, the last ones, come after the loop
+        const int64_t ring = kv_ring_first(t.s.len, B), coded_to = ring < to ? (ring > from ? ring : from) : to;
         Blocks<B> blocks;
         T cur;
         int buf = 0, at = 0;
@@ -1082,14 +1080,15 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
                 cur = next;
             }
         }
-        if (ring) {
+#pragma unroll 1
+        for (int64_t kt = coded_to; kt < to; ++kt) {
             __syncthreads();   // both buffers are written
-            blocks.load(a, t.s, t.seq, slot, head, nullptr, to - 1, to, 1);
-            cur.take(blocks, 0, to - 1);
+            blocks.load(a, t.s, t.seq, slot, head, nullptr, kt, to, 1);
+            cur.take(blocks, 0, kt);
             buf = 0;
             keep_pairs(cur, 0);
             __syncthreads();
-            if (sees(to - 1)) compute(std::true_type());
+            if (sees(kt)) compute(std::true_type());
         }
     }
 

@@ -52,6 +52,19 @@ int main()
         }
         for (int c : seen) CHECK(c == 1);
     }
+    // every tile before the first one of the ring has complete blocks only, every row of an
+    // incomplete block lies in a tile from that one to the end
+    for (int B : {16, 32, 64, 128})
+        for (int len = 0; len < 1000; ++len) {
+            const int64_t first = kv_ring_first(len, B), end = kv_ring_end(len, B);
+            for (int64_t kt = 0; kt * 64 < len; ++kt) {
+                bool ring = false;
+                for (int64_t p = kt * 64; p < kt * 64 + 64 && p < len; ++p) ring |= (p / B + 1) * B > len;
+                CHECK(ring == (kt >= first));
+                CHECK(kt < end);
+            }
+            CHECK(len % B == 0 || (end - 1) * 64 < len);
+        }
     const int blocks[] = {16, 32, 64, 128}, groups[] = {1, 2, 3, 4, 7, 16, 17, 64};
     for (round = 0; round < 3000; ++round) {
         const int B = blocks[rnd(4)], G = groups[rnd(8)], R = rnd(2) ? 16 : 128, seqs = 1 + rnd(9);

@@ -539,6 +539,152 @@ def test_offsets_past_32_bits():
     assert (sel[0] == [0, 1]).all() and (sel[1] == [0, 2]).all()
 
 
+# ---- prompts: 128-row tiles ------------------------------------------------------
+
+
+def _check_prompts(w, counts, group, causal=True, window=0, tile=128, hidden=(), strided=False):
+    """As _check_attention for many rows at a time, of a call that takes 128-row tiles."""
+    import ctypes
+    T, heads_q = sum(counts), w.heads * group
+    cu = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    kw = w.kw()
+    batch = heal._CBatch(w.seqs, T, 1, 1, 1, w.cols, w.cols, 1)
+    assert heal.lib().heal_kv_attention_tile(w.cache._ref, ctypes.byref(batch), heads_q, window, 0, 0) == tile
+    q = w.rows(T, heads_q)
+    g = dev(q)
+    out = torch.full((T, heads_q, w.dim), 7.0, device="cuda")
+    if strided:   # heads outermost, rows that are not 16-byte aligned
+        g = torch.nn.functional.pad(g.transpose(0, 1), (0, 1)).contiguous()[..., :-1].transpose(0, 1)
+        out = torch.full((heads_q, T, w.dim + 1), 7.0, device="cuda")[..., :-1].transpose(0, 1)
+    lse = torch.full((T, heads_q), 7.0, device="cuda")
+    announce("prompts %s of %s, %s causal %s window %d" % (counts, w.lens(), q.shape, causal, window))
+    heal.heal_kv_attention(w.cache, g, cu=dev(cu), **kw, causal=causal, window=window, out=out, lse=lse)
+    torch.cuda.synchronize()
+    out, lse = out.cpu().numpy().astype(np.float64), lse.cpu().numpy().astype(np.float64)
+    assert np.array_equal(g.cpu().numpy(), q)
+    scale = w.dim ** -0.5
+    for i, r in enumerate(w.ref):
+        n, t = len(r.k), counts[i]
+        if not t:
+            continue
+        rows = slice(cu[i], cu[i + 1])
+        place, at = np.arange(n - t, n)[:, None], np.arange(n)
+        seen = (at <= place) if causal else np.repeat(place >= 0, n, 1)
+        if window:
+            seen = seen & (at > place - window)
+        for i2, b in hidden:
+            if i2 == i:
+                seen = seen & (at // w.block != b)
+        for h in range(heads_q):
+            K, V = r.values("k")[:, h // group], r.values("v")[:, h // group]
+            x = q[rows, h].astype(np.float64)
+            s = np.where(seen, scale * (x @ K.T), -np.inf)
+            m = s.max(1, initial=-np.inf)
+            e = np.where(seen, np.exp(s - np.where(np.isinf(m), 0.0, m)[:, None]), 0.0)
+            l = e.sum(1)
+            p = e / np.where(l == 0, 1.0, l)[:, None]
+            S = scale * np.where(seen, np.abs(x) @ np.abs(K).T, 0.0).max(1, initial=0.0)
+            top = np.abs(K).max(initial=0.0)
+            rel, floor, off = kv_ref.bound(S, np.maximum(1, seen.sum(1)), w.dim,
+                                           scale * np.abs(x).max(1) * np.abs(K).sum(1).max(initial=0.0),
+                                           scale * np.abs(x).sum(1) * top, np.abs(V).max(initial=0.0) * 1.01)
+            assert np.all(np.abs(out[rows, h] - p @ V) <= rel[:, None] * (p @ np.abs(V)) + floor[:, None]), (i, h)
+            empty = l == 0
+            assert np.all(np.isneginf(lse[rows, h][empty])) and not out[rows, h][empty].any()
+            want = m[~empty] + np.log(l[~empty])
+            assert np.all(np.abs(lse[rows, h][~empty] - want) <= off[~empty] + 2.0 ** -23 * np.abs(want)), (i, h)
+
+
+@pytest.mark.parametrize("block", [16, 32, 64, 128])
+@pytest.mark.parametrize("dim", [64, 96, 128])
+def test_prompts(dim, block):
+    """Ragged prompts and continued ones, of any length modulo the tiles, none among them."""
+    heads, group = (8, 4) if dim != 96 else (5, 7)
+    w = World(20, heads=heads, dim=dim, block=block, cols=-(-260 // block), seed=dim * block)
+    first = [(i * 37) % 140 for i in range(20)]
+    w.append(first)
+    counts = [64 + (i * 29) % 50 for i in range(20)]
+    counts[3] = 0
+    w.append(counts)
+    _check_prompts(w, counts, group)
+    _check_prompts(w, counts, group, strided=True)
+
+
+@pytest.mark.parametrize("window", [1, 30, 64, 100])
+def test_prompts_with_windows(window):
+    w = World(24, heads=8, dim=64, block=32, cols=8, seed=window)
+    counts = [150 + i for i in range(24)]
+    w.append(counts)
+    _check_prompts(w, counts, 2, window=window)
+
+
+def test_prompts_not_causal_and_beyond_their_length():
+    w = World(20, heads=8, dim=64, block=16, cols=14)
+    w.append([(i * 23) % 200 for i in range(20)])
+    counts = [150] * 20    # longer than some of the sequences: those rows see nothing
+    _check_prompts(w, counts, 4, causal=False)
+    _check_prompts(w, counts, 4)
+
+
+def test_prompts_with_pages_that_are_not_there():
+    w = World(16, heads=8, dim=128, block=32, cols=8)
+    counts = [130 + 5 * i for i in range(16)]
+    w.append(counts)
+    hidden = [(0, 0), (1, 1), (1, 2), (2, 4), (3, 3)]
+    for i, b in hidden:
+        w.table[i, b] = -1 if b % 2 else w.cache.blocks + 7
+    hidden.append((5, len(w.ref[5].k) // 32))
+    w.slots[5] = -3        # its incomplete block
+    w.cache.k_codes[[p for p in range(w.cache.blocks) if p not in set(w.table.ravel().tolist())]] = -128
+    _check_prompts(w, counts, 4, hidden=hidden)
+
+
+def test_a_chunk_of_a_long_prompt():
+    """Few row tiles, so that each is cut into parts."""
+    w = World(1, heads=4, dim=128, block=64, cols=100, places=7000)
+    w.append([6123])
+    _check_prompts(w, [300], 4)
+    _check_prompts(w, [297], 4, strided=True)
+
+
+@pytest.mark.parametrize("seqs", [256, 257, 700])
+def test_many_sequences(seqs):
+    """Row tiles found by counting, and (past 256 sequences) from bounds."""
+    w = World(seqs, heads=1, dim=64, block=16, cols=9, seed=seqs)
+    w.append([1 + (i * 13) % 140 for i in range(seqs)])
+    counts = [(i * 7) % 6 for i in range(seqs)]
+    counts = [min(c, len(r.k)) for c, r in zip(counts, w.ref)]
+    _check_prompts(w, counts, 3, tile=16)
+    _check_prompts(w, [min(140, len(r.k)) for r in w.ref], 16, tile=128)
+
+
+def test_anything_behind_a_prompt():
+    """NaN and infinities in the ring behind the last row of a prompt."""
+    w = World(16, heads=8, dim=64, block=64, cols=3)
+    counts = [100 + i for i in range(16)]
+    w.append(counts)
+    for i, n in enumerate(counts):
+        w.cache.k_recent[int(w.slots[i]), :, n:] = NAN
+        w.cache.v_recent[int(w.slots[i]), :, :, n:] = float("inf")
+        w.table[i, 2] = -1
+    _check_prompts(w, counts, 4)
+
+
+def test_select_of_more_blocks_than_four_tokens_fit():
+    """Past 4096 columns each token is a workgroup's alone, in ragged calls too."""
+    w = World(2, heads=1, dim=64, block=16, cols=4100, places=1)
+    mean = torch.randn(w.cache.k_mean.shape, device="cuda")
+    w.cache.k_mean.copy_(mean)
+    lens, cu = [16 * 4099 + 3, 500], [0, 3, 5]
+    q = w.rows(5, 2)
+    announce("select of 4100 columns")
+    got = heal.heal_kv_select(w.cache, dev(q), 9, cu=ints(cu), **w.kw(lens)).cpu().numpy()
+    mean = mean.cpu().numpy().astype(np.float64)
+    for t, (i, j, n) in enumerate([(0, 0, 3), (0, 1, 3), (0, 2, 3), (1, 0, 2), (1, 1, 2)]):
+        want = kv_ref.select(q[t], mean[w.table[i], 0], lens[i] - n + j, 16, 9, 1, 1)
+        assert got[t, 0].tolist() == want, t
+
+
 # ---- which blocks -----------------------------------------------------------------
 
 

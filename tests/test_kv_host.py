@@ -134,6 +134,29 @@ def test_workspace():
     assert size(tokens=1 << 30, heads_q=2048, chunk=64, table_cols=1 << 24, table_ld=1 << 24) == -1
 
 
+def test_which_kernel_takes_a_call():
+    """16-row tiles for single tokens, drafts and short prompts; 128-row tiles for long ones,
+    or many (us on one MI355X with 16-row and 128-row tiles)."""
+    f = heal.lib().heal_kv_attention_tile
+
+    def tile(seqs, tokens, length, heads=8, group=4, dim=128, block=64, chunk=0, n_sel=0, window=0, cu=FAKE):
+        c = _cache(heads=heads, dim=dim, block=block)
+        b = _batch(seqs=seqs, tokens=seqs * tokens, cu=cu, table_cols=-(-length // block),
+                   table_ld=-(-length // block))
+        return f(ctypes.byref(c), ctypes.byref(b), heads * group, window, n_sel, chunk)
+    assert tile(64, 1, 8192) == 16 and tile(64, 1, 8192, cu=None) == 16
+    assert tile(8, 4, 4096) == 16 and tile(8, 16, 4096) == 16              # 24, 35; 44, 49
+    assert tile(8, 64, 4096) == 128 and tile(32, 512, 2048) == 128         # 117, 90; 1807, 927
+    assert tile(1, 256, 256) == 16 and tile(16, 256, 256) == 128           # 14, 22; 140, 60
+    assert tile(1, 512, 16001) == 128 and tile(2, 2048, 2048) == 128
+    # sums that do not depend on the call's sizes, and blocks of each token's own
+    assert tile(2, 2048, 2048, chunk=64) == 16 and tile(2, 2048, 2048, n_sel=4) == 16
+    # a window leaves little to read
+    assert tile(1, 512, 16001, window=64) == 16
+    assert tile(1, 1, 64, dim=65) == 0 and tile(1, 1, 64, group=0) == 0
+    assert tile(1, 1 << 30, 64, group=2) == 0
+
+
 class OnDevice(torch.Tensor):
     """A CPU tensor that the checks take for one on the device."""
     is_cuda = True
