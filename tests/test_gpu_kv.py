@@ -461,6 +461,41 @@ def test_tokens_of_no_sequence_are_left_alone():
             assert (x[:3] == y).all() and (x[16:] == y).all() and not (x[3:16] == y).any()
 
 
+def test_lengths_past_the_table():
+    """Places that the table has no block for hold nothing, without columns no place does."""
+    w = World(2, dim=64, block=16, cols=4)
+    w.append([50, 64])
+    q = w.rows(2, 4)
+    kw = w.kw([50, 64 + 37])      # the second length is 37 past the table: its query sees all 64
+    announce("lengths past the table")
+    out = heal.heal_kv_attention(w.cache, dev(q), **kw).cpu().numpy()
+    K, V = w.ref[1].values("k"), w.ref[1].values("v")
+    for h in range(4):
+        o, _, S, A = kv_ref.attention(q[1, h], K[:, h // 2], V[:, h // 2], 0.125, np.ones(64))
+        rel, floor, _ = kv_ref.bound(S, 64, 64, v=float(np.abs(V).max()) * 1.01)
+        assert np.all(np.abs(out[1, h] - o) <= rel * A + floor)
+    sel = heal.heal_kv_select(w.cache, dev(q), 4, **kw).cpu().numpy()
+    assert (sel == [0, 1, 2, 3]).all()
+    none = dict(kw, table=kw["table"][:, :0])
+    for x in (w.rows(2, 4), w.rows(80, 4)):
+        cu = ints([0, len(x) // 2, len(x)])
+        assert not heal.heal_kv_attention(w.cache, dev(x), **none, cu=cu).any()
+        assert (heal.heal_kv_select(w.cache, dev(x), 3, **none, cu=cu) == -1).all()
+        k, v = heal.heal_kv_read(w.cache, len(x), **none, cu=cu)
+        assert not k.any() and not v.any()
+
+
+def test_calls_without_tokens():
+    w = World(2, dim=64, block=16, cols=4)
+    w.append([5, 6])
+    kw, cu, q = dict(w.kw(), cu=ints([0, 0, 0])), ints([0, 0, 0]), torch.empty(0, 4, 64, device="cuda")
+    assert heal.heal_kv_append(w.cache, q[:, :2], q[:, :2], **kw, q=q).shape == (0, 4, 64)
+    assert heal.heal_kv_attention(w.cache, q, **kw).shape == (0, 4, 64)
+    assert heal.heal_kv_select(w.cache, q, 3, **kw).shape == (0, 2, 3)
+    assert heal.heal_kv_read(w.cache, 0, **kw)[0].shape == (0, 2, 64)
+    w.check()
+
+
 def test_strided_queries_and_outputs():
     w = World(2, heads=2, dim=96, block=32, cols=4)
     w.append([40, 77])
@@ -643,8 +678,11 @@ def test_a_chunk_of_a_long_prompt():
     """Few row tiles, so that each is cut into parts."""
     w = World(1, heads=4, dim=128, block=64, cols=100, places=7000)
     w.append([6123])
-    _check_prompts(w, [300], 4)
-    _check_prompts(w, [297], 4, strided=True)
+    _check_prompts(w, [300], 4, tile=16)
+    w = World(1, heads=8, dim=128, block=64, cols=100, places=7000)
+    w.append([6123])
+    _check_prompts(w, [500], 4)
+    _check_prompts(w, [497], 4, strided=True)
 
 
 @pytest.mark.parametrize("seqs", [256, 257, 700])
@@ -815,6 +853,24 @@ def test_a_decode_step_captured_and_replayed():
         for name in ("out", "out2", "q_out", "sel"):
             assert torch.equal(a[name], b[name]), (r, name)
         assert torch.equal(a["kw"]["lens"], b["kw"]["lens"])
+
+
+def test_a_long_selection_captured():
+    """More blocks than a kernel's LDS holds by default, in a graph."""
+    c = heal.KVCache.empty(9000, 1, 1, 64, 16)
+    c.k_mean.normal_()
+    table, lens = torch.arange(9000, dtype=torch.int32, device="cuda")[None], ints([9000 * 16])
+    q, out = torch.randn(1, 4, 64, device="cuda"), torch.empty(1, 1, 50, dtype=torch.int32, device="cuda")
+    announce("a long selection")
+    want = heal.heal_kv_select(c, q, 50, table, lens)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        heal.heal_kv_select(c, q, 50, table, lens, out=out)
+    for _ in range(3):
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
 
 
 def test_two_streams_at_once():
