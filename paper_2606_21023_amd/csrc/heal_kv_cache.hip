@@ -566,11 +566,11 @@ __device__ __forceinline__ void pick_blocks(const uint64_t *key, int lo, int n, 
 // it), so the maximum over a token's queries is taken within the lane; with one
 // token the 16 rows are its queries.  The order of the sum is the same for every block,
 // so equal blocks score equally.
-template <int D, int SLOTS>
-__global__ void __launch_bounds__(SLOTS == 1 ? 512 : 256, 4)
+template <int D, int SLOTS, int THREADS>
+__global__ void __launch_bounds__(THREADS, 4)
 kv_select_kernel(KvSelectArgs a, int B, int64_t wg0)
 {
-    constexpr int slots = SLOTS, kSelectThreads = SLOTS == 1 ? 512 : 256;
+    constexpr int slots = SLOTS;
     extern __shared__ char lds[];
     uint64_t *key = reinterpret_cast<uint64_t *>(lds);   // [slots][cols]
     const int wave = uniform((int)threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, kk = lane >> 4;
@@ -614,7 +614,7 @@ kv_select_kernel(KvSelectArgs a, int B, int64_t wg0)
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) m[i] = page >= 0 ? src[i] : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             };
-            constexpr int STEP = kSelectThreads / 64 * 16;
+            constexpr int STEP = THREADS / 64 * 16;
             int b0 = lo + wave * 16;
             int page = b0 < hi ? page_of(b0) : -1, next = b0 + STEP < hi ? page_of(b0 + STEP) : -1;
             f32x4 m[D / 16];
@@ -670,6 +670,8 @@ kv_select_kernel(KvSelectArgs a, int B, int64_t wg0)
         pick_blocks<2>(key, lo, n, nb, r, sel);
     else if (n <= 512)
         pick_blocks<8>(key, lo, n, nb, r, sel);
+    else if (n <= 2048)
+        pick_blocks<32>(key, lo, n, nb, r, sel);
     else
         pick_blocks<0>(key, lo, n, nb, r, sel);
 }
@@ -692,12 +694,12 @@ hipError_t read_sized(const KvSeqs &b, const KvCache &c, float *k, float *v, hip
     });
 }
 
-template <int SLOTS>
+template <int SLOTS, int THREADS>
 hipError_t select_slots(const KvSelectArgs &a, int64_t n, size_t lds, hipStream_t stream)
 {
-    auto kernel = a.c.dim == 64   ? kv_select_kernel<64, SLOTS>
-                  : a.c.dim == 96 ? kv_select_kernel<96, SLOTS>
-                                  : kv_select_kernel<128, SLOTS>;
+    auto kernel = a.c.dim == 64   ? kv_select_kernel<64, SLOTS, THREADS>
+                  : a.c.dim == 96 ? kv_select_kernel<96, SLOTS, THREADS>
+                                  : kv_select_kernel<128, SLOTS, THREADS>;
     if (lds > 32768) {   // beyond what a kernel may ask for by itself
         const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                                    hipFuncAttributeMaxDynamicSharedMemorySize,
@@ -705,7 +707,7 @@ hipError_t select_slots(const KvSelectArgs &a, int64_t n, size_t lds, hipStream_
         if (err != hipSuccess) return err;
     }
     return in_parts(n, [&](int64_t at, unsigned m) {
-        hipLaunchKernelGGL(kernel, dim3(m), dim3(SLOTS == 1 ? 512 : 256), lds, stream, a, a.c.block, at);
+        hipLaunchKernelGGL(kernel, dim3(m), dim3(THREADS), lds, stream, a, a.c.block, at);
     });
 }
 
@@ -727,7 +729,12 @@ hipError_t launch_kv_select(const KvSelectArgs &a, hipStream_t stream)
     const int slots = a.b.cu && a.b.cols * 4 <= kMaxSelectBlocks ? 4 : 1;
     const int64_t n = (slots == 4 ? kv_tiles(a.b.tokens, a.b.seqs, 1, 4) : a.b.tokens) * a.c.heads;
     const size_t lds = (size_t)a.b.cols * slots * sizeof(uint64_t);
-    return slots == 4 ? select_slots<4>(a, n, lds, stream) : select_slots<1>(a, n, lds, stream);
+    if (slots == 4) return select_slots<4, 256>(a, n, lds, stream);
+    // one token to a workgroup: sixteen waves where every compute unit has at most one of
+    // them with much to read (32 sequences of 512 blocks 24.7 us, 28.4 with eight waves),
+    // else eight (256 sequences of 32 blocks 27.6 us, 51.0 with sixteen)
+    return n <= 256 && a.b.cols >= 256 ? select_slots<1, 1024>(a, n, lds, stream)
+                                       : select_slots<1, 512>(a, n, lds, stream);
 }
 
 }  // namespace heal
