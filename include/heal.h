@@ -17,7 +17,7 @@
  * Reduction order.  For every output element the sum runs over K in 32-deep
  * chunks, k ascending, each chunk adding its three products into one FP32
  * accumulator in the order hiA*hiB, hiA*loB, loA*hiB; the K tail is padded
- * with zeros.  No entry point splits K across workgroups or uses atomics, and
+ * with zeros.  No product splits K across workgroups, nothing uses atomics, and
  * every kernel instance follows this order, so results are bitwise identical
  * run to run, for every M (a row's bits do not depend on the other rows), for
  * every N, and between the plain and batched entry points.
@@ -344,6 +344,8 @@ heal_status_t heal_scores_i16(int64_t M, int64_t N, int64_t K, const int16_t *Q,
  *   scales   [blocks][heads][2]         m of the keys, m of the values; for a block that is
  *                                       not complete, of the rows it has
  *   k_mean   [blocks][heads][dim]       mean of the block's (rotated) keys, FP64 sum
+ *                                       (both of the rows that the block had when it was
+ *                                       last appended to: cutting back leaves them)
  *   k_recent [slots][heads][2 * block][dim]    row of the token at place p: p % (2 * block)
  *   v_recent [slots][heads][dim][2 * block]
  * Nothing needs to be cleared before use.  A block holds one sequence's tokens for
