@@ -239,6 +239,44 @@ def test_read():
     assert torch.equal(k[17:].cpu(), heal.heal_kv_read(w.cache, 33, cu=ints([0, 0, 0, 33]), **w.kw())[0].cpu())
 
 
+@pytest.mark.parametrize("block", [16, 32, 64, 128])
+@pytest.mark.parametrize("dim", [64, 96, 128])
+def test_read_a_few_rows(dim, block):
+    """The last 1, 8, 9 and more rows of blocks that are not complete, as they came."""
+    w = World(3, heads=2, dim=dim, block=block, cols=3, seed=dim + block)
+    w.append([block + 13, block - 1, 2 * block + 15])
+    for n in (1, 2, 8, 9, 13):
+        announce("the last %d rows" % n)
+        got = heal.heal_kv_read(w.cache, 3 * n, cu=ints([0, n, 2 * n, 3 * n]), **w.kw())
+        for t, name in zip(got, ("k", "v")):
+            t = t.cpu().numpy()
+            for i, r in enumerate(w.ref):
+                assert np.array_equal(t[i * n:(i + 1) * n], getattr(r, name)[len(r.k) - n:]), (n, i, name)
+
+
+def test_a_shared_beginning():
+    """Sequences that list the same complete blocks and go on in their own."""
+    w = World(1, heads=2, dim=64, block=32, cols=4, seed=8)
+    k, v = w.rows(64 + 40), w.rows(64 + 40)
+    w.append([64], k[:64], v[:64])
+    table = np.concatenate([w.table, w.table])
+    spare = sorted(set(range(7)) - set(w.table[0].tolist()))
+    table[1, 2:] = spare[:2]
+    slots = [int(w.slots[0]), (int(w.slots[0]) + 1) % 3]
+    kw = {"table": dev(table), "lens": ints([64 + 40, 64 + 40]), "slots": ints(slots), "cu": ints([0, 40, 80])}
+    announce("append behind a shared beginning")
+    two = lambda x: dev(np.concatenate([x[64:], x[64:]]))  # noqa: E731
+    heal.heal_kv_append(w.cache, two(k), two(v), cos=dev(w.cos), sin=dev(w.sin), **kw)
+    w.ref[0].append(k[64:], v[64:], w.cos, w.sin, w.interleaved)
+    for p in range(64, 104):
+        w.ring[0][p % 64] = p
+    w.check()
+    q = dev(w.rows(40, 4))
+    out = heal.heal_kv_attention(w.cache, torch.cat([q, q]), **kw)
+    assert torch.equal(out[:40], out[40:])
+    _check_attention(w, [40], q.cpu().numpy())
+
+
 # ---- attention ------------------------------------------------------------------
 
 
@@ -853,6 +891,45 @@ def test_a_decode_step_captured_and_replayed():
         for name in ("out", "out2", "q_out", "sel"):
             assert torch.equal(a[name], b[name]), (r, name)
         assert torch.equal(a["kw"]["lens"], b["kw"]["lens"])
+
+
+def test_a_prompt_captured_and_replayed():
+    """A ragged call of the prompts' kernel in parts, with other lengths at each replay.
+    (Its tokens begin at a block's first, so that doing it again changes nothing.)"""
+    w = World(3, heads=2, dim=128, block=64, cols=40, seed=12)
+    w.append([2500, 900, 2500])
+    T, kw = 700, w.kw()
+    k, v, q = dev(w.rows(T)), dev(w.rows(T)), dev(w.rows(T, 8))
+    cu, cos, sin = ints([0, 640, 640, 690]), dev(w.cos), dev(w.sin)   # (ten tokens are nobody's)
+    out, lse, q_out = torch.empty_like(q), torch.empty(T, 8, device="cuda"), torch.empty_like(q)
+
+    def step():
+        heal.heal_kv_append(w.cache, k, v, cos=cos, sin=sin, q=q, q_out=q_out, cu=cu, **kw)
+        heal.heal_kv_attention(w.cache, q_out, cu=cu, out=out, lse=lse, **kw)
+
+    g = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    announce("capture of a prompt")
+    with torch.cuda.graph(g):
+        step()
+    for lens in ([2560, 900, 114], [640, 0, 50], [1280, 900, 1970], [2240, 5, 2098]):
+        kw["lens"].copy_(ints(lens))
+        got = []
+        for run in (step, g.replay, g.replay):
+            for t in (out, lse, q_out):
+                t.fill_(9.0)
+            announce("lengths %s %s" % (lens, run.__name__))
+            run()
+            torch.cuda.synchronize()
+            got.append([t.clone() for t in (out, lse, q_out)])
+            assert (out[690:] == 9.0).all() and (lse[690:] == 9.0).all() and (q_out[690:] == 9.0).all()
+        for x in got[1:]:
+            assert all(torch.equal(a, b) for a, b in zip(x, got[0])), lens
 
 
 def test_a_long_selection_captured():
