@@ -558,20 +558,13 @@ __device__ __forceinline__ float soften(const Tile<B> &t, f32x4 *st, const float
                                         const int32_t *row_hi, int g, Soft &w, f16x8 *ph, f16x8 *pl)
 {
     using T = Tile<B>;
-    float big = -__builtin_inff(), f[T::NB], vm[T::NB];
-    if (__builtin_expect(all, true)) {
+    float f[T::NB], vm[T::NB];
 #pragma unroll
-        for (int i = 0; i < T::NB; ++i) {
-            float top = -__builtin_inff();
-#pragma unroll
-            for (int s = i * T::GS; s < (i + 1) * T::GS; ++s)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) top = __builtin_fmaxf(top, st[s][e]);
-            f[i] = fk[i];
-            vm[i] = t.v[i];
-            big = __builtin_fmaxf(big, top * f[i]);
-        }
-    } else {
+    for (int i = 0; i < T::NB; ++i) {
+        f[i] = fk[i];
+        vm[i] = t.v[i];
+    }
+    if (__builtin_expect(!all, false)) {
         const int32_t lo = *row_lo, hi = *row_hi;
 #pragma unroll
         for (int i = 0; i < T::NB; ++i) {
@@ -588,9 +581,18 @@ __device__ __forceinline__ float soften(const Tile<B> &t, f32x4 *st, const float
                 for (int e = 0; e < 4; ++e) {
                     const int at = (s - i * T::GS) * 16 + e;
                     st[s][e] = at >= from && at <= to ? st[s][e] * fk[i] : -__builtin_inff();
-                    big = __builtin_fmaxf(big, st[s][e]);
                 }
         }
+    }
+    float big = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < T::NB; ++i) {
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int s = i * T::GS; s < (i + 1) * T::GS; ++s)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = __builtin_fmaxf(top, st[s][e]);
+        big = __builtin_fmaxf(big, top * f[i]);
     }
     int ev = kNoScale;
 #pragma unroll
