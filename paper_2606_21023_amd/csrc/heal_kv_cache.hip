@@ -573,9 +573,11 @@ __device__ __forceinline__ void pick_blocks(const uint64_t *key, int lo, int n, 
 // token the 16 rows are its queries.  The order of the sum is the same for every block,
 // so equal blocks score equally.  Bound by the latency of a workgroup's own stream of
 // means and then of the search (32 sequences of up to 512 blocks 25 us, 66 MB; 777 tokens
-// over up to 79 blocks 30 us, the same for a quarter of the means read four times).
+// over up to 79 blocks 27 us).  Where waves have few tiles each (all but the sixteen-wave
+// kernel) the next means are not asked for ahead: five waves fit on a SIMD instead of
+// four (those 777 tokens 29.3 us with, 26.9 without).
 template <int D, int SLOTS, int THREADS>
-__global__ void __launch_bounds__(THREADS, 4)
+__global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 5)
 kv_select_kernel(KvSelectArgs a, int B, int64_t wg0)
 {
     constexpr int slots = SLOTS;
@@ -623,15 +625,21 @@ kv_select_kernel(KvSelectArgs a, int B, int64_t wg0)
                 for (int i = 0; i < D / 16; ++i) m[i] = page >= 0 ? src[i] : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             };
             constexpr int STEP = THREADS / 64 * 16;
+            constexpr bool AHEAD = THREADS == 1024;
             int b0 = lo + wave * 16;
-            int page = b0 < hi ? page_of(b0) : -1, next = b0 + STEP < hi ? page_of(b0 + STEP) : -1;
+            int page = b0 < hi ? page_of(b0) : -1;
+            int next = AHEAD && b0 + STEP < hi ? page_of(b0 + STEP) : -1;
             f32x4 m[D / 16];
-            mean_of(page, m);
+            if (AHEAD) mean_of(page, m);
             for (; b0 < hi; b0 += STEP) {
-                // the next tile's means and the page behind it are on the way
-                f32x4 m2[D / 16];
-                mean_of(next, m2);
-                const int after = b0 + 2 * STEP < hi ? page_of(b0 + 2 * STEP) : -1;
+                // the page of the next tile is on the way, or its means and the page behind
+                f32x4 m2[AHEAD ? D / 16 : 1];
+                if (AHEAD)
+                    mean_of(next, m2);
+                else
+                    mean_of(page, m);
+                const int ahead = b0 + (AHEAD ? 2 : 1) * STEP;
+                const int after = ahead < hi ? page_of(ahead) : -1;
                 f64x4 sum = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll
                 for (int i = 0; i < D / 4; ++i)
@@ -657,10 +665,12 @@ kv_select_kernel(KvSelectArgs a, int B, int64_t wg0)
                     uint64_t *at = key + (int64_t)kk * a.b.cols + (b0 + col - lo);
                     *at = g0 > 0 && *at > best ? *at : best;
                 }
-                page = next;
+                page = AHEAD ? next : after;
                 next = after;
+                if (AHEAD) {
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) m[i] = m2[i];
+                    for (int i = 0; i < D / 16; ++i) m[i] = m2[AHEAD ? i : 0];
+                }
             }
         }
     }
@@ -738,11 +748,13 @@ hipError_t launch_kv_select(const KvSelectArgs &a, hipStream_t stream)
     const int64_t n = (slots == 4 ? kv_tiles(a.b.tokens, a.b.seqs, 1, 4) : a.b.tokens) * a.c.heads;
     const size_t lds = (size_t)a.b.cols * slots * sizeof(uint64_t);
     if (slots == 4) return select_slots<4, 256>(a, n, lds, stream);
-    // one token to a workgroup: sixteen waves where every compute unit has at most one of
-    // them with much to read (32 sequences of 512 blocks 24.7 us, 28.4 with eight waves),
-    // else eight (256 sequences of 32 blocks 27.6 us, 51.0 with sixteen)
-    return n <= 256 && a.b.cols >= 256 ? select_slots<1, 1024>(a, n, lds, stream)
-                                       : select_slots<1, 512>(a, n, lds, stream);
+    // one token to a workgroup: sixteen waves where a compute unit has at most one workgroup
+    // with much to read (32 sequences of up to 234 blocks 15.0 us, 17.9 with four waves),
+    // else so few that each has a tile of 16 blocks and the next workgroups find room (256
+    // sequences of 16 blocks 10.6 us with two waves, 24.8 with eight; of 62 blocks 22.2 us
+    // with four, 31.1)
+    if (n <= 256 && a.b.cols >= 128) return select_slots<1, 1024>(a, n, lds, stream);
+    return a.b.cols <= 32 ? select_slots<1, 128>(a, n, lds, stream) : select_slots<1, 256>(a, n, lds, stream);
 }
 
 }  // namespace heal

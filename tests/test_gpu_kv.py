@@ -790,6 +790,29 @@ def test_select(dim, block, group):
     _check_select(w, [3, 4, 0, 2], w.rows(9, 2 * group), 6)   # more tokens than the length: places below 0
 
 
+@pytest.mark.parametrize("seqs,cols", [(3, 20), (3, 32), (3, 33), (3, 127), (3, 128), (2, 700), (140, 130)])
+@pytest.mark.parametrize("dim,group", [(64, 1), (96, 5), (128, 16), (128, 17)])
+def test_select_for_single_tokens(dim, group, seqs, cols):
+    """One token of each sequence, without cu: from no block to as many as the table has."""
+    rng = np.random.default_rng(dim + group + cols)
+    c = heal.KVCache.empty(seqs * cols, seqs, 2, dim, 16)
+    mean = rng.standard_normal((seqs * cols, 2, dim)).astype(np.float32)
+    c.k_mean.copy_(dev(mean))
+    table = rng.permutation(seqs * cols).reshape(seqs, cols).astype(np.int32)
+    lens = rng.integers(0, cols * 16 + 1, seqs)
+    lens[0], lens[-1] = cols * 16, cols * 8 + 1
+    q = rng.standard_normal((seqs, 2 * group, dim)).astype(np.float32)
+    for n_sel, first, last in ((2, 1, 1), (17, 2, 3)):
+        announce("select %s of %s" % (n_sel, lens[:3]))
+        got = heal.heal_kv_select(c, dev(q), n_sel, dev(table), ints(lens.tolist()), keep_first=first,
+                                  keep_last=last).cpu().numpy()
+        for i in range(seqs):
+            for h in range(2):
+                want = kv_ref.select(q[i, h * group:(h + 1) * group], mean[table[i], h].astype(np.float64),
+                                     int(lens[i]) - 1, 16, n_sel, first, last)
+                assert got[i, h].tolist() == want, (i, h)
+
+
 def test_select_equal_scores_and_no_numbers():
     w = World(1, heads=2, dim=64, block=16, cols=200)
     w.append([16 * 200])
