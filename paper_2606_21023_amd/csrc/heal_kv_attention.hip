@@ -674,7 +674,7 @@ __device__ __forceinline__ float unit_of(int ref)
 // LDS, and the waves' results are joined at the end.  The next tile's keys are asked
 // for as soon as this one's are in the matrix units, its values likewise, so that a
 // wave has 16 KiB on the way while it computes.  Bound by memory where a sequence has
-// one token (64 of 4096 to 8192 tokens, 8 heads of 128: 151 us, 816 MB, 5.4 TB/s), by
+// one token (64 of 4096 to 8192 tokens, 8 heads of 128: 150 us, 816 MB, 5.4 TB/s), by
 // latency where there is little to read (8191 tokens of one sequence 13 us).
 template <int D, int B, bool ONCE>
 __global__ void __launch_bounds__(256, 2)
@@ -894,8 +894,8 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
 // wait in LDS in the order of the matrix operands (lane by lane, no bank conflicts).
 // A key fragment feeds four matrix instructions (two groups of 16 rows, two parts of
 // the pair) and a value fragment likewise.  Bound by instruction issue: the matrix
-// units are busy 43% of the time, the vector units (exponentials, pairs, masks) 55%
-// (512 tokens of 32 heads over 16001: 264 GFLOP of FP16 products in 253 us, 1.04 PFLOP/s).
+// units are busy 44% of the time, the vector units (exponentials, pairs, masks) 53%
+// (512 tokens of 32 heads over 16001: 264 GFLOP of FP16 products in 255 us, 1.04 PFLOP/s).
 template <int D, int B>
 __global__ void __launch_bounds__(256, 2)
 kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
