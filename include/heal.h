@@ -345,7 +345,8 @@ heal_status_t heal_scores_i16(int64_t M, int64_t N, int64_t K, const int16_t *Q,
  *                                       not complete, of the rows it has
  *   k_mean   [blocks][heads][dim]       mean of the block's (rotated) keys, FP64 sum
  *                                       (both of the rows that the block had when it was
- *                                       last appended to: cutting back leaves them)
+ *                                       last appended to: cutting back leaves them, and
+ *                                       what reads an incomplete block goes by its rows)
  *   k_recent [slots][heads][2 * block][dim]    row of the token at place p: p % (2 * block)
  *   v_recent [slots][heads][dim][2 * block]
  * Nothing needs to be cleared before use.  A block holds one sequence's tokens for
@@ -397,8 +398,13 @@ typedef struct heal_kv_batch_t {
  *             below `places` is taken as it is, without rotation;
  *   q, q_out: [tokens][heads_q][dim] or both NULL: queries rotated likewise; q_out
  *             may be q itself with the same strides, and must not overlap it otherwise.
- * Values are not rotated.  Rows must be finite for their block's codes to mean
- * anything.
+ * Values are not rotated.
+ *
+ * A key or value that is not finite: while its block is not complete, a key makes the
+ * whole output of the rows that see its token no number, a value the column that it is
+ * in; other rows do not notice it, and nothing of it is left when the sequence is cut
+ * back.  The codes of a complete block with such a row are no numbers, to all that see
+ * any token of the block and when they are read back.
  */
 heal_status_t heal_kv_append(const heal_kv_cache_t *cache, const heal_kv_batch_t *batch,
                              const float *k, int64_t k_token, int64_t k_head,

@@ -8,8 +8,11 @@
 // 2^-25 of 2^14), so  q . c = hi . c + lo . c  on FP16 MFMA with FP32 sums.  The
 // softmax weights p in [0, 1] are multiplied by the block's value maximum, scaled by
 // a power of two (below) and split alike:  o += (p_hi + p_lo) . c.  An FP32 row of
-// the cache is scaled by its block's maximum and split too; the product of the two
-// residuals is left out (2^-22 of 2^-11).
+// the cache is scaled by a power of two of its own, from its largest finite element,
+// and split too (2^-22 of an element, and 2^-25 of 2^14 for keys and of 2^7 for values);
+// the product of the two residuals is left out (2^-22 of 2^-11).  What a query does not
+// see has the weight 0, so a value that is not finite is taken as 0 in the products and
+// put into the columns of the rows that see it behind them.
 //
 // S^T = K q^T is formed rather than S: a lane then holds four tokens in a row of one
 // query, and the 16 scores it has of a 64-token tile are, as they stand, its part of
@@ -75,8 +78,8 @@ __device__ __forceinline__ void pairs8(const float *x, f16x8 &hi, f16x8 &lo)
     }
 }
 
-// e with |x| in [2^(e-1), 2^e), or kNoScale for 0 (and for what is not finite: its
-// products come out as no numbers with any scale).
+// e with |x| in [2^(e-1), 2^e), or kNoScale for 0 (and for what is not finite: a block's
+// codes times such a maximum are no numbers with any scale, nor is a row with such a key).
 __device__ __forceinline__ int exponent(float x)
 {
     if (!(__builtin_fabsf(x) > 0.0f) || __builtin_isinf(x)) return kNoScale;
@@ -108,6 +111,29 @@ __device__ __forceinline__ float max_over_groups(float x)
     x = __builtin_fmaxf(x, __shfl_xor(x, 16));
     return __builtin_fmaxf(x, __shfl_xor(x, 32));
 }
+
+// (without LDS: of a swap with itself one result has the lower half of the wave, or of each
+// half, twice, and the other one the upper)
+__device__ __forceinline__ int max_over_groups(int x)
+{
+    const auto h = __builtin_amdgcn_permlane32_swap((uint32_t)x, (uint32_t)x, false, false);
+    x = max((int)h[0], (int)h[1]);
+    const auto q = __builtin_amdgcn_permlane16_swap((uint32_t)x, (uint32_t)x, false, false);
+    return max((int)q[0], (int)q[1]);
+}
+
+// The largest x of a lane's group of 16.
+__device__ __forceinline__ uint32_t max_in_group(uint32_t x)
+{
+    // (row_ror: the 16 lanes turned by 8, 4, 2 and 1)
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x128, 0xf, 0xf, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x124, 0xf, 0xf, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x122, 0xf, 0xf, true));
+    return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x121, 0xf, 0xf, true));
+}
+
+constexpr uint32_t kInfinity = 0x7f800000u;
+__device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
 
 __device__ __forceinline__ float sum_over_groups(float x)
 {
@@ -262,7 +288,7 @@ struct Blocks {
     static constexpr int EPT = B < 64 ? 64 / B : 1, TILES = 64 / EPT, STEP = B < 64 ? B : 64;
     int blk;     // block of the sequence, or -1 where the cache holds nothing of it
     int page;    // its page (0 where there is none), or -1 - page where it is read from the ring
-    float k, v;  // m of its keys and values
+    float k, v;  // m of its keys and values (a block that is not complete goes by its rows)
 
     __device__ __forceinline__ void load(const KvAttnArgs &a, const KvSeq &s, int seq, int slot, int head,
                                          const int32_t *list, int64_t first, int64_t to, int waves)
@@ -331,27 +357,39 @@ struct Tile {
             coded = coded && page[i] >= 0;
         }
     }
-    // of the block of group s, which need not be a constant
-    __device__ __forceinline__ int blk_of(int s) const { return blk[NB == 1 ? 0 : s / GS]; }
-    __device__ __forceinline__ int page_of(int s) const { return page[NB == 1 ? 0 : s / GS]; }
-    __device__ __forceinline__ float key_of(int s) const { return k[NB == 1 ? 0 : s / GS]; }
-    __device__ __forceinline__ float value_of(int s) const { return v[NB == 1 ? 0 : s / GS]; }
-    // the factor of the scores with block i (of group s), but for the query's
-    __device__ __forceinline__ float key_factor(int i) const { return factor(blk[i], page[i], k[i]); }
-    __device__ __forceinline__ float key_factor_of(int s) const { return factor(blk_of(s), page_of(s), key_of(s)); }
-    static __device__ __forceinline__ float factor(int blk, int page, float k)
-    {
-        if (blk < 0) return 0.0f;
-        if (page >= 0) return k * (1.0f / 127.0f);
-        const int e = exponent(k);
-        return ldexpf(1.0f, e == kNoScale ? 0 : e - 14);
-    }
+    // the factor of the scores with coded block i, but for the query's (0 where there is none)
+    __device__ __forceinline__ float key_factor(int i) const { return k[i] * (1.0f / 127.0f); }
     // place of the first token of group s
     __device__ __forceinline__ int32_t place(int s) const
     {
-        return blk_of(s) * B + off + s % GS * 16;
+        return blk[s / GS] * B + off + s % GS * 16;
     }
 };
+
+// One group of 16 tokens of a tile that is not coded throughout.
+struct Group {
+    int blk, page;   // as in Blocks
+    float k, v;
+    int off;         // of its first token within the block
+    int32_t place;   // of its first token
+
+    __device__ __forceinline__ bool coded() const { return blk < 0 || page >= 0; }
+};
+template <int B>
+__device__ __forceinline__ Group group_of(const Tile<B> &t, int s)
+{
+    const int i = s / Tile<B>::GS;
+    return Group{t.blk[i], t.page[i], t.k[i], t.v[i], t.off + s % Tile<B>::GS * 16, t.place(s)};
+}
+// ... of the first of the tiles that a wave's lanes hold the blocks of; s need not be a
+// constant.
+template <int B>
+__device__ __forceinline__ Group group_of(const Blocks<B> &b, int64_t kt, int s)
+{
+    const int i = s / Tile<B>::GS, off = (B > 64 ? (int)(kt & 1) * 64 : 0) + s % Tile<B>::GS * 16;
+    const int blk = from_lane(b.blk, i);
+    return Group{blk, from_lane(b.page, i), from_lane(b.k, i), from_lane(b.v, i), off, blk * B + off};
+}
 
 // Codes as they come from memory, in the registers of one lane: of the keys of group
 // s, the D/4 bytes of row r that belong to lanes g; of row 16 n + r of V^T, the four
@@ -370,7 +408,7 @@ template <int D, int B, bool ONCE>
 __device__ __forceinline__ void load_group_keys(const KvAttnArgs &a, const Tile<B> &t, int s, int head, int r, int g,
                                                 uint32_t *k)
 {
-    const int8_t *src = a.c.kc + ((int64_t)t.page_of(s) * a.c.heads + head) * (B * D) + (t.off + s % Tile<B>::GS * 16) * D;
+    const int8_t *src = a.c.kc + ((int64_t)t.page[s / Tile<B>::GS] * a.c.heads + head) * (B * D) + (t.off + s % Tile<B>::GS * 16) * D;
     const uint32_t at = hidden(r * D + g * (D / 4));
     if constexpr (D % 64 == 0) {
 #pragma unroll
@@ -429,52 +467,63 @@ struct Codes {
     }
 };
 
-// Keys of group s of a tile that is not coded throughout, as FP16 pairs: f(k, hi, lo)
-// for each chunk of 32 elements.
+// Keys of a group, as FP16 pairs: f(k, hi, lo)
+// for each chunk of 32 elements.  Returns the factor of the scores with token r, but for
+// the query's.
 template <int D, int B, class F>
-__device__ __forceinline__ void keys_of_group(const KvAttnArgs &a, const Tile<B> &t, int s, int slot, int head,
-                                              int64_t len, int r, int g, F f)
+__device__ __forceinline__ float keys_of_group(const KvAttnArgs &a, const Group &t, int slot, int head,
+                                               int64_t len, int r, int g, F f)
 {
     const f16x8 zero = {};
-    const int blk = t.blk_of(s), page = t.page_of(s), off = t.off + s % Tile<B>::GS * 16;
+    const int blk = t.blk, page = t.page, off = t.off;
     if (blk < 0) {
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) f(k, zero, zero);
-    } else if (page >= 0) {
+        return 0.0f;
+    }
+    if (page >= 0) {
         const int8_t *src = a.c.kc + ((int64_t)page * a.c.heads + head) * (B * D) + (off + r) * D + g * (D / 4);
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
             const u32x2 w = *reinterpret_cast<const u32x2 *>(src + 8 * k);
             f(k, codes8(w[0], w[1]), zero);
         }
-    } else {
-        // FP32 rows; what lies behind the last one may be anything
-        const float *src = a.c.kr + ((int64_t)slot * a.c.heads + head) * (2 * B * D) + ((blk & 1) * B + off + r) * D + g * (D / 4);
-        const bool there = (int64_t)t.place(s) + r < len;
-        const int e = exponent(t.key_of(s)), shift = e == kNoScale ? 0 : 14 - e;
+        return t.k * (1.0f / 127.0f);
+    }
+    // FP32 rows; what lies behind the last one may be anything
+    const float *src = a.c.kr + ((int64_t)slot * a.c.heads + head) * (2 * B * D) + ((blk & 1) * B + off + r) * D + g * (D / 4);
+    const bool there = (int64_t)t.place + r < len;
+    float x[D / 4];
+    uint32_t top = 0u;
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k) {
-            float x[8];
+    for (int i = 0; i < D / 4; i += 4) {
+        const f32x4 y = *reinterpret_cast<const f32x4 *>(src + i);
 #pragma unroll
-            for (int j = 0; j < 8; j += 4) {
-                const f32x4 y = *reinterpret_cast<const f32x4 *>(src + 8 * k + j);
-#pragma unroll
-                for (int b = 0; b < 4; ++b) x[j + b] = there ? ldexpf(y[b], shift) : 0.0f;
-            }
-            f16x8 hi, lo;
-            pairs8(x, hi, lo);
-            f(k, hi, lo);
+        for (int b = 0; b < 4; ++b) {
+            x[i + b] = there ? y[b] : 0.0f;
+            top = max(top, magnitude(x[i + b]));
         }
     }
+    // (a key that is not finite: every score with it is no number)
+    const int e = exponent(__builtin_bit_cast(float, max_over_groups((int)top))), shift = e == kNoScale ? 0 : 14 - e;
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) {
+        f16x8 hi, lo;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[8 * k + j] = ldexpf(x[8 * k + j], shift);
+        pairs8(x + 8 * k, hi, lo);
+        f(k, hi, lo);
+    }
+    return ldexpf(1.0f, -shift);
 }
 
-// The lane's four values of group s in row 16 n + r of V^T: codes as they are, FP32
-// rows scaled by a power of two.
+// The lane's four values of a group in row 16 n + r of V^T: codes, or FP32 rows, as they
+// are.
 template <int D, int B>
-__device__ __forceinline__ f32x4 values_of_group(const KvAttnArgs &a, const Tile<B> &t, int s, int n, int slot, int head,
+__device__ __forceinline__ f32x4 values_of_group(const KvAttnArgs &a, const Group &t, int n, int slot, int head,
                                                  int64_t len, int r, int g)
 {
-    const int blk = t.blk_of(s), page = t.page_of(s), off = t.off + s % Tile<B>::GS * 16;
+    const int blk = t.blk, page = t.page, off = t.off;
     f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
     if (blk < 0) return x;
     if (page >= 0) {
@@ -485,27 +534,83 @@ __device__ __forceinline__ f32x4 values_of_group(const KvAttnArgs &a, const Tile
         return x;
     }
     const float *src = a.c.vr + ((int64_t)slot * a.c.heads + head) * (2 * B * D) + (int64_t)(16 * n + r) * (2 * B) + (blk & 1) * B + off + 4 * g;
-    const int e = exponent(t.value_of(s)), shift = e == kNoScale ? 0 : 7 - e;
-    const int64_t rows = len - t.place(s);
+    const int64_t rows = len - t.place;
     const f32x4 y = *reinterpret_cast<const f32x4 *>(src);
 #pragma unroll
-    for (int b = 0; b < 4; ++b) x[b] = 4 * g + b < rows ? ldexpf(y[b], shift) : 0.0f;
+    for (int b = 0; b < 4; ++b) x[b] = 4 * g + b < rows ? y[b] : 0.0f;
     return x;
 }
 
-// ... of groups 2 c and 2 c + 1, as FP16 pairs.
-template <int D, int B>
-__device__ __forceinline__ void values_of_half(const KvAttnArgs &a, const Tile<B> &t, int c, int n, int slot, int head,
-                                               int64_t len, int r, int g, f16x8 &hi, f16x8 &lo)
+// 0 for what is not finite.
+__device__ __forceinline__ f32x4 finite(f32x4 x)
 {
-    float x[8];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const f32x4 y = values_of_group<D, B>(a, t, 2 * c + j, n, slot, head, len, r, g);
+    for (int b = 0; b < 4; ++b) x[b] = magnitude(x[b]) < kInfinity ? x[b] : 0.0f;
+    return x;
+}
+
+// The exponents of the lane's four tokens of a group, values(n) being its values in row
+// 16 n + r of V^T: of an FP32 row that of its largest finite value, of a coded block that
+// of its maximum.  odd: there is a value that is not finite (the wave's).
+template <int N, class F>
+__device__ __forceinline__ i32x4 value_exponents(const Group &t, F values, bool &odd)
+{
+    odd = false;
+    const int eb = exponent(t.v);
+    if (t.coded()) return i32x4{eb, eb, eb, eb};
+    uint32_t top[4] = {};
+    auto add = [&](f32x4 x) HEAL_INLINE {
 #pragma unroll
-        for (int b = 0; b < 4; ++b) x[4 * j + b] = y[b];
+        for (int b = 0; b < 4; ++b) top[b] = max(top[b], magnitude(x[b]));
+    };
+#pragma unroll
+    for (int n = 0; n < N; ++n) add(values(n));
+    odd = __ballot(max(max(top[0], top[1]), max(top[2], top[3])) >= kInfinity) != 0;
+    if (__builtin_expect(odd, false)) {
+        for (int b = 0; b < 4; ++b) top[b] = 0u;
+#pragma unroll
+        for (int n = 0; n < N; ++n) add(finite(values(n)));
     }
-    pairs8(x, hi, lo);
+    i32x4 e;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) e[b] = exponent(__builtin_bit_cast(float, max_in_group(top[b])));
+    return e;
+}
+
+// Finite values as the products take them: codes as they are, FP32 rows scaled by their
+// powers of two.
+__device__ __forceinline__ f32x4 scaled_values(const Group &t, f32x4 x, i32x4 e)
+{
+    if (t.coded()) return x;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) x[b] = ldexpf(x[b], 7 - e[b]);
+    return x;
+}
+
+// 1 where a value is not finite, else 0.
+__device__ __forceinline__ f32x4 odd_values(f32x4 x)
+{
+#pragma unroll
+    for (int b = 0; b < 4; ++b) x[b] = magnitude(x[b]) < kInfinity ? 0.0f : 1.0f;
+    return x;
+}
+
+__device__ __forceinline__ f16x8 to_f16(f32x4 a, f32x4 b)
+{
+    f16x8 x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[i] = (_Float16)a[i];
+        x[4 + i] = (_Float16)b[i];
+    }
+    return x;
+}
+
+// No number where x counts anything.
+__device__ __forceinline__ void spoil(f32x4 &o, f32x4 x)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = x[i] > 0.0f ? __builtin_nanf("") : o[i];
 }
 
 // Where a row's result goes: its place in out, or in the workspace of its part.
@@ -549,8 +654,8 @@ struct Soft {
     int ref;
 };
 
-// A tile's scores become weights.  st: the lane's scores, of tokens 4 g + i of group s,
-// before their factors fk (one for each block).  Returns the weights times the
+// The scores of a tile whose blocks are all coded become weights.  st: the lane's scores, of
+// tokens 4 g + i of group s, before their factors fk (one for each block).  Returns the weights times the
 // blocks' value factors as FP16 pairs, in the order of the values' operand, and
 // what the output so far is to be multiplied by.
 template <int B>
@@ -606,8 +711,7 @@ __device__ __forceinline__ float soften(const Tile<B> &t, f32x4 *st, const float
     float wv[T::NB];
 #pragma unroll
     for (int i = 0; i < T::NB; ++i) {
-        const int e = exponent(vm[i]);
-        wv[i] = t.page[i] >= 0 ? ldexpf(vm[i], 14 - rn) : e == kNoScale ? 0.0f : ldexpf(127.0f, e + 7 - rn);
+        wv[i] = ldexpf(vm[i], 14 - rn);
     }
     float sum = 0.0f;
 #pragma unroll
@@ -628,35 +732,57 @@ __device__ __forceinline__ float soften(const Tile<B> &t, f32x4 *st, const float
     return turn;
 }
 
-// ... of one group s, four scores to a lane; the other half of the operand is zeros.
-template <int B>
-__device__ __forceinline__ float soften_group(const Tile<B> &t, int s, f32x4 st, float fk, int32_t lo, int32_t hi, int g,
-                                              Soft &w, f16x8 &ph, f16x8 &pl)
+// Whether the row that sees lo .. hi sees each of the lane's four tokens of a group.
+__device__ __forceinline__ void sees_tokens(const Group &t, int32_t lo, int32_t hi, int g, bool *is)
 {
-    const int32_t p0 = t.place(s);
-    const bool met = t.blk_of(s) >= 0 && p0 <= hi && p0 + 15 >= lo;
-    const float vm = met ? t.value_of(s) : 0.0f;
-    float big = -__builtin_inff();
+    const int32_t p0 = t.place + 4 * g;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int32_t p = p0 + 4 * g + e;
-        st[e] = met && p >= lo && p <= hi ? st[e] * fk : -__builtin_inff();
-        big = __builtin_fmaxf(big, st[e]);
+    for (int e = 0; e < 4; ++e) is[e] = t.blk >= 0 && p0 + e >= lo && p0 + e <= hi;
+}
+
+// ... of a tile that may hold FP32 rows: N groups, factors(s) and exponents(s) being the
+// factors and the values' exponents of the lane's tokens of group s; the tokens that the row
+// sees make its units.  Leaves the weights in st.
+template <int N, class F, class E>
+__device__ __forceinline__ float soften_tokens(const Group *t, f32x4 *st, F factors, E exponents, int32_t lo,
+                                               int32_t hi, int g, Soft &w)
+{
+    float big = -__builtin_inff(), vm[N];
+    int ev = kNoScale;
+#pragma unroll
+    for (int s = 0; s < N; ++s) {
+        const bool met = t[s].blk >= 0 && t[s].place <= hi && t[s].place + 15 >= lo;
+        vm[s] = met ? t[s].v : 0.0f;
+        if (t[s].coded()) ev = max(ev, exponent(vm[s]));
+        const f32x4 fk = factors(s);
+        const i32x4 ve = exponents(s);
+        bool is[4];
+        sees_tokens(t[s], lo, hi, g, is);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            st[s][e] = is[e] ? st[s][e] * fk[e] : -__builtin_inff();
+            big = __builtin_fmaxf(big, st[s][e]);
+            ev = is[e] && !t[s].coded() ? max(ev, ve[e]) : ev;
+        }
     }
     const float mn = __builtin_fmaxf(w.m, max_over_groups(big));
     const float mz = mn == -__builtin_inff() ? 0.0f : mn;
     const float alpha = __builtin_amdgcn_exp2f(w.m - mz);
-    const int ev = exponent(vm), rn = max(w.ref, ev);
+    const int rn = max(w.ref, max_over_groups(ev));
     const float turn = w.ref == kNoScale ? alpha : ldexpf(alpha, w.ref - rn);
-    const float wv = t.page_of(s) >= 0 ? ldexpf(vm, 14 - rn) : ev == kNoScale ? 0.0f : ldexpf(127.0f, ev + 7 - rn);
-    float p[8] = {}, sum = 0.0f;
+    float sum = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const float x = __builtin_amdgcn_exp2f(st[e] - mz);
-        sum += x;
-        p[e] = x * wv;
+    for (int s = 0; s < N; ++s) {
+        const i32x4 ve = exponents(s);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float x = __builtin_amdgcn_exp2f(st[s][e] - mz);
+            sum += x;
+            // (a row that is not seen may be larger than rn stands for: its x is 0)
+            const float wv = t[s].coded() ? ldexpf(vm[s], 14 - rn) : ldexpf(127.0f, min(ve[e] - rn, 0) + 7);
+            st[s][e] = x * wv;
+        }
     }
-    pairs8(p, ph, pl);
     w.m = mn;
     w.l = w.l * alpha + sum;
     w.ref = rn;
@@ -800,37 +926,61 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
     // the bytes of a coded tile to wait for (8191 tokens of one sequence: 17.7 us, 12.5 so).
     auto ring_tile = [&](int64_t kt) HEAL_INLINE {
         Blocks<B> blocks;
-        T tile;
         blocks.load(a, t.s, t.seq, slot, head, list, kt, to, 1);
-        tile.take(blocks, 0, kt);
-        if (tile.coded || tile.blk_of(wave) < 0) return;
+        const Group own = group_of(blocks, kt, wave);
+        if (Blocks<B>::EPT == 1 ? own.coded() : own.blk < 0 || !__ballot(lane < Blocks<B>::EPT && blocks.page < 0))
+            return;   // the loop has done it, or there is nothing
         f16x8 qh[KC], ql[KC], kh[KC], kl[KC];
         f32x4 v[N];
         const float fq = load_query<D>(a, token < 0 ? nullptr : a.q + token * a.q_token + head_q * a.q_head + g * (D / 4), qh, ql);
 #pragma unroll
-        for (int n = 0; n < N; ++n) v[n] = values_of_group<D, B>(a, tile, wave, n, slot, head, t.s.len, r, g);
-        keys_of_group<D, B>(a, tile, wave, slot, head, t.s.len, r, g, [&](int k, f16x8 h, f16x8 x) {
+        for (int n = 0; n < N; ++n) v[n] = values_of_group<D, B>(a, own, n, slot, head, t.s.len, r, g);
+        const float fr = keys_of_group<D, B>(a, own, slot, head, t.s.len, r, g, [&](int k, f16x8 h, f16x8 x) {
             kh[k] = h;
             kl[k] = x;
         });
-        f32x4 st = {0.0f, 0.0f, 0.0f, 0.0f};
+        // (the lane has the scores of tokens 4 g + i, and lane r the factor of token r)
+        f32x4 st = {0.0f, 0.0f, 0.0f, 0.0f}, fk;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) fk[e] = __shfl(fr, 4 * g + e);
 #pragma unroll
         for (int k = 0; k < KC; ++k) {
             st = mfma16(kh[k], qh[k], st);
             st = mfma16(kh[k], ql[k], st);
             st = mfma16(kl[k], qh[k], st);
         }
+        fk *= fq;
+        bool odd;
+        const i32x4 ve = value_exponents<N>(own, [&](int n) { return v[n]; }, odd);
+        if (__builtin_expect(odd, false)) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) v[n] = finite(v[n]);
+        }
+        const float turn = soften_tokens<1>(
+            &own, &st, [&](int) { return fk; }, [&](int) { return ve; }, row_lo[r], row_hi[r], g, w);
         f16x8 ph, pl;
-        const float turn = soften_group<B>(tile, wave, st, tile.key_factor_of(wave) * fq, row_lo[r], row_hi[r], g, w, ph, pl);
+        const float p[8] = {st[0], st[1], st[2], st[3]};   // (the other half of the operand is zeros)
+        pairs8(p, ph, pl);
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const float x[8] = {v[n][0], v[n][1], v[n][2], v[n][3]};
+            const f32x4 y = scaled_values(own, v[n], ve);
+            const float x[8] = {y[0], y[1], y[2], y[3]};
             f16x8 vh, vl;
             pairs8(x, vh, vl);
             o[n] *= turn;
             o[n] = mfma16(vh, ph, o[n]);
             o[n] = mfma16(vh, pl, o[n]);
             o[n] = mfma16(vl, ph, o[n]);
+        }
+        if (__builtin_expect(odd, false)) {   // (the wave's)
+            const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
+            const int r2 = hidden(r), g2 = hidden(g);
+            bool is[4];
+            sees_tokens(own, row_lo[r2], row_hi[r2], g2, is);
+            const f16x8 seen = to_f16(f32x4{is[0] ? 1.0f : 0.0f, is[1] ? 1.0f : 0.0f, is[2] ? 1.0f : 0.0f, is[3] ? 1.0f : 0.0f}, none);
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+                spoil(o[n], mfma16(to_f16(odd_values(values_of_group<D, B>(a, own, n, slot, head, t.s.len, r2, g2)), none), seen, none));
         }
     };
     if (t.s.len % B != 0 && span.last >= span.first) {
@@ -908,6 +1058,10 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
     // what a row needs once a tile, or seldom: kept out of the registers, which are full
     __shared__ float row_factor[R];
     __shared__ int32_t row_lo[R], row_hi[R];
+    // of a tile with FP32 rows: each token's factor of the scores and exponent of its values,
+    // and whether a wave met a value that is not finite
+    __shared__ float token_factor[64];
+    __shared__ int32_t token_exponent[64], odd[4];
     const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int64_t wg = wg0 + blockIdx.x;
     // heads side by side, so that with eight of them each XCD has its own head's keys in
@@ -972,19 +1126,50 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
         // a tile with FP32 rows (or without some of its blocks): both parts of the pairs
         auto keep_pairs = [&](const T &x, int b) HEAL_INLINE {
             const int r2 = hidden(r), g2 = hidden(g);
-            keys_of_group<D, B>(a, x, wave, slot, head, t.s.len, r2, g2, [&](int k, f16x8 h, f16x8 l) {
+            const Group own = group_of(x, wave);
+            const float fr = keys_of_group<D, B>(a, own, slot, head, t.s.len, r2, g2, [&](int k, f16x8 h, f16x8 l) {
                 frag[b][wave * KC + k][lane] = h;
                 frag[b ^ 1][wave * KC + k][lane] = l;
             });
+            bool bad;
+            const i32x4 ve = value_exponents<N>(
+                own, [&](int n) { return values_of_group<D, B>(a, own, n, slot, head, t.s.len, r2, g2); }, bad);
+            if (g == 0) token_factor[16 * wave + r] = fr;
+            if (r == 0) *reinterpret_cast<i32x4 *>(&token_exponent[16 * wave + 4 * g]) = ve;
+            if (lane == 0) odd[wave] = bad;
+            __syncthreads();
+            const bool any = uniform(odd[0] | odd[1] | odd[2] | odd[3]);
 #pragma unroll 1
             for (int n = wave; n < N; n += 4)
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
+                    float y[8];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const i32x4 e = *reinterpret_cast<const i32x4 *>(&token_exponent[16 * (2 * c + j) + 4 * g2]);
+                        const Group of = group_of(x, 2 * c + j);
+                        f32x4 v = values_of_group<D, B>(a, of, n, slot, head, t.s.len, r2, g2);
+                        if (any) v = finite(v);
+                        v = scaled_values(of, v, e);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[4 * j + i] = v[i];
+                    }
                     f16x8 h, l;
-                    values_of_half<D, B>(a, x, c, n, slot, head, t.s.len, r2, g2, h, l);
+                    pairs8(y, h, l);
                     frag[b][4 * KC + 2 * n + c][lane] = h;
                     frag[b ^ 1][4 * KC + 2 * n + c][lane] = l;
                 }
+        };
+        // ... and 1 for each value that is not finite, in place of the values
+        auto keep_odd = [&](const T &x, int b) HEAL_INLINE {
+            const int r2 = hidden(r), g2 = hidden(g);
+#pragma unroll 1
+            for (int n = wave; n < N; n += 4)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    frag[b][4 * KC + 2 * n + c][lane] =
+                        to_f16(odd_values(values_of_group<D, B>(a, group_of(x, 2 * c), n, slot, head, t.s.len, r2, g2)),
+                               odd_values(values_of_group<D, B>(a, group_of(x, 2 * c + 1), n, slot, head, t.s.len, r2, g2)));
         };
 
         // the tiles of the ring's block, the last ones, come after the loop
@@ -995,9 +1180,10 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
         // the tile in LDS; residuals: with FP32 rows, whose residuals the other buffer has
         auto compute = [&](auto residuals) HEAL_INLINE {
             constexpr bool X = decltype(residuals)::value;
-            // fragments are read from LDS three steps (of four matrix instructions) ahead
+            // fragments are read from LDS three steps (of four matrix instructions) ahead, or one
+            // where residuals take the registers
             const f16x8(*hi)[64] = frag[buf], (*res)[64] = frag[buf ^ 1];
-            constexpr int A = 3;
+            constexpr int A = X ? 1 : 3;
             f32x4 st[Q][4];
             f16x8 f[A + 1];
 #pragma unroll
@@ -1024,7 +1210,7 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
             }
 #pragma unroll
             for (int u = 0; u < A; ++u) f[u] = hi[4 * KC + u][lane];
-            bool all = !X;
+            bool all = true;
 #pragma unroll
             for (int i = 0; i < T::NB; ++i)
                 all = all && cur.place(i * T::GS) >= wspan.all_lo && cur.place(i * T::GS) + T::GS * 16 - 1 <= wspan.all_hi;
@@ -1033,10 +1219,27 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
             for (int i = 0; i < Q; ++i) {
                 const int at = 32 * wave + 16 * i + r;
                 const float fq = row_factor[at];
-                float fk[T::NB];
+                float turn;
+                if constexpr (X) {
+                    const Group of[4] = {group_of(cur, 0), group_of(cur, 1), group_of(cur, 2), group_of(cur, 3)};
+                    // (read from LDS when they are needed, twice: registers are full)
+                    turn = soften_tokens<4>(
+                        of, st[i], [&](int s) { return *reinterpret_cast<const f32x4 *>(&token_factor[16 * s + hidden(4 * g)]) * fq; },
+                        [&](int s) { return *reinterpret_cast<const i32x4 *>(&token_exponent[16 * s + hidden(4 * g)]); },
+                        row_lo[at], row_hi[at], g, w[i]);
 #pragma unroll
-                for (int b = 0; b < T::NB; ++b) fk[b] = cur.key_factor(b) * fq;
-                const float turn = soften<B>(cur, st[i], fk, all, row_lo + at, row_hi + at, g, w[i], ph[i], pl[i]);
+                    for (int c = 0; c < 2; ++c) {
+                        float p[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) p[e] = st[i][2 * c + e / 4][e % 4];
+                        pairs8(p, ph[i][c], pl[i][c]);
+                    }
+                } else {
+                    float fk[T::NB];
+#pragma unroll
+                    for (int b = 0; b < T::NB; ++b) fk[b] = cur.key_factor(b) * fq;
+                    turn = soften<B>(cur, st[i], fk, all, row_lo + at, row_hi + at, g, w[i], ph[i], pl[i]);
+                }
                 if (__ballot(turn != 1.0f)) {
 #pragma unroll
                     for (int n = 0; n < N; ++n) o[i][n] *= turn;
@@ -1095,6 +1298,31 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
             keep_pairs(cur, 0);
             __syncthreads();
             if (sees(kt)) compute(std::true_type());
+            if (__builtin_expect(uniform(odd[0] | odd[1] | odd[2] | odd[3]), 0)) {   // (the workgroup's)
+                __syncthreads();
+                keep_odd(cur, 0);
+                __syncthreads();
+                if (sees(kt)) {
+#pragma unroll
+                    for (int i = 0; i < Q; ++i) {
+                        const int at = 32 * wave + 16 * i + r;
+                        f32x4 seen[4];
+#pragma unroll
+                        for (int s = 0; s < 4; ++s) {
+                            bool is[4];
+                            sees_tokens(group_of(cur, s), row_lo[at], row_hi[at], g, is);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) seen[s][e] = is[e] ? 1.0f : 0.0f;
+                        }
+                        const f16x8 s0 = to_f16(seen[0], seen[1]), s1 = to_f16(seen[2], seen[3]);
+#pragma unroll
+                        for (int n = 0; n < N; ++n) {
+                            const f32x4 x = mfma16(frag[0][4 * KC + 2 * n][lane], s0, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+                            spoil(o[i][n], mfma16(frag[0][4 * KC + 2 * n + 1][lane], s1, x));
+                        }
+                    }
+                }
+            }
         }
     }
 
