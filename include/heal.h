@@ -450,8 +450,16 @@ heal_status_t heal_kv_select(const heal_kv_cache_t *cache, const heal_kv_batch_t
  * causal = 0) and, with window > 0 (causal = 1 only), t > place - window.  A row that sees nothing
  * gives o = 0 and lse = -infinity.  Codes are exact in FP16; queries and softmax
  * weights go to the matrix units as FP16 pairs (head and residual, scaled by powers
- * of two, off by at most 2^-22 of the value), FP32 rows of the cache likewise, all
- * sums in FP32: the output has FP32's accuracy, not FP16's.
+ * of two), FP32 rows of the cache likewise, all sums in FP32.  A pair is off by 2^-22 of
+ * the value, or, where that is less, by
+ *     an element of a query or of an FP32 key row   2^-38 of the row's largest,
+ *     an element of an FP32 value row               2^-31 of the row's largest,
+ *     a weight with its block's or row's values     2^-38 V,
+ * V being the largest value of the complete blocks and FP32 rows that the output's row
+ * sees.  So an output is FP32's in accuracy, not FP16's, in relation to V: beside the
+ * relative errors it may be off by (2^-31 + 2^-38 n) V with n tokens seen, which is more
+ * than FP32's last place only where the sum of p |v| is below (2^-7 + 2^-14 n) V, as in a
+ * column far smaller than the others.  Rows with scores of 2^30 or more may be no numbers.
  *   sel  : NULL, or [tokens][heads][n_sel] int32, dense: only these blocks of the
  *          sequence are read for a token and head (a block listed twice counts
  *          twice; numbers outside the table hold nothing);
