@@ -246,7 +246,7 @@ bool kv_attention_sizes(const heal_kv_cache_t *c, const heal_kv_batch_t *b, int6
 {
     const int64_t lim = ((int64_t)1 << 31) - 1;
     if (!kv_cache_sizes(c) || !kv_batch_sizes(c, b) || !kv_group(c, heads_q)) return false;
-    if (window < 0 || window > lim || n_sel < 0 || n_sel * c->block > lim || chunk < 0 || chunk % 64 != 0 ||
+    if (window < 0 || window > lim || n_sel < 0 || n_sel > lim / c->block || chunk < 0 || chunk % 64 != 0 ||
         chunk > lim)
         return false;
     if (b->tokens * (heads_q / c->heads) > lim - 128) return false;   // rows are counted in 32 bits
