@@ -189,7 +189,8 @@ bool kv_apart(int64_t tokens, int64_t heads, int64_t dim, int64_t token, int64_t
     if (!kv_stride(token) || !kv_stride(head)) return false;
     if ((tokens > 1 && token < dim) || (heads > 1 && head < dim)) return false;
     if (tokens <= 1 || heads <= 1) return true;
-    return token >= (heads - 1) * head + dim || head >= (tokens - 1) * token + dim;
+    // (tokens times their stride may need 70 bits)
+    return token >= (heads - 1) * head + dim || (head - dim) / token >= tokens - 1;
 }
 
 bool kv_cache_sizes(const heal_kv_cache_t *c)
