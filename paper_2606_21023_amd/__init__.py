@@ -438,7 +438,9 @@ class KVCache:
       v_recent float32 (slots, heads, dim, 2 * block)
 
     dim is 64, 96 or 128, block 16, 32, 64 or 128 tokens.  The arrays are the
-    caller's: contiguous CUDA tensors of one device, kept as attributes.
+    caller's: contiguous CUDA tensors of one device, kept as attributes.  Their
+    addresses are taken once, so the attributes cannot be set and a tensor must not get
+    other memory (``set_``, ``resize_``, ``data``); other arrays are another KVCache.
     """
 
     def __init__(self, k_codes, v_codes, scales, k_mean, k_recent, v_recent):
@@ -463,13 +465,16 @@ class KVCache:
         if dim not in (64, 96, 128) or block not in (16, 32, 64, 128) or not (blocks and slots and heads):
             raise HealError("no cache of %d blocks, %d slots, %d heads, dim %d, block %d"
                             % (blocks, slots, heads, dim, block))
-        self.__dict__.update(arrays)
-        self.blocks, self.slots, self.heads, self.dim, self.block = blocks, slots, heads, dim, block
-        self.device = k_codes.device
-        self._index = k_codes.get_device()
-        self._f32, self._i32 = torch.float32, torch.int32
-        self._c = _CCache(blocks, slots, heads, dim, block, *(t.data_ptr() for t in arrays.values()))
-        self._ref = ctypes.byref(self._c)
+        c = _CCache(blocks, slots, heads, dim, block, *(t.data_ptr() for t in arrays.values()))
+        self.__dict__.update(arrays, blocks=blocks, slots=slots, heads=heads, dim=dim, block=block,
+                             device=k_codes.device, _index=k_codes.get_device(), _f32=torch.float32,
+                             _i32=torch.int32, _c=c, _ref=ctypes.byref(c))
+
+    def __setattr__(self, name, value):
+        raise HealError("a KVCache keeps the addresses of its arrays: make another one to change %s" % name)
+
+    def __delattr__(self, name):
+        raise HealError("a KVCache keeps the addresses of its arrays: %s stays" % name)
 
     @classmethod
     def empty(cls, blocks, slots, heads, dim, block=64, device="cuda"):
