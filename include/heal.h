@@ -429,8 +429,8 @@ heal_status_t heal_kv_read(const heal_kv_cache_t *cache, const heal_kv_batch_t *
  * the first keep_first and the last keep_last blocks up to the token's own, and of
  * the others those that score highest,
  *     score(b) = max over the head's queries of  sum_d q_d k_mean[b]_d   (FP64),
- * equal scores by the lower block; a score that is no number, or that belongs to a
- * block that the cache does not hold, is -infinity.
+ * equal scores by the lower block; a sum that is no number is left out, and a block
+ * without any other, or that the cache does not hold, scores -infinity.
  *   q   : [tokens][heads_q][dim], heads_q a multiple of heads: head h has the queries
  *         h * heads_q / heads and on;
  *   sel : [tokens][heads][n_sel] int32, dense: block numbers of the sequence,
