@@ -395,8 +395,7 @@ __device__ __forceinline__ Group group_of(const Blocks<B> &b, int64_t kt, int s)
 // s, the D/4 bytes of row r that belong to lanes g; of row 16 n + r of V^T, the four
 // bytes of each group that do.  (The block's address is the wave's, the lane's part an
 // unsigned 32-bit offset, hidden so that the two are not added outside the loop: no
-// 64-bit address per lane.)  ONCE: nobody else reads them, so they pass the caches by
-// (a decode step of 64 sequences 162 us, 179 with ordinary loads).
+// 64-bit address per lane.)  ONCE: they pass the caches by.
 template <bool ONCE, class X>
 __device__ __forceinline__ X load_codes(const int8_t *p)
 {
@@ -1400,10 +1399,17 @@ template <int D, int B>
 hipError_t attention_sized(KvAttnArgs &a, const KvPlan &plan, hipStream_t stream)
 {
     const int64_t n = plan.tiles * a.c.heads * plan.parts;
+    // Loads pass the caches by where a sequence has one token, whose queries fit one row tile:
+    // nobody else reads its blocks then, unless sequences share them (64 tokens over 4096 to
+    // 8192: 141 us, 152 with ordinary loads; 32 tokens with lists of 48 of 500 blocks 49, 54;
+    // with half of their 64 blocks shared by 64 sequences 78, 82, with 64 of 68 69, 66).  Not in
+    // ragged calls with lists, where tokens of a sequence list the same blocks (777 tokens, 16 of
+    // 79 blocks: 231 us so, 215 with ordinary loads; four drafts of 32 sequences, 48 of 500
+    // blocks, the same for all four 109, 100, lists of their own 134, 133).
     hipError_t err = in_parts(n, [&](int64_t at, unsigned m) {
         if (plan.wide)
             hipLaunchKernelGGL((kv_prompt_kernel<D, B>), dim3(m), dim3(256), 0, stream, a, plan.tiles, at);
-        else if (plan.by_token && a.group <= 16)
+        else if (plan.by_token && !a.b.cu && a.group <= 16)
             hipLaunchKernelGGL((kv_attention_kernel<D, B, true>), dim3(m), dim3(256), 0, stream, a, true, at);
         else
             hipLaunchKernelGGL((kv_attention_kernel<D, B, false>), dim3(m), dim3(256), 0, stream, a, plan.by_token, at);
