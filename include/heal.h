@@ -334,7 +334,8 @@ heal_status_t heal_scores_i16(int64_t M, int64_t N, int64_t K, const int16_t *Q,
  * the ring's rows, once.  The cache therefore does not depend on how tokens were cut
  * into calls, and a sequence may be cut back (drafted tokens that were refused) by
  * passing a smaller length: as far as the beginning of the block before the last one
- * that it has reached, whose rows the ring still has.
+ * that it has reached, whose rows the ring still has, but not into blocks that were
+ * appended with another slot, such as a beginning that it shares.
  *
  * Arrays (device, 16-byte aligned, owned by the caller, dense):
  *   k_codes  [blocks][heads][block][dim]
@@ -468,7 +469,9 @@ heal_status_t heal_kv_select(const heal_kv_cache_t *cache, const heal_kv_batch_t
  *   lse  : [tokens][heads_q] dense, or NULL;
  *   chunk: 0, or a multiple of 64: each row's tokens are summed in chunks of so many
  *          from the first one it can see, joined in ascending order.  0 chooses by the
- *          call's sizes, so that a row's bits may depend on the batch it is in; with a
+ *          call's sizes, so that a row's bits may depend on the batch it is in, and the
+ *          time on table_cols: the lengths are not known to the host, so a table's width
+ *          is best that of the longest sequence in the call; with a
  *          chunk of the caller's they depend on the row's own data only (in calls of
  *          one token per sequence, with cu NULL, or with sel).  Results are bitwise
  *          the same from run to run either way;

@@ -1043,8 +1043,8 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
 // wait in LDS in the order of the matrix operands (lane by lane, no bank conflicts).
 // A key fragment feeds four matrix instructions (two groups of 16 rows, two parts of
 // the pair) and a value fragment likewise.  Bound by instruction issue: the matrix
-// units are busy 44% of the time, the vector units (exponentials, pairs, masks) 53%
-// (512 tokens of 32 heads over 16001: 264 GFLOP of FP16 products in 255 us, 1.04 PFLOP/s).
+// units are busy 44% of the time, the vector units (exponentials, pairs, masks) 50%
+// (512 tokens of 32 heads over 16001: 264 GFLOP of FP16 products in 253 us, 1.04 PFLOP/s).
 template <int D, int B>
 __global__ void __launch_bounds__(256, 2)
 kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
@@ -1435,7 +1435,9 @@ void cut(KvPlan &p, int64_t tokens, int64_t seqs, int heads, int group, int bloc
     const int64_t each = seqs > 0 ? (tokens * group + seqs * R - 1) / (seqs * R) : 0;
     const int64_t real = p.by_token || seqs * each > p.tiles ? p.tiles : seqs * each;
     p.wgs = real * heads > 0 ? real * heads : 1;
-    // 64-token tiles that a row tile can have to read (its rows' windows begin at up to R places)
+    // 64-token tiles that a row tile can have to read (its rows' windows begin at up to R places).
+    // Lengths are on the device: a table wider than they are leaves the last parts without
+    // work (one token over 8191: 20 us with 128 columns, 45 with 2048)
     int64_t places = n_sel > 0 ? n_sel * block : cols * block;
     if (n_sel == 0 && window > 0 && window + R + 63 < places) places = window + R + 63;
     const int64_t span = (places + 63) / 64 > 0 ? (places + 63) / 64 : 1;
