@@ -460,7 +460,9 @@ heal_status_t heal_kv_select(const heal_kv_cache_t *cache, const heal_kv_batch_t
  * sees.  So an output is FP32's in accuracy, not FP16's, in relation to V: beside the
  * relative errors it may be off by (2^-31 + 2^-38 n) V with n tokens seen, which is more
  * than FP32's last place only where the sum of p |v| is below (2^-7 + 2^-14 n) V, as in a
- * column far smaller than the others.  Rows with scores of 2^30 or more may be no numbers.
+ * column far smaller than the others (and by 2^-146, in FP32's subnormal range).  Rows with
+ * scores of 2^30 or more may be no numbers, and scores of query rows or keys that are below
+ * 2^-100 throughout have fewer digits (which shows beside keys or queries above 2^100).
  *   sel  : NULL, or [tokens][heads][n_sel] int32, dense: only these blocks of the
  *          sequence are read for a token and head (a block listed twice counts
  *          twice; numbers outside the table hold nothing);

@@ -788,10 +788,13 @@ __device__ __forceinline__ float soften_tokens(const Group *t, f32x4 *st, F fact
     return turn;
 }
 
-// The factor of a finished output.
-__device__ __forceinline__ float unit_of(int ref)
+// Four columns of a finished output out of its units.  (In two steps: the units of values
+// below 2^-105 would be an FP32 number below 2^-126, which has few digits, or 0.)
+__device__ __forceinline__ f32x4 from_units(f32x4 o, int ref)
 {
-    return ref == kNoScale ? 0.0f : ldexpf(1.0f / 127.0f, ref - 14);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = ldexpf(o[i] * (1.0f / 127.0f), ref - 14);
+    return o;
 }
 
 // Attention of 16 rows by the four waves of a workgroup, each on 64-token tiles of
@@ -1007,9 +1010,9 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
     }
 
     // join the waves
-    const float sum = sum_over_groups(w.l), unit = unit_of(w.ref);
+    const float sum = sum_over_groups(w.l);
 #pragma unroll
-    for (int n = 0; n < N; ++n) *reinterpret_cast<f32x4 *>(&part_o[wave][r][16 * n + 4 * g]) = o[n] * unit;
+    for (int n = 0; n < N; ++n) *reinterpret_cast<f32x4 *>(&part_o[wave][r][16 * n + 4 * g]) = from_units(o[n], w.ref);
     if (g == 0) {
         part_m[wave][r] = w.m;
         part_l[wave][r] = sum;
@@ -1327,14 +1330,14 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
 
 #pragma unroll
     for (int i = 0; i < Q; ++i) {
-        const float sum = sum_over_groups(w[i].l), unit = unit_of(w[i].ref);
+        const float sum = sum_over_groups(w[i].l);
         const int at = 32 * wave + 16 * i + hidden(r), row = t.row0 + at;
         if (at >= t.rows) continue;
         const Place to_row = place_of(a, t.s.first + row / a.group, head * a.group + row % a.group, part);
         if (g == 0) to_row.sums(a, w[i].m, sum);
         if (a.parts > 1 && sum == 0.0f) continue;
 #pragma unroll
-        for (int n = 0; n < N; ++n) to_row.store(a, 16 * n + 4 * g, o[i][n] * unit, sum);
+        for (int n = 0; n < N; ++n) to_row.store(a, 16 * n + 4 * g, from_units(o[i][n], w[i].ref), sum);
     }
 }
 
