@@ -466,9 +466,8 @@ struct Codes {
     }
 };
 
-// Keys of a group, as FP16 pairs: f(k, hi, lo)
-// for each chunk of 32 elements.  Returns the factor of the scores with token r, but for
-// the query's.
+// Keys of a group, as FP16 pairs: f(k, hi, lo) for each chunk of 32 elements.  Returns the
+// factor of the scores with token r, but for the query's.
 template <int D, int B, class F>
 __device__ __forceinline__ float keys_of_group(const KvAttnArgs &a, const Group &t, int slot, int head,
                                                int64_t len, int r, int g, F f)
@@ -654,9 +653,9 @@ struct Soft {
 };
 
 // The scores of a tile whose blocks are all coded become weights.  st: the lane's scores, of
-// tokens 4 g + i of group s, before their factors fk (one for each block).  Returns the weights times the
-// blocks' value factors as FP16 pairs, in the order of the values' operand, and
-// what the output so far is to be multiplied by.
+// tokens 4 g + i of group s, before their factors fk (one for each block).  Returns the
+// weights times the blocks' value factors as FP16 pairs, in the order of the values'
+// operand, and what the output so far is to be multiplied by.
 template <int B>
 __device__ __forceinline__ float soften(const Tile<B> &t, f32x4 *st, const float *fk, bool all, const int32_t *row_lo,
                                         const int32_t *row_hi, int g, Soft &w, f16x8 *ph, f16x8 *pl)
@@ -739,7 +738,18 @@ __device__ __forceinline__ void sees_tokens(const Group &t, int32_t lo, int32_t 
     for (int e = 0; e < 4; ++e) is[e] = t.blk >= 0 && p0 + e >= lo && p0 + e <= hi;
 }
 
-// ... of a tile that may hold FP32 rows: N groups, factors(s) and exponents(s) being the
+// ... as 1 and 0.
+__device__ __forceinline__ f32x4 seen_tokens(const Group &t, int32_t lo, int32_t hi, int g)
+{
+    bool is[4];
+    sees_tokens(t, lo, hi, g, is);
+    f32x4 x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = is[e] ? 1.0f : 0.0f;
+    return x;
+}
+
+// As soften, of a tile that may hold FP32 rows: N groups, factors(s) and exponents(s) being the
 // factors and the values' exponents of the lane's tokens of group s; the tokens that the row
 // sees make its units.  Leaves the weights in st.
 template <int N, class F, class E>
@@ -977,12 +987,12 @@ kv_attention_kernel(KvAttnArgs a, bool by_token, int64_t wg0)
         if (__builtin_expect(odd, false)) {   // (the wave's)
             const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
             const int r2 = hidden(r), g2 = hidden(g);
-            bool is[4];
-            sees_tokens(own, row_lo[r2], row_hi[r2], g2, is);
-            const f16x8 seen = to_f16(f32x4{is[0] ? 1.0f : 0.0f, is[1] ? 1.0f : 0.0f, is[2] ? 1.0f : 0.0f, is[3] ? 1.0f : 0.0f}, none);
+            const f16x8 seen = to_f16(seen_tokens(own, row_lo[r2], row_hi[r2], g2), none);
 #pragma unroll
-            for (int n = 0; n < N; ++n)
-                spoil(o[n], mfma16(to_f16(odd_values(values_of_group<D, B>(a, own, n, slot, head, t.s.len, r2, g2)), none), seen, none));
+            for (int n = 0; n < N; ++n) {
+                const f32x4 y = values_of_group<D, B>(a, own, n, slot, head, t.s.len, r2, g2);
+                spoil(o[n], mfma16(to_f16(odd_values(y), none), seen, none));
+            }
         }
     };
     if (t.s.len % B != 0 && span.last >= span.first) {
@@ -1225,10 +1235,13 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
                 if constexpr (X) {
                     const Group of[4] = {group_of(cur, 0), group_of(cur, 1), group_of(cur, 2), group_of(cur, 3)};
                     // (read from LDS when they are needed, twice: registers are full)
-                    turn = soften_tokens<4>(
-                        of, st[i], [&](int s) { return *reinterpret_cast<const f32x4 *>(&token_factor[16 * s + hidden(4 * g)]) * fq; },
-                        [&](int s) { return *reinterpret_cast<const i32x4 *>(&token_exponent[16 * s + hidden(4 * g)]); },
-                        row_lo[at], row_hi[at], g, w[i]);
+                    auto factors = [&](int s) HEAL_INLINE {
+                        return *reinterpret_cast<const f32x4 *>(&token_factor[16 * s + hidden(4 * g)]) * fq;
+                    };
+                    auto exponents = [&](int s) HEAL_INLINE {
+                        return *reinterpret_cast<const i32x4 *>(&token_exponent[16 * s + hidden(4 * g)]);
+                    };
+                    turn = soften_tokens<4>(of, st[i], factors, exponents, row_lo[at], row_hi[at], g, w[i]);
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         float p[8];
@@ -1310,12 +1323,7 @@ kv_prompt_kernel(KvAttnArgs a, int64_t tiles, int64_t wg0)
                         const int at = 32 * wave + 16 * i + r;
                         f32x4 seen[4];
 #pragma unroll
-                        for (int s = 0; s < 4; ++s) {
-                            bool is[4];
-                            sees_tokens(group_of(cur, s), row_lo[at], row_hi[at], g, is);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) seen[s][e] = is[e] ? 1.0f : 0.0f;
-                        }
+                        for (int s = 0; s < 4; ++s) seen[s] = seen_tokens(group_of(cur, s), row_lo[at], row_hi[at], g);
                         const f16x8 s0 = to_f16(seen[0], seen[1]), s1 = to_f16(seen[2], seen[3]);
 #pragma unroll
                         for (int n = 0; n < N; ++n) {
