@@ -25,6 +25,15 @@ Functions (names follow the C ABI):
   heal_kv_read(cache, tokens, table, lens, ...)  -> (k, v) rows of the cache as FP32
   heal_kv_select(cache, q, n_sel, table, lens, ...)  -> the blocks that each token should read
   heal_kv_attention(cache, q, table, lens, ...)  -> attention over the cache, FP32
+  KVPool(refs, block), KVPool.empty(...)  -> who holds which blocks of a cache
+  heal_kv_release(pool, table, lens)  -> sequences give blocks up
+  heal_kv_fork(pool, table, lens, parents, children)  -> sequences that share their beginning
+  heal_kv_reserve(pool, tokens, table, lens, cu)  -> blocks of their own for tokens to append
+  heal_kv_compact(pool, table)        -> held blocks first; (src, dst, count) of the moves
+  heal_kv_copy(cache, blocks, slots)  -> blocks and slots copied by lists
+  heal_block_norm(h, x, post, gate, scale, pre, ...)  -> (h + scale gate N(x), its norm), FP32
+  LoraBank(a, b, ranks, scales)       -> the adapters of a projection
+  heal_lora_add(y, x, bank, ids, cu)  -> y + s B (A x), each token with its request's adapter
   lib()                               -> the raw ctypes library
   build_id(), check_build()           -> the library's source hash; refuse a stale binary
 """
@@ -37,7 +46,8 @@ __all__ = ["HealError", "lib", "library_path", "build_id", "check_build", "heal_
            "heal_split_f16", "heal_packed_size", "heal_maxabs_f32", "heal_f16_weight_exponent",
            "heal_pack_f16_weight", "heal_gemm_f16w", "heal_presplit_b", "heal_gemm_f32_presplit",
            "heal_quantize_i16", "heal_scores_i16", "KVCache", "heal_kv_append", "heal_kv_read",
-           "heal_kv_select", "heal_kv_attention"]
+           "heal_kv_select", "heal_kv_attention", "KVPool", "heal_kv_release", "heal_kv_fork", "heal_kv_reserve",
+           "heal_kv_compact", "heal_kv_copy", "heal_block_norm", "LoraBank", "heal_lora_add"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 library_path = os.path.join(_HERE, "libheal.so")
@@ -130,6 +140,27 @@ def lib():
     L.heal_kv_attention_workspace.restype = _i64
     L.heal_kv_attention_tile.argtypes = L.heal_kv_attention_workspace.argtypes
     L.heal_kv_attention_tile.restype = _c
+    L.heal_kv_release.argtypes = [_vp, _i64, _vp, _vp, _i64, _i64, _vp]
+    L.heal_kv_release.restype = _c
+    L.heal_kv_fork.argtypes = [_vp, _i64, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp]
+    L.heal_kv_fork.restype = _c
+    L.heal_kv_reserve.argtypes = [_vp, _vp, _vp, _i64, _i64, _vp, _vp, _i64, _vp]
+    L.heal_kv_reserve.restype = _c
+    L.heal_kv_reserve_workspace.argtypes = [_vp, _vp]
+    L.heal_kv_reserve_workspace.restype = _i64
+    L.heal_kv_compact.argtypes = [_vp, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _i64, _vp]
+    L.heal_kv_compact.restype = _c
+    L.heal_kv_compact_workspace.argtypes = [_vp]
+    L.heal_kv_compact_workspace.restype = _i64
+    L.heal_kv_copy.argtypes = [_vp, _i64, _vp, _vp, _vp, _i64, _vp, _vp, _vp]
+    L.heal_kv_copy.restype = _c
+    L.heal_block_norm.argtypes = [_i64] * 3 + [_vp, _i64, _i64] * 2 + [_vp, _vp, _i64, _i64, _i64, ctypes.c_float,
+                                                                      _vp] + [_vp, _i64, _i64] * 2 + [_vp]
+    L.heal_block_norm.restype = _c
+    L.heal_lora_add.argtypes = [_vp, _i64, _i64, _vp, _vp] + [_vp, _i64] * 3 + [_vp, _i64, _vp]
+    L.heal_lora_add.restype = _c
+    L.heal_lora_workspace.argtypes = [_vp, _i64]
+    L.heal_lora_workspace.restype = _i64
     _lib = L
     return L
 
@@ -721,4 +752,311 @@ def heal_kv_attention(cache, q, table, lens, cu=None, slots=None, scale=None, ca
         window, sel.data_ptr() if n_sel else None, n_sel, out.data_ptr(), out_token, out_head,
         lse.data_ptr() if lse is not None else None, chunk, space.data_ptr() if size > 0 else None,
         max(size, 0), _stream()), "heal_kv_attention")
+    return out
+
+# ---- pages of a cache ----------------------------------------------------------
+
+class _CPool(ctypes.Structure):
+    _fields_ = [("blocks", _i64), ("block", _i64), ("refs", _vp)]
+
+
+class KVPool:
+    """Who holds which block of a cache (or of one for each layer): refs, a contiguous
+    int32 CUDA vector with the number of table entries that hold each block, 0 where
+    it is free; block: tokens of a block.  Its address is taken once, as a KVCache takes
+    those of its arrays."""
+
+    def __init__(self, refs, block):
+        (blocks,), _ = _tensor(refs, "refs", torch.int32, 1)
+        if block not in (16, 32, 64, 128) or not 1 <= blocks <= 1 << 30:
+            raise HealError("no pool of %d blocks of %s tokens" % (blocks, block))
+        c = _CPool(blocks, block, refs.data_ptr())
+        self.__dict__.update(refs=refs, blocks=blocks, block=block, device=refs.device, _index=refs.get_device(),
+                             _i32=torch.int32, _c=c, _ref=ctypes.byref(c))
+
+    def __setattr__(self, name, value):
+        raise HealError("a KVPool keeps the address of its counts: make another one to change %s" % name)
+
+    def __delattr__(self, name):
+        raise HealError("a KVPool keeps the address of its counts: %s stays" % name)
+
+    @classmethod
+    def empty(cls, blocks, block=64, device="cuda"):
+        """A pool of its own, all blocks free."""
+        return cls(torch.zeros(blocks, dtype=torch.int32, device=device), block)
+
+
+def _kv_pool(pool, table):
+    """Checks pool and table; returns rows, row stride, columns."""
+    if not isinstance(pool, KVPool):
+        raise HealError("pool must be a KVPool")
+    if _device() != pool._index:
+        raise HealError("the pool is on %s, the current device is another" % pool.device)
+    try:
+        shape, stride = table.shape, table.stride()
+        if not (table.dtype is pool._i32 and table.get_device() == pool._index and len(shape) == 2
+                and (stride[1] == 1 or shape[1] <= 1)):
+            shape = None
+    except AttributeError:
+        shape = None
+    if shape is None:
+        shape, stride = _kv_ints(pool, table, "table", 2)
+    rows, cols = shape
+    return rows, stride[0] if rows > 1 else cols or 1, cols
+
+
+def _kv_scratch(pool, size):
+    """size bytes of workspace beside the pool, or None."""
+    return torch.empty((size + 3) // 4, dtype=torch.int32, device=pool.device) if size > 0 else None
+
+
+def heal_kv_release(pool, table, lens):
+    """Rows of table (rows, columns) int32 are cut back to lens (rows) int32 tokens: the
+    entries behind give their blocks up and become -1 (0 frees a row)."""
+    rows, ld, cols = _kv_pool(pool, table)
+    _check((_lib or lib()).heal_kv_release(pool._ref, rows, _kv_list(pool, lens, "lens", rows), table.data_ptr(),
+                                           ld, cols, _stream()), "heal_kv_release")
+
+
+def heal_kv_fork(pool, table, lens, parents, children):
+    """Rows children[j] of table become copies of rows parents[j], whose blocks (as many as
+    lens says) are then held once more; what the children held is given up.  A pair
+    whose child is a parent too, or the child of an earlier pair, is left out."""
+    rows, ld, cols = _kv_pool(pool, table)
+    at = _kv_list(pool, lens, "lens", rows)
+    pairs = len(parents)
+    _check((_lib or lib()).heal_kv_fork(
+        pool._ref, rows, at, table.data_ptr(), ld, cols, pairs, _kv_list(pool, parents, "parents", pairs),
+        _kv_list(pool, children, "children", pairs), _stream()), "heal_kv_fork")
+
+
+def heal_kv_reserve(pool, tokens, table, lens, cu=None, missing=None):
+    """Before ``heal_kv_append`` of `tokens` tokens with the same table, lens and cu: every block
+    that they touch becomes its sequence's own.  Returns missing, an int32 (1) on the device: the
+    number of blocks that the pool lacked, in which case nothing is changed, or 0."""
+    rows, ld, cols = _kv_pool(pool, table)
+    if cu is not None:
+        cu = _kv_list(pool, cu, "cu", rows + 1)
+    elif tokens != rows:
+        raise HealError("%d tokens of %d sequences need cu" % (tokens, rows))
+    if missing is None:
+        missing = torch.empty(1, dtype=torch.int32, device=pool.device)
+    batch = _CBatch(rows, tokens, cu, _kv_list(pool, lens, "lens", rows), None, 1, 0, None)
+    ref, L = ctypes.byref(batch), _lib or lib()
+    size = L.heal_kv_reserve_workspace(pool._ref, ref)
+    space = _kv_scratch(pool, size)
+    _check(L.heal_kv_reserve(pool._ref, ref, table.data_ptr(), ld, cols, _kv_list(pool, missing, "missing", 1),
+                             space.data_ptr() if space is not None else None, max(size, 0), _stream()),
+           "heal_kv_reserve")
+    return missing
+
+
+def heal_kv_compact(pool, table, src=None, dst=None, count=None):
+    """The held blocks become the first ones of the pool; table (all of the program's
+    rows) and refs follow.  Returns (src, dst, count) for ``heal_kv_copy``: int32 (blocks // 2),
+    -1 behind the moves, and their number (1)."""
+    rows, ld, cols = _kv_pool(pool, table)
+    most = pool.blocks // 2
+
+    def ints(t, name, n):
+        if t is None:
+            t = torch.empty(n, dtype=torch.int32, device=pool.device)
+        return t, _kv_list(pool, t, name, n)
+    src, at_src = ints(src, "src", most)
+    dst, at_dst = ints(dst, "dst", most)
+    count, at_count = ints(count, "count", 1)
+    L = _lib or lib()
+    size = L.heal_kv_compact_workspace(pool._ref)
+    space = _kv_scratch(pool, size)
+    _check(L.heal_kv_compact(pool._ref, rows, table.data_ptr(), ld, cols, at_src if most else None,
+                             at_dst if most else None, at_count, space.data_ptr(), size, _stream()),
+           "heal_kv_compact")
+    return src, dst, count
+
+
+def heal_kv_copy(cache, blocks=None, slots=None, count=None):
+    """Copies blocks (codes, scales, means) and slots (FP32 rows) of a cache: blocks = (src,
+    dst), slots = (src, dst), int32 vectors; count: None, or an int32 (1), how many of the
+    pairs of blocks.  No destination twice, nor a source as destination."""
+    if not isinstance(cache, KVCache):
+        raise HealError("cache must be a KVCache")
+    if _device() != cache._index:
+        raise HealError("the cache is on %s, the current device is another" % cache.device)
+
+    def pairs(lists, name):
+        if lists is None:
+            return 0, None, None
+        src, dst = lists
+        n = len(src)
+        return n, _kv_list(cache, src, name + "[0]", n), _kv_list(cache, dst, name + "[1]", n)
+    n_blocks, b_src, b_dst = pairs(blocks, "blocks")
+    n_slots, s_src, s_dst = pairs(slots, "slots")
+    if count is not None:
+        if blocks is None:
+            raise HealError("count without blocks")
+        count = _kv_list(cache, count, "count", 1)
+    _check((_lib or lib()).heal_kv_copy(cache._ref, n_blocks, b_src, b_dst, count, n_slots, s_src, s_dst, _stream()),
+           "heal_kv_copy")
+
+
+# ---- the residual stream, adapters ------------------------------------------------
+
+class _CNorm(ctypes.Structure):
+    _fields_ = [("weight", _vp), ("bias", _vp), ("eps", ctypes.c_float), ("centred", ctypes.c_int)]
+
+
+class _CBank(ctypes.Structure):
+    _fields_ = [("adapters", _i64), ("rank", _i64), ("K", _i64), ("N", _i64), ("type", ctypes.c_int), ("a", _vp),
+                ("b", _vp), ("ranks", _vp), ("scales", _vp)]
+
+
+def _norm_rows(t, name, shape, index):
+    """A float32 tensor of that shape (2-D or 3-D); its address and two strides."""
+    got, stride = _tensor(t, name, torch.float32, len(shape))
+    if got != shape:
+        raise HealError("%s has shape %s, expected %s" % (name, tuple(got), tuple(shape)))
+    if t.get_device() != index:
+        raise HealError("%s is on %s, h on another device" % (name, t.device))
+    return t.data_ptr(), stride[0], stride[1] if len(shape) == 3 else 0
+
+
+def _norm_vector(t, name, dim, index):
+    if t is None:
+        return None
+    (n,), _ = _tensor(t, name, torch.float32, 1)
+    if n != dim or t.get_device() != index:
+        raise HealError("%s must be a vector of %d beside h" % (name, dim))
+    return t.data_ptr()
+
+
+def _norm_spec(weight, bias, name, dim, index, eps, centred):
+    if weight is None:
+        if bias is not None:
+            raise HealError("%s_bias without %s" % (name, name))
+        return None
+    return ctypes.byref(_CNorm(_norm_vector(weight, name, dim, index), _norm_vector(bias, name + "_bias", dim, index),
+                               eps, 1 if centred else 0))
+
+
+def heal_block_norm(h, x=None, post=None, gate=None, scale=1.0, pre=None, eps=1e-6, centred=False, post_bias=None,
+                    pre_bias=None, h_out=None, out=None):
+    """(h', out): h' = h + scale * gate * N(x; post) and out = N(h'; pre), as
+    ``include/heal.h`` writes them.
+
+    h: float32 (tokens, dim) or (tokens, heads, dim); x the same, or None: then h' is h
+    itself.  post, pre: weights (dim) of the norms, or None for no norm there (without
+    pre, out is None).  gate: a float32 tensor that broadcasts to h, its last dimension
+    dense, or None.  centred: norms about the mean, with biases post_bias and pre_bias where they
+    are given.  h_out (which may be h or x) and out (h or x likewise) are new tensors by default.
+    """
+    shape, stride = _tensor(h, "h", torch.float32)
+    if len(shape) not in (2, 3) or shape[-1] < 1:
+        raise HealError("h must be (tokens, dim) or (tokens, heads, dim), got %s" % (tuple(shape),))
+    index, dim = h.get_device(), shape[-1]
+    if _device() != index:
+        raise HealError("h is on %s, the current device is another" % h.device)
+    wide = len(shape) == 3
+    if x is None and (post is not None or gate is not None or h_out is not None):
+        raise HealError("post, gate and h_out need x")
+    if x is None and pre is None:
+        raise HealError("nothing to do: neither x nor pre")
+    x_at = _norm_rows(x, "x", shape, index) if x is not None else (None, 0, 0)
+    g = (None, 0, 0, 0)
+    if gate is not None:
+        got, gs = _tensor(gate, "gate", torch.float32, len(shape))
+        if gate.get_device() != index or any(a != b and a != 1 for a, b in zip(got, shape)):
+            raise HealError("gate %s does not broadcast to h %s" % (tuple(got), tuple(shape)))
+        g = (gate.data_ptr(), gs[0] if got[0] > 1 else 0, gs[1] if wide and got[1] > 1 else 0, 1 if got[-1] > 1 else 0)
+    specs = [_norm_spec(post, post_bias, "post", dim, index, eps, centred),
+             _norm_spec(pre, pre_bias, "pre", dim, index, eps, centred)]
+    ho_at = out_at = (None, 0, 0)
+    if x is not None:
+        if h_out is None:
+            h_out = torch.empty(shape, dtype=torch.float32, device=h.device)
+        ho_at = _norm_rows(h_out, "h_out", shape, index)
+    if pre is not None:
+        if out is None:
+            out = torch.empty(shape, dtype=torch.float32, device=h.device)
+        out_at = _norm_rows(out, "out", shape, index)
+    elif out is not None:
+        raise HealError("out without pre")
+    _check((_lib or lib()).heal_block_norm(
+        shape[0], shape[1] if wide else 1, dim, h.data_ptr(), stride[0], stride[1] if wide else 0, *x_at, specs[0], *g,
+        scale, specs[1], *ho_at, *out_at, _stream()), "heal_block_norm")
+    return (h if x is None else h_out), out
+
+
+class LoraBank:
+    """Low-rank adapters of one projection, for ``heal_lora_add``: a (adapters, rank, K)
+    and b (adapters, N, rank), contiguous CUDA tensors of float32, bfloat16 or float16;
+    ranks int32 (adapters) where some use fewer of the rows of a and columns of b; scales
+    float32 (adapters), 1 by default.  Addresses are taken once, as in a KVCache."""
+
+    def __init__(self, a, b, ranks=None, scales=None):
+        types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+        if not isinstance(a, torch.Tensor) or a.dtype not in types:
+            raise HealError("a must be a float32, bfloat16 or float16 CUDA tensor")
+        (many, rank, K), _ = _tensor(a, "a", a.dtype, 3)
+        (many_b, N, rank_b), _ = _tensor(b, "b", a.dtype, 3)
+        if many_b != many or rank_b != rank or not (many and rank and K and N):
+            raise HealError("a %s and b %s are not (adapters, rank, K) and (adapters, N, rank)"
+                            % (tuple(a.shape), tuple(b.shape)))
+        for name, t, dtype in (("ranks", ranks, torch.int32), ("scales", scales, torch.float32)):
+            if t is not None:
+                (n,), _ = _tensor(t, name, dtype, 1)
+                if n != many:
+                    raise HealError("%s has %d entries for %d adapters" % (name, n, many))
+        for name, t in (("a", a), ("b", b), ("ranks", ranks), ("scales", scales)):
+            if t is None:
+                continue
+            if t.device != a.device:
+                raise HealError("%s is on %s, a on %s" % (name, t.device, a.device))
+            if not t.is_contiguous() or (name in "ab" and t.data_ptr() % 16):
+                raise HealError("%s must be contiguous, a and b 16-byte aligned" % name)
+        c = _CBank(many, rank, K, N, types[a.dtype], a.data_ptr(), b.data_ptr(),
+                   ranks.data_ptr() if ranks is not None else None, scales.data_ptr() if scales is not None else None)
+        self.__dict__.update(a=a, b=b, ranks=ranks, scales=scales, adapters=many, rank=rank, K=K, N=N, device=a.device,
+                             _index=a.get_device(), _i32=torch.int32, _c=c, _ref=ctypes.byref(c))
+
+    def __setattr__(self, name, value):
+        raise HealError("a LoraBank keeps the addresses of its arrays: make another one to change %s" % name)
+
+    def __delattr__(self, name):
+        raise HealError("a LoraBank keeps the addresses of its arrays: %s stays" % name)
+
+
+def heal_lora_add(y, x, bank, ids, cu=None, out=None):
+    """out = y + s B (A x) with the adapter of each token's sequence.
+
+    y (tokens, N), x (tokens, K): float32; ids (sequences) int32, -1 for none; cu
+    (sequences + 1) int32, or None where every token is a sequence.  out may be y, a new
+    tensor by default.
+    """
+    if not isinstance(bank, LoraBank):
+        raise HealError("bank must be a LoraBank")
+    if _device() != bank._index:
+        raise HealError("the adapters are on %s, the current device is another" % bank.device)
+    shape, x_stride = _tensor(x, "x", torch.float32, 2)
+    y_shape, y_stride = _tensor(y, "y", torch.float32, 2)
+    tokens = shape[0]
+    if shape[1] != bank.K or tuple(y_shape) != (tokens, bank.N):
+        raise HealError("x %s and y %s for adapters of %d by %d" % (tuple(shape), tuple(y_shape), bank.K, bank.N))
+    out, o_stride = _output(out, y, (tokens, bank.N))
+    for name, t in (("x", x), ("y", y), ("out", out)):
+        if t.get_device() != bank._index:
+            raise HealError("%s is on %s, the adapters on %s" % (name, t.device, bank.device))
+    seqs = len(ids)
+    ids = _kv_list(bank, ids, "ids", seqs)
+    if cu is not None:
+        cu = _kv_list(bank, cu, "cu", seqs + 1)
+    elif tokens != seqs:
+        raise HealError("%d tokens of %d sequences need cu" % (tokens, seqs))
+    if tokens == 0:
+        return out
+    L = _lib or lib()
+    size = L.heal_lora_workspace(bank._ref, tokens)
+    space = torch.empty((size + 3) // 4, dtype=torch.float32, device=bank.device) if size > 0 else None
+    _check(L.heal_lora_add(bank._ref, tokens, seqs, cu, ids, x.data_ptr(), _ld(shape, x_stride), y.data_ptr(),
+                           _ld(y_shape, y_stride), out.data_ptr(), _ld(y_shape, o_stride),
+                           space.data_ptr() if size > 0 else None, max(size, 0), _stream()), "heal_lora_add")
     return out

@@ -9,6 +9,7 @@
 #include "heal.h"
 #include "heal_internal.h"
 #include "heal_kv.h"
+#include "heal_layer.h"
 
 namespace {
 
@@ -254,6 +255,87 @@ bool kv_attention_sizes(const heal_kv_cache_t *c, const heal_kv_batch_t *b, int6
     *plan = heal::kv_plan(b->tokens, b->seqs, b->cu != nullptr, (int)c->heads, (int)(heads_q / c->heads),
                           (int)c->dim, (int)c->block, b->table_cols, window, n_sel, chunk);
     return plan->bytes >= 0;
+}
+
+// ---- pages of a cache ----------------------------------------------------------
+
+constexpr int64_t kMaxForks = 65536, kMaxPool = (int64_t)1 << 30;
+
+bool kv_pool_sizes(const heal_kv_pool_t *p)
+{
+    return p && p->blocks >= 1 && p->blocks <= kMaxPool && p->refs && aligned4(p->refs) &&
+           (p->block == 16 || p->block == 32 || p->block == 64 || p->block == 128);
+}
+
+bool kv_pages(const heal_kv_pool_t *pool, int64_t rows, const int32_t *lens, int32_t *table, int64_t table_ld,
+              int64_t table_cols, heal::KvPages *p)
+{
+    if (!kv_pool_sizes(pool) || rows < 0 || rows > kMaxSeqs || table_cols < 0 ||
+        table_cols >= ((int64_t)1 << 31) / pool->block || table_ld < (table_cols > 1 ? table_cols : 1) ||
+        table_ld > kMaxStride || !aligned4(lens) || !aligned4(table))
+        return false;
+    if (rows > 0 && (!lens || (table_cols > 0 && !table)) && !(lens == table && table_cols == 0)) return false;
+    *p = heal::KvPages{pool->refs, table, lens, table_ld, (int32_t)pool->blocks, (int32_t)pool->block, (int32_t)rows,
+                       (int32_t)table_cols};
+    return true;
+}
+
+// Work units of heal_kv_reserve, or -1 where its sizes are refused.
+int64_t kv_reserve_units(const heal_kv_pool_t *p, const heal_kv_batch_t *b)
+{
+    if (!kv_pool_sizes(p) || !b || b->seqs < 0 || b->seqs > kMaxSeqs || b->tokens < 0 || b->tokens > kMaxTokens ||
+        (!b->cu && b->tokens != b->seqs))
+        return -1;
+    return heal::kv_units(b->cu != nullptr, b->tokens, b->seqs, (int)p->block);   // below 2^27
+}
+
+bool kv_array(const void *p) { return p && aligned16(p); }
+
+// ---- the residual stream, adapters ------------------------------------------------
+
+constexpr int64_t kMaxNormDim = (int64_t)1 << 24, kMaxLoraTokens = (int64_t)1 << 24;
+
+// rows x heads rows of `cols` floats at these strides (a stride of 0 where there is one).
+struct Rows {
+    const float *at;
+    int64_t rows, heads, cols, row, head;
+};
+
+// (Strides and counts are bounded to 2^40 and 2^31, so extents may need more than 64 bits.)
+__int128 width_of(const Rows &r) { return 4 * ((__int128)(r.heads - 1) * r.head + r.cols); }
+__int128 bytes_of(const Rows &r) { return 4 * (__int128)(r.rows - 1) * r.row + width_of(r); }
+
+// Whether `bytes` bytes at p end before the rows, or begin behind them.
+bool bytes_apart(const void *p, __int128 bytes, const Rows &r)
+{
+    const __int128 a = (__int128)reinterpret_cast<uintptr_t>(p), b = (__int128)reinterpret_cast<uintptr_t>(r.at);
+    return a + bytes <= b || b + bytes_of(r) <= a;
+}
+
+// Whether no element of the one is one of the other: apart as a whole, or in rows
+// of one stride, side by side.
+bool rows_apart(const Rows &a, const Rows &b)
+{
+    if (bytes_apart(a.at, bytes_of(a), b)) return true;
+    if (a.rows != b.rows || a.row != b.row || a.row <= 0) return false;
+    const __int128 stride = 4 * (__int128)a.row;
+    __int128 off = ((__int128)reinterpret_cast<uintptr_t>(b.at) - (__int128)reinterpret_cast<uintptr_t>(a.at)) % stride;
+    if (off < 0) off += stride;
+    return width_of(a) <= off && off + width_of(b) <= stride;
+}
+
+bool norm_fine(const heal_norm_t *n)
+{
+    return !n || (n->weight && aligned4(n->weight) && aligned4(n->bias) && n->eps >= 0.0f && n->eps <= 3.4028235e38f &&
+                  (n->centred == 0 || n->centred == 1));
+}
+
+bool lora_sizes(const heal_lora_bank_t *b, int64_t tokens)
+{
+    const int64_t lim = (int64_t)1 << 24;
+    return b && b->adapters >= 1 && b->adapters < ((int64_t)1 << 31) && b->rank >= 1 && b->rank <= 1024 && b->K >= 1 &&
+           b->K <= lim && b->N >= 1 && b->N <= lim && b->type >= HEAL_FP32 && b->type <= HEAL_FP16 && tokens >= 0 &&
+           tokens <= kMaxLoraTokens;
 }
 
 }  // namespace
@@ -671,6 +753,213 @@ heal_status_t heal_kv_attention(const heal_kv_cache_t *cache, const heal_kv_batc
     a.ws_o = static_cast<float *>(workspace);
     a.ws_ml = a.ws_o + batch->tokens * heads_q * plan.parts * cache->dim;
     return heal::launch_kv_attention(a, plan, stream) == hipSuccess ? HEAL_OK : HEAL_ERR_LAUNCH;
+}
+
+// ---- pages of a cache ----------------------------------------------------------
+
+heal_status_t heal_kv_release(const heal_kv_pool_t *pool, int64_t rows, const int32_t *lens, int32_t *table,
+                              int64_t table_ld, int64_t table_cols, hipStream_t stream)
+{
+    heal::KvPages p;
+    if (!kv_pages(pool, rows, lens, table, table_ld, table_cols, &p)) return HEAL_ERR_INVALID_VALUE;
+    if (rows == 0 || table_cols == 0) return HEAL_OK;
+    const heal_status_t st = check_device();
+    if (st != HEAL_OK) return st;
+    return heal::launch_kv_release(p, stream) == hipSuccess ? HEAL_OK : HEAL_ERR_LAUNCH;
+}
+
+heal_status_t heal_kv_fork(const heal_kv_pool_t *pool, int64_t rows, const int32_t *lens, int32_t *table,
+                           int64_t table_ld, int64_t table_cols, int64_t pairs, const int32_t *parents,
+                           const int32_t *children, hipStream_t stream)
+{
+    heal::KvPages p;
+    if (!kv_pages(pool, rows, lens, table, table_ld, table_cols, &p) || pairs < 0 || pairs > kMaxForks)
+        return HEAL_ERR_INVALID_VALUE;
+    if (rows == 0 || table_cols == 0 || pairs == 0) return HEAL_OK;
+    if (!parents || !children || !aligned4(parents) || !aligned4(children)) return HEAL_ERR_INVALID_VALUE;
+    const heal_status_t st = check_device();
+    if (st != HEAL_OK) return st;
+    return heal::launch_kv_fork(p, (int32_t)pairs, parents, children, stream) == hipSuccess ? HEAL_OK
+                                                                                           : HEAL_ERR_LAUNCH;
+}
+
+int64_t heal_kv_reserve_workspace(const heal_kv_pool_t *pool, const heal_kv_batch_t *batch)
+{
+    const int64_t units = kv_reserve_units(pool, batch);
+    return units < 0 ? -1 : heal::kv_reserve_bytes(units);
+}
+
+heal_status_t heal_kv_reserve(const heal_kv_pool_t *pool, const heal_kv_batch_t *batch, int32_t *table,
+                              int64_t table_ld, int64_t table_cols, int32_t *missing, void *workspace,
+                              int64_t workspace_bytes, hipStream_t stream)
+{
+    heal::KvPages p;
+    const int64_t units = kv_reserve_units(pool, batch);
+    if (units < 0 || !kv_pages(pool, batch->seqs, batch->lens, table, table_ld, table_cols, &p) ||
+        !missing || !aligned4(missing) || !aligned4(batch->cu))
+        return HEAL_ERR_INVALID_VALUE;
+    const int64_t bytes = heal::kv_reserve_bytes(units);
+    if (bytes > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < bytes)) return HEAL_ERR_INVALID_VALUE;
+    const heal_status_t st = check_device();
+    if (st != HEAL_OK) return st;
+    // (a call without tokens still writes *missing)
+    const heal::KvSeqs b = {batch->cu, batch->lens, table, nullptr, table_ld, (int32_t)batch->seqs,
+                            (int32_t)batch->tokens, (int32_t)table_cols, p.blocks, 0};
+    return heal::launch_kv_reserve(p, b, batch->seqs > 0 ? units : 0, workspace, missing, stream) == hipSuccess
+               ? HEAL_OK
+               : HEAL_ERR_LAUNCH;
+}
+
+int64_t heal_kv_compact_workspace(const heal_kv_pool_t *pool)
+{
+    return kv_pool_sizes(pool) ? heal::kv_compact_bytes(pool->blocks) : -1;
+}
+
+heal_status_t heal_kv_compact(const heal_kv_pool_t *pool, int64_t rows, int32_t *table, int64_t table_ld,
+                              int64_t table_cols, int32_t *src, int32_t *dst, int32_t *count, void *workspace,
+                              int64_t workspace_bytes, hipStream_t stream)
+{
+    heal::KvPages p;
+    // (lens are not read)
+    if (!kv_pages(pool, rows, table, table, table_ld, table_cols, &p) || !count || !aligned4(count) ||
+        (pool->blocks > 1 && (!src || !dst || !aligned4(src) || !aligned4(dst))) || !workspace ||
+        !aligned16(workspace) || workspace_bytes < heal::kv_compact_bytes(pool->blocks))
+        return HEAL_ERR_INVALID_VALUE;
+    const heal_status_t st = check_device();
+    if (st != HEAL_OK) return st;
+    return heal::launch_kv_compact(p, src, dst, count, workspace, stream) == hipSuccess ? HEAL_OK : HEAL_ERR_LAUNCH;
+}
+
+heal_status_t heal_kv_copy(const heal_kv_cache_t *cache, int64_t blocks, const int32_t *block_src,
+                           const int32_t *block_dst, const int32_t *count, int64_t slots, const int32_t *slot_src,
+                           const int32_t *slot_dst, hipStream_t stream)
+{
+    const int64_t lim = ((int64_t)1 << 31) - 1;
+    if (!kv_cache_sizes(cache) || blocks < 0 || blocks > lim || slots < 0 || slots > lim || !aligned4(count))
+        return HEAL_ERR_INVALID_VALUE;
+    if (blocks > 0 && (!block_src || !block_dst || !aligned4(block_src) || !aligned4(block_dst) ||
+                       !kv_array(cache->k_codes) || !kv_array(cache->v_codes) || !kv_array(cache->scales) ||
+                       !kv_array(cache->k_mean)))
+        return HEAL_ERR_INVALID_VALUE;
+    if (slots > 0 && (!slot_src || !slot_dst || !aligned4(slot_src) || !aligned4(slot_dst) ||
+                      !kv_array(cache->k_recent) || !kv_array(cache->v_recent)))
+        return HEAL_ERR_INVALID_VALUE;
+    if (blocks == 0 && slots == 0) return HEAL_OK;
+    const heal_status_t st = check_device();
+    if (st != HEAL_OK) return st;
+    const heal::KvCache c = {(int32_t)cache->heads, (int32_t)cache->dim, (int32_t)cache->block, cache->k_codes,
+                             cache->v_codes, cache->scales, cache->k_mean, cache->k_recent, cache->v_recent};
+    const heal::KvCopy l = {blocks, slots, block_src, block_dst, count, slot_src, slot_dst};
+    return heal::launch_kv_copy(c, l, (int32_t)cache->blocks, (int32_t)cache->slots, stream) == hipSuccess
+               ? HEAL_OK
+               : HEAL_ERR_LAUNCH;
+}
+
+// ---- the residual stream, adapters ------------------------------------------------
+
+heal_status_t heal_block_norm(int64_t rows, int64_t heads, int64_t dim, const float *h, int64_t h_row,
+                              int64_t h_head, const float *x, int64_t x_row, int64_t x_head,
+                              const heal_norm_t *post, const float *gate, int64_t gate_row, int64_t gate_head,
+                              int64_t gate_col, float scale, const heal_norm_t *pre, float *h_out, int64_t ho_row,
+                              int64_t ho_head, float *out, int64_t out_row, int64_t out_head, hipStream_t stream)
+{
+    const int64_t lim = ((int64_t)1 << 31) - 1;
+    if (rows < 0 || heads < 0 || rows > lim || heads > lim || dim < 1 || dim > kMaxNormDim ||
+        (rows > 0 && heads > lim / rows) || !(fabsf(scale) <= 3.4028235e38f))
+        return HEAL_ERR_INVALID_VALUE;
+    if (rows == 0 || heads == 0) return HEAL_OK;
+    if (!norm_fine(post) || !norm_fine(pre) || (pre != nullptr) != (out != nullptr) || (!x && (post || gate || h_out)) ||
+        (!out && !h_out) || (gate_col != 0 && gate_col != 1))
+        return HEAL_ERR_INVALID_VALUE;
+    if (!h || !aligned4(h) || !aligned4(x) || !aligned4(gate) || !aligned4(h_out) || !aligned4(out))
+        return HEAL_ERR_INVALID_VALUE;
+    // a stride that leads nowhere does not count
+    auto array = [&](const void *p, int64_t row, int64_t head, int64_t cols) {
+        return Rows{static_cast<const float *>(p), rows, heads, cols, rows > 1 ? row : 0, heads > 1 ? head : 0};
+    };
+    const Rows ins[] = {array(h, h_row, h_head, dim), array(x, x_row, x_head, dim),
+                        array(gate, gate_row, gate_head, gate_col ? dim : 1)};
+    const Rows outs[] = {array(h_out, ho_row, ho_head, dim), array(out, out_row, out_head, dim)};
+    for (const Rows &r : ins)
+        if (r.at && (!kv_stride(r.row) || !kv_stride(r.head))) return HEAL_ERR_INVALID_VALUE;
+    for (const Rows &r : outs) {
+        if (!r.at) continue;
+        if (!kv_apart(rows, heads, dim, r.row, r.head)) return HEAL_ERR_INVALID_VALUE;
+        for (int i = 0; i < 3; ++i) {
+            const bool same = i < 2 && ins[i].at == r.at && ins[i].row == r.row && ins[i].head == r.head;
+            if (ins[i].at && !same && !rows_apart(ins[i], r)) return HEAL_ERR_INVALID_VALUE;
+        }
+        for (const heal_norm_t *n : {post, pre})
+            for (const float *w : {n ? n->weight : nullptr, n ? n->bias : nullptr})
+                if (w && !rows_apart(Rows{w, 1, 1, dim, 0, 0}, r)) return HEAL_ERR_INVALID_VALUE;
+    }
+    if (h_out && out && !rows_apart(outs[0], outs[1])) return HEAL_ERR_INVALID_VALUE;
+    const heal_status_t st = check_device();
+    if (st != HEAL_OK) return st;
+    heal::NormArgs a = {};
+    a.rows = (int32_t)(rows * heads);
+    a.heads = (int32_t)heads;
+    a.dim = (int32_t)dim;
+    a.h = h;
+    a.h_row = ins[0].row;
+    a.h_head = ins[0].head;
+    a.x = x;
+    a.x_row = ins[1].row;
+    a.x_head = ins[1].head;
+    if (post) a.post = heal::Norm{post->weight, post->bias, post->eps, post->centred};
+    if (pre) a.pre = heal::Norm{pre->weight, pre->bias, pre->eps, pre->centred};
+    a.gate = gate;
+    a.gate_row = ins[2].row;
+    a.gate_head = ins[2].head;
+    a.gate_col = (int32_t)gate_col;
+    a.scale = scale;
+    a.h_out = h_out;
+    a.ho_row = outs[0].row;
+    a.ho_head = outs[0].head;
+    a.out = out;
+    a.out_row = outs[1].row;
+    a.out_head = outs[1].head;
+    a.vec = dim % 4 == 0;
+    for (const Rows *r : {&ins[0], &ins[1], &outs[0], &outs[1]})
+        if (r->at && !(aligned16(r->at) && r->row % 4 == 0 && r->head % 4 == 0)) a.vec = 0;
+    if (gate && gate_col && !(aligned16(gate) && ins[2].row % 4 == 0 && ins[2].head % 4 == 0)) a.vec = 0;
+    for (const heal_norm_t *n : {post, pre})
+        if (n && !(aligned16(n->weight) && aligned16(n->bias))) a.vec = 0;
+    return heal::launch_block_norm(a, stream) == hipSuccess ? HEAL_OK : HEAL_ERR_LAUNCH;
+}
+
+int64_t heal_lora_workspace(const heal_lora_bank_t *bank, int64_t tokens)
+{
+    return lora_sizes(bank, tokens) ? heal::lora_workspace(tokens, bank->rank, bank->K) : -1;
+}
+
+heal_status_t heal_lora_add(const heal_lora_bank_t *bank, int64_t tokens, int64_t seqs, const int32_t *cu,
+                            const int32_t *ids, const float *x, int64_t ldx, const float *y, int64_t ldy, float *out,
+                            int64_t ldo, void *workspace, int64_t workspace_bytes, hipStream_t stream)
+{
+    if (!lora_sizes(bank, tokens) || seqs < 0 || seqs > kMaxSeqs || (!cu && tokens != seqs)) return HEAL_ERR_INVALID_VALUE;
+    if (ldx < bank->K || ldy < bank->N || ldo < bank->N || ldx > kMaxStride || ldy > kMaxStride || ldo > kMaxStride)
+        return HEAL_ERR_INVALID_VALUE;
+    if (tokens == 0 || seqs == 0) return HEAL_OK;
+    if (!bank->a || !bank->b || !aligned16(bank->a) || !aligned16(bank->b) || !aligned4(bank->ranks) ||
+        !aligned4(bank->scales) || !ids || !aligned4(ids) || !aligned4(cu) || !x || !aligned4(x) || !y || !aligned4(y) ||
+        !out || !aligned4(out))
+        return HEAL_ERR_INVALID_VALUE;
+    const int64_t bytes = heal::lora_workspace(tokens, bank->rank, bank->K);
+    if (!workspace || !aligned16(workspace) || workspace_bytes < bytes) return HEAL_ERR_INVALID_VALUE;
+    const Rows xs = {x, tokens, 1, bank->K, ldx, 0}, ys = {y, tokens, 1, bank->N, ldy, 0},
+               os = {out, tokens, 1, bank->N, ldo, 0};
+    const bool same = y == out && (ldy == ldo || tokens == 1);
+    const __int128 values = (__int128)bank->adapters * bank->rank * (bank->type == HEAL_FP32 ? 4 : 2);
+    if (!rows_apart(xs, os) || (!same && !rows_apart(ys, os)) || !bytes_apart(bank->a, values * bank->K, os) ||
+        !bytes_apart(bank->b, values * bank->N, os))
+        return HEAL_ERR_INVALID_VALUE;
+    const heal_status_t st = check_device();
+    if (st != HEAL_OK) return st;
+    const heal::LoraArgs a = {(int32_t)bank->adapters, (int32_t)bank->rank, (int32_t)tokens, (int32_t)seqs, bank->K,
+                              bank->N, bank->a, bank->b, bank->ranks, bank->scales, cu, ids, x, ldx, y, ldy, out, ldo,
+                              static_cast<float *>(workspace)};
+    return heal::launch_lora(bank->type, a, stream) == hipSuccess ? HEAL_OK : HEAL_ERR_LAUNCH;
 }
 
 }  // extern "C"

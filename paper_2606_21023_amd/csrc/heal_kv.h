@@ -185,6 +185,20 @@ struct KvAttnArgs {
     float *ws_o, *ws_ml;         // parts x rows x dim, parts x rows x 2 (m in log2 units, l)
 };
 
+// Tables and counts of the blocks that they hold (heal_kv_pool_t).
+struct KvPages {
+    int32_t *refs, *table;
+    const int32_t *lens;
+    int64_t table_ld;
+    int32_t blocks, block, rows, cols;
+};
+
+// Lists of heal_kv_copy.
+struct KvCopy {
+    int64_t blocks, slots;
+    const int32_t *block_src, *block_dst, *count, *slot_src, *slot_dst;
+};
+
 // Blocks of a sequence that heal_kv_select can score: 8 bytes of LDS each.
 constexpr int64_t kMaxSelectBlocks = 16384;
 
@@ -204,6 +218,17 @@ hipError_t launch_kv_append(const KvAppendArgs &a, hipStream_t stream);
 hipError_t launch_kv_read(const KvSeqs &b, const KvCache &c, float *k, float *v, hipStream_t stream);
 hipError_t launch_kv_select(const KvSelectArgs &a, hipStream_t stream);
 hipError_t launch_kv_attention(KvAttnArgs &a, const KvPlan &plan, hipStream_t stream);
+
+hipError_t launch_kv_release(const KvPages &p, hipStream_t stream);
+hipError_t launch_kv_fork(const KvPages &p, int32_t pairs, const int32_t *parents, const int32_t *children,
+                          hipStream_t stream);
+int64_t kv_reserve_bytes(int64_t units);     // of workspace, for the units of kv_units
+hipError_t launch_kv_reserve(const KvPages &p, const KvSeqs &b, int64_t units, void *workspace, int32_t *missing,
+                             hipStream_t stream);
+int64_t kv_compact_bytes(int64_t blocks);
+hipError_t launch_kv_compact(const KvPages &p, int32_t *src, int32_t *dst, int32_t *count, void *workspace,
+                             hipStream_t stream);
+hipError_t launch_kv_copy(const KvCache &c, const KvCopy &lists, int32_t blocks, int32_t slots, hipStream_t stream);
 
 // A dispatch counts work-items in 32 bits: launches of at most 2^22 workgroups.
 constexpr int64_t kMaxWorkgroups = (int64_t)1 << 22;

@@ -1,0 +1,248 @@
+"""heal_lora_add against its formula in 64 bits.
+
+v = A x is a sum of K FP32 products (16-bit weights are exact): off by 4 sqrt(K) 2^-24 of the
+sum of their magnitudes (roundings as random as their operands, four deviations).  B v adds what its
+terms inherit, and 4 sqrt(rank) 2^-24 of its own terms' magnitudes; scaling and adding to y are
+three roundings of 2^-24 at most."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_21023_amd as heal
+from gpu_util import announce, needs_gpu
+
+pytestmark = [pytest.mark.gpu, needs_gpu]
+
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+def ints(v):
+    return torch.tensor(np.asarray(v), dtype=torch.int32, device="cuda")
+
+
+def make(adapters, rank, K, N, dtype, ranks=True, seed=0):
+    """A bank whose adapters have ranks of their own; what lies behind a rank is no number."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    a = torch.randn((adapters, rank, K), generator=g, device="cuda") * K ** -0.5
+    b = torch.randn((adapters, N, rank), generator=g, device="cuda")
+    r = None
+    if ranks:
+        r = [max(1, rank - i * 5 % rank) if i != 2 else 0 for i in range(adapters)]
+        for i, n in enumerate(r):
+            a[i, n:] = float("nan")
+            b[i, :, n:] = float("nan")
+        r = ints(r)
+    scales = torch.rand(adapters, generator=g, device="cuda") + 0.5 if ranks else None
+    return heal.LoraBank(a.to(dtype), b.to(dtype), r, scales)
+
+
+def reference(y, x, bank, owner):
+    """(out, bound) in 64 bits; owner[t]: the adapter of token t, None for a token of no sequence."""
+    out, limit = y.double().cpu().numpy(), np.zeros(y.shape)
+    X = x.double().cpu().numpy()
+    for a in set(owner):
+        rows = [t for t, o in enumerate(owner) if o == a]
+        if a is None or not 0 <= a < bank.adapters:
+            continue
+        r = bank.rank if bank.ranks is None else max(0, min(bank.rank, bank.ranks[a].item()))
+        s = 1.0 if bank.scales is None else float(bank.scales[a])
+        A, B = bank.a[a, :r].double().cpu().numpy(), bank.b[a, :, :r].double().cpu().numpy()
+        xa = X[rows]
+        v = xa @ A.T
+        ev = 4 * np.sqrt(bank.K) * 2.0 ** -24 * (np.abs(xa) @ np.abs(A).T)
+        d = s * (v @ B.T)
+        terms = abs(s) * (np.abs(v) @ np.abs(B).T)
+        limit[rows] = (abs(s) * (ev @ np.abs(B).T) + 4 * np.sqrt(max(r, 1)) * 2.0 ** -24 * terms
+                       + 3 * 2.0 ** -24 * (np.abs(out[rows]) + np.abs(d)) + 2.0 ** -140)
+        out[rows] += d
+    return out, limit
+
+
+def check(bank, ids, counts, ragged=True, seed=0, wide=0, place="new", before=0, behind=0):
+    """One call of sequences ids with counts tokens each (tokens of no sequence before and
+    behind them), rows of x, y and out `wide` elements longer than needed."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    T = before + sum(counts) + behind
+    x = torch.randn((T, bank.K + wide), generator=g, device="cuda")[:, wide // 2:wide // 2 + bank.K]
+    y = torch.randn((T, bank.N + wide), generator=g, device="cuda")[:, :bank.N]
+    owner = [None] * before + [a for a, n in zip(ids, counts) for _ in range(n)] + [None] * behind
+    want, limit = reference(y, x, bank, owner)
+    y0 = y.clone()
+    out = {"new": None, "y": y, "given": torch.full((T, bank.N + 3), 7.0, device="cuda")[:, :bank.N]}[place]
+    cu = ints(before + np.concatenate([[0], np.cumsum(counts)])) if ragged else None
+    announce("lora %s ids %s counts %s wide %d %s" % ((bank.adapters, bank.rank, bank.K, bank.N, bank.a.dtype), ids[:8], counts[:8], wide, place))
+    got = heal.heal_lora_add(y, x, bank, ints(ids).view(-1), cu=cu, out=out)
+    torch.cuda.synchronize()
+    mine = [t for t, o in enumerate(owner) if o is not None]
+    err = np.abs(got.double().cpu().numpy() - want)
+    bad = ~(err <= limit)
+    assert not bad[mine].any(), (np.argwhere(bad)[:5], err[bad][:5], limit[bad][:5])
+    bare = [t for t, o in enumerate(owner) if o is not None and not 0 <= o < bank.adapters]
+    assert torch.equal(got[bare], y0[bare])
+    if place == "y":
+        lone = [t for t, o in enumerate(owner) if o is None]
+        assert got is y and torch.equal(y[lone], y0[lone])
+    else:
+        assert torch.equal(y, y0)
+    if place == "given":
+        lone = [t for t, o in enumerate(owner) if o is None]
+        assert (got[lone] == 7.0).all() and (got._base[:, bank.N:] == 7.0).all()
+    return got
+
+
+@pytest.mark.parametrize("type_", list(TYPES))
+@pytest.mark.parametrize("rank", [1, 3, 4, 8, 12, 16, 17, 24, 32, 64, 100, 128, 130, 300])
+def test_ranks(rank, type_):
+    bank = make(4, rank, 320, 200, TYPES[type_], seed=rank)
+    check(bank, [0, 3, 1, 2, -1, 0], [1, 5, 0, 3, 2, 20])
+    check(bank, [3], [1], ragged=False)
+    check(make(2, rank, 64, 48, TYPES[type_], ranks=False), [1, 0, 1], [1, 1, 1], ragged=False)
+
+
+@pytest.mark.parametrize("type_", list(TYPES))
+@pytest.mark.parametrize("K,N", [(1, 1), (3, 5), (31, 33), (32, 16), (64, 64), (100, 130), (127, 511), (513, 1025), (1000, 36), (1024, 4096),
+                                 (4096, 1001), (4100, 260), (14336, 64), (14335, 99), (20000, 20)])
+def test_widths(K, N, type_):
+    bank = make(3, 16, K, N, TYPES[type_], seed=K)
+    check(bank, [0, 1, 0, -1], [3, 1, 1, 2])
+    check(bank, [1], [70])
+
+
+@pytest.mark.parametrize("wide", [1, 2, 4, 9])
+@pytest.mark.parametrize("type_", list(TYPES))
+def test_strides_and_alignment(wide, type_):
+    bank = make(5, 8, 384, 272, TYPES[type_], seed=wide)
+    check(bank, [4, 1, 0, 4, 7], [1, 2, 18, 4, 1], wide=wide)
+    check(bank, [4, 1, 0, 4, -7], [1, 2, 18, 4, 1], wide=wide, place="y")
+    check(bank, [4, 1, 0], [1, 2, 1], wide=wide, place="given", before=3, behind=2)
+
+
+@pytest.mark.parametrize("place", ["new", "y", "given"])
+def test_batches(place):
+    bank = make(7, 16, 256, 160, torch.float32)
+    rng = np.random.default_rng(0)
+    some = lambda n: rng.integers(-2, 9, n).tolist()  # noqa: E731
+    check(bank, some(64), [1] * 64, ragged=False, place=place)
+    check(bank, some(257), [1] * 257, ragged=False, place=place)
+    check(bank, some(100), rng.choice([0, 1, 2, 7], 100).tolist(), place=place)
+    check(bank, some(6), [64, 1, 63, 65, 200, 128], place=place)
+    check(bank, some(3), [0, 0, 0], place=place, before=2, behind=70)
+    check(bank, [3] * 200, [1] * 200, ragged=False, place=place)
+    check(bank, [3] * 40, [5] * 40, place=place)
+    check(bank, [1, 2] * 50, [1, 0] * 50, place=place)
+    check(bank, list(range(7)) * 3, [3] * 21, place=place, before=61, behind=67)
+    # many sequences without tokens between two that share a tile and an adapter
+    check(bank, [4] + some(300) + [4, 5], [3] + [0] * 300 + [3, 2], place=place)
+    check(bank, [4] + some(300) + [4, 5], [3] + [0] * 300 + [300, 2], place=place)
+
+
+def test_no_adapter_at_all():
+    bank = make(3, 16, 128, 64, torch.float32)
+    check(bank, [-1, 3, 2**31 - 1, -2**31, 2], [2, 70, 3, 1, 4])   # (2 has rank 0)
+    check(bank, [-1], [1], ragged=False)
+    x, y = torch.randn(0, 128, device="cuda"), torch.randn(0, 64, device="cuda")
+    assert heal.heal_lora_add(y, x, bank, ints([])).shape == (0, 64)
+    assert heal.heal_lora_add(y, x, bank, ints([1]), cu=ints([0, 0])).shape == (0, 64)
+
+
+def test_ranks_outside_the_bank_are_bounded():
+    a, b = torch.randn(3, 8, 96, device="cuda"), torch.randn(3, 40, 8, device="cuda")
+    check(heal.LoraBank(a, b, ints([9, -1, 2**31 - 1])), [0, 1, 2], [2, 2, 2])
+
+
+@pytest.mark.parametrize("type_", list(TYPES))
+@pytest.mark.parametrize("rank", [8, 64, 200])
+def test_a_rows_bits_do_not_depend_on_the_batch(rank, type_):
+    bank = make(6, rank, 5000, 300, TYPES[type_], ranks=False)
+    torch.manual_seed(0)
+    x, y = torch.randn(300, 5000, device="cuda"), torch.randn(300, 300, device="cuda")
+    ids = np.random.default_rng(1).integers(-1, 6, 300)
+    want = heal.heal_lora_add(y, x, bank, ints(ids))
+    assert torch.equal(heal.heal_lora_add(y, x, bank, ints(ids)), want)
+    for t in (0, 5, 64, 299):
+        assert torch.equal(heal.heal_lora_add(y[t:t + 1], x[t:t + 1], bank, ints(ids[t:t + 1])), want[t:t + 1])
+    one = heal.heal_lora_add(y, x, bank, ints([3]), cu=ints([0, 300]))
+    mine = torch.from_numpy(np.flatnonzero(ids == 3)).cuda()
+    assert torch.equal(one[mine], want[mine])
+    cut = heal.heal_lora_add(y[7:111], x[7:111], bank, ints([3, 3]), cu=ints([0, 50, 104]))
+    assert torch.equal(cut, one[7:111])
+
+
+def test_what_is_not_finite_stays_in_its_row():
+    bank = make(4, 16, 300, 100, torch.float32, ranks=False)
+    torch.manual_seed(0)
+    x, y = torch.randn(40, 300, device="cuda"), torch.randn(40, 100, device="cuda")
+    ids = ints([i % 3 for i in range(40)])
+    want = heal.heal_lora_add(y, x, bank, ids)
+    x[7, 299], x[8, 0], y[30, 5] = float("nan"), float("inf"), float("-inf")
+    got = heal.heal_lora_add(y, x, bank, ids)
+    fine = [i for i in range(40) if i not in (7, 8, 30)]
+    assert torch.equal(got[fine], want[fine])
+    assert got[7].isnan().all() and not got[8].isfinite().any() and got[30, 5] == float("-inf")
+    # an adapter that nothing uses may hold anything
+    bank.a[3], bank.b[3] = float("nan"), float("inf")
+    assert torch.equal(heal.heal_lora_add(y, x, bank, ids)[fine], want[fine])
+
+
+def test_captured():
+    """Two graphs that share nothing but the bank, replayed with other requests."""
+    bank = make(6, 24, 1030, 520, torch.bfloat16)
+    torch.manual_seed(2)
+    x, y = torch.randn(90, 1030, device="cuda"), torch.randn(90, 520, device="cuda")
+    ids, cu = ints([0] * 30), ints(range(0, 93, 3))
+    one = ints([0] * 90)
+    out, out1 = torch.zeros_like(y), torch.zeros_like(y)
+    heal.heal_lora_add(y, x, bank, ids, cu=cu, out=out)
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    with torch.cuda.graph(graphs[0]):
+        heal.heal_lora_add(y, x, bank, ids, cu=cu, out=out)
+    with torch.cuda.graph(graphs[1]):
+        heal.heal_lora_add(y, x, bank, one, out=out1)
+    rng = np.random.default_rng(3)
+    for turn in range(3):
+        x.copy_(torch.randn_like(x))
+        ids.copy_(ints(rng.integers(-1, 7, 30)))
+        one.copy_(ints(rng.integers(-1, 7, 90)))
+        want = heal.heal_lora_add(y, x, bank, ids, cu=cu), heal.heal_lora_add(y, x, bank, one)
+        out.zero_(), out1.zero_()
+        torch.cuda.synchronize()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(out1, want[1])
+
+
+def test_calls_on_two_streams():
+    bank = make(3, 16, 2048, 2048, torch.float32)
+    torch.manual_seed(3)
+    x, y = torch.randn(2, 200, 2048, device="cuda"), torch.randn(2, 200, 2048, device="cuda")
+    ids = [ints([i % 4 - 1 for i in range(200)]), ints([2 - i % 4 for i in range(200)])]
+    want = [heal.heal_lora_add(y[i], x[i], bank, ids[i]) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(heal.heal_lora_add(y[i], x[i], bank, ids[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(o, want[i]) for o in got[i])
+
+
+def test_refusals():
+    bank = make(3, 8, 64, 32, torch.float32)
+    x, y, ids = torch.randn(4, 64, device="cuda"), torch.randn(4, 32, device="cuda"), ints([0, 1, 2, 0])
+    a, b = bank.a, bank.b
+    for f in (lambda: heal.heal_lora_add(y, x[:, :63], bank, ids), lambda: heal.heal_lora_add(y[:3], x, bank, ids),
+              lambda: heal.heal_lora_add(y, x, bank, ids[:3]), lambda: heal.heal_lora_add(y, x, bank, ids.long()),
+              lambda: heal.heal_lora_add(y, x.half(), bank, ids), lambda: heal.heal_lora_add(y, x, bank, ids, cu=ids),
+              lambda: heal.heal_lora_add(y, x, bank, ids, out=y[:, :31]), lambda: heal.heal_lora_add(y, x, bank, ids, out=x[:, :32]),
+              lambda: heal.heal_lora_add(y, x, bank, ids.cpu()), lambda: heal.heal_lora_add(y, x, (a, b), ids),
+              lambda: heal.heal_lora_add(y, x.t(), bank, ids), lambda: heal.LoraBank(a, b.half()), lambda: heal.LoraBank(a, b[:2]),
+              lambda: heal.LoraBank(a, b.transpose(1, 2)), lambda: heal.LoraBank(a[:, :, 1:], b), lambda: heal.LoraBank(a.double(), b.double()),
+              lambda: heal.LoraBank(a, b, ranks=ids), lambda: heal.LoraBank(a, b, scales=ids[:3]), lambda: heal.LoraBank(a, b.cpu()),
+              lambda: setattr(bank, "a", b), lambda: delattr(bank, "b"), lambda: heal.LoraBank(torch.empty(0, 8, 64, device="cuda"), b[:0])):
+        with pytest.raises(heal.HealError):
+            f()

@@ -1,0 +1,133 @@
+"""The pages of a cache where no GPU is needed: refusals, empty calls, workspace."""
+import ctypes
+
+import pytest
+
+import paper_2606_21023_amd as heal
+from test_kv_host import BAD_CACHE, _batch, _cache
+
+FAKE, OK, INVALID = 0x10000, 0, 1   # FAKE is never dereferenced
+
+
+def _pool(**kw):
+    a = dict(blocks=100, block=64, refs=FAKE)
+    a.update(kw)
+    return heal._CPool(*a.values())
+
+
+def _release(pool=None, **kw):
+    a = dict(rows=3, lens=FAKE, table=FAKE, table_ld=7, table_cols=6)
+    a.update(kw)
+    return heal.lib().heal_kv_release(ctypes.byref(pool or _pool()), *a.values(), None)
+
+
+def _fork(pool=None, **kw):
+    a = dict(rows=3, lens=FAKE, table=FAKE, table_ld=7, table_cols=6, pairs=2, parents=FAKE, children=FAKE)
+    a.update(kw)
+    return heal.lib().heal_kv_fork(ctypes.byref(pool or _pool()), *a.values(), None)
+
+
+def _reserve(pool=None, batch=None, **kw):
+    a = dict(table=FAKE, table_ld=7, table_cols=6, missing=FAKE, workspace=FAKE, size=1 << 40)
+    a.update(kw)
+    return heal.lib().heal_kv_reserve(ctypes.byref(pool or _pool()), ctypes.byref(batch or _batch(table=None, slots=None)),
+                                      *a.values(), None)
+
+
+def _compact(pool=None, **kw):
+    a = dict(rows=3, table=FAKE, table_ld=7, table_cols=6, src=FAKE, dst=FAKE, count=FAKE, workspace=FAKE, size=1 << 40)
+    a.update(kw)
+    return heal.lib().heal_kv_compact(ctypes.byref(pool or _pool()), *a.values(), None)
+
+
+def _copy(cache=None, **kw):
+    a = dict(blocks=3, block_src=FAKE, block_dst=FAKE, count=None, slots=2, slot_src=FAKE, slot_dst=FAKE)
+    a.update(kw)
+    return heal.lib().heal_kv_copy(ctypes.byref(cache or _cache()), *a.values(), None)
+
+
+CALLS = [_release, _fork, _reserve, _compact]
+BAD_TABLE = [dict(table=None), dict(table=FAKE + 2), dict(table_ld=5), dict(table_cols=-1),
+             dict(table_ld=(1 << 40) + 1), dict(table_cols=1 << 25, table_ld=1 << 25)]
+
+
+@pytest.mark.parametrize("call", CALLS)
+@pytest.mark.parametrize("kw", [dict(blocks=0), dict(blocks=(1 << 30) + 1), dict(block=48), dict(block=0), dict(refs=None),
+                                dict(refs=FAKE + 1)], ids=str)
+def test_a_bad_pool_is_refused(call, kw):
+    assert call(pool=_pool(**kw)) == INVALID
+
+
+@pytest.mark.parametrize("call", CALLS)
+@pytest.mark.parametrize("kw", BAD_TABLE, ids=str)
+def test_a_bad_table_is_refused(call, kw):
+    assert call(**kw) == INVALID
+
+
+@pytest.mark.parametrize("call,kw", [(_release, kw) for kw in (
+    dict(rows=-1), dict(rows=(1 << 24) + 1), dict(lens=None), dict(lens=FAKE + 2))] + [(_fork, kw) for kw in (
+        dict(rows=-1), dict(lens=None), dict(pairs=-1), dict(pairs=65537), dict(parents=None), dict(children=None),
+        dict(parents=FAKE + 1), dict(children=FAKE + 3))] + [(_reserve, kw) for kw in (
+            dict(missing=None), dict(missing=FAKE + 2))] + [(_compact, kw) for kw in (
+                dict(rows=-1), dict(src=None), dict(dst=None), dict(count=None), dict(src=FAKE + 2), dict(count=FAKE + 1),
+                dict(workspace=None), dict(workspace=FAKE + 8), dict(size=399))] + [(_copy, kw) for kw in (
+                    dict(blocks=-1), dict(slots=-1), dict(block_src=None), dict(block_dst=None), dict(slot_src=None),
+                    dict(slot_dst=None), dict(block_src=FAKE + 2), dict(slot_dst=FAKE + 1), dict(count=FAKE + 2),
+                    dict(blocks=1 << 31))],
+    ids=lambda x: getattr(x, "__name__", None) or ",".join("%s=%s" % i for i in x.items()))
+def test_bad_arguments_are_refused(call, kw):
+    assert call(**kw) == INVALID
+
+
+@pytest.mark.parametrize("kw", [dict(seqs=-1), dict(seqs=(1 << 24) + 1), dict(tokens=-1), dict(tokens=(1 << 30) + 1),
+                                dict(cu=None, tokens=4), dict(cu=FAKE + 2), dict(lens=None), dict(lens=FAKE + 1)], ids=str)
+def test_a_bad_batch_is_refused(kw):
+    assert _reserve(batch=_batch(**kw)) == INVALID
+
+
+@pytest.mark.parametrize("kw", BAD_CACHE, ids=str)
+def test_a_bad_cache_is_refused(kw):
+    assert _copy(cache=_cache(**kw)) == INVALID
+
+
+def test_arrays_that_a_copy_does_not_touch_may_be_missing():
+    none = dict(blocks=0, block_src=None, block_dst=None, slots=0, slot_src=None, slot_dst=None)
+    assert _copy(cache=_cache(k_codes=0, v_codes=0, scales=0, k_mean=0, k_recent=0, v_recent=0), **none) == OK
+
+
+def test_calls_without_rows_do_nothing():
+    assert _release(rows=0, lens=None, table=None) == OK
+    assert _release(table=None, table_cols=0) == OK
+    assert _fork(rows=0, lens=None, table=None) == OK
+    assert _fork(pairs=0, parents=None, children=None) == OK
+    assert _fork(table=None, table_cols=0) == OK
+
+
+def test_workspace():
+    L = heal.lib()
+
+    def reserve(pool=None, **kw):
+        return L.heal_kv_reserve_workspace(ctypes.byref(pool or _pool()), ctypes.byref(_batch(**kw)))
+    assert reserve() == 0 and reserve(cu=None, tokens=2000, seqs=2000) == 0
+    assert reserve(cu=None, tokens=5000, seqs=5000) == 12 * 5000
+    assert reserve(tokens=640000, seqs=3) == (12 * 10006 + 15) // 16 * 16
+    assert reserve(tokens=-1) == -1 and reserve(pool=_pool(block=10)) == -1 and reserve(cu=None) == -1
+    assert reserve(lens=None) == 0   # sizes are all that it reads
+    assert L.heal_kv_compact_workspace(ctypes.byref(_pool())) >= 4 * 100
+    assert L.heal_kv_compact_workspace(ctypes.byref(_pool(blocks=0))) == -1
+    # what lacks workspace is refused
+    big = _batch(cu=None, tokens=5000, seqs=5000)
+    for kw in (dict(workspace=None), dict(workspace=FAKE + 4), dict(size=59999)):
+        assert _reserve(batch=big, **kw) == INVALID
+
+
+def test_the_binding_refuses_what_is_no_pool():
+    import torch
+    for refs, block in ((torch.zeros(4, dtype=torch.int32), 64), (torch.zeros(4), 64), ([0, 0], 64)):
+        with pytest.raises(heal.HealError):
+            heal.KVPool(refs, block)   # (no CUDA tensor)
+    for f in (lambda: heal.heal_kv_release(None, None, None), lambda: heal.heal_kv_fork(1, None, None, [], []),
+              lambda: heal.heal_kv_reserve("pool", 1, None, None), lambda: heal.heal_kv_compact(None, None),
+              lambda: heal.heal_kv_copy(None)):
+        with pytest.raises(heal.HealError):
+            f()
