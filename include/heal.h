@@ -677,7 +677,7 @@ typedef enum heal_type_t { HEAL_FP32 = 0, HEAL_BF16 = 1, HEAL_FP16 = 2 } heal_ty
 
 typedef struct heal_lora_bank_t {
     int64_t adapters;       /* 1 .. 2^31 - 1 */
-    int64_t rank;           /* 1 .. 1024 */
+    int64_t rank;           /* 1 .. 512 */
     int64_t K, N;           /* 1 .. 2^24 each */
     int type;               /* heal_type_t of a and b */
     const void *a, *b;      /* 16-byte aligned */

@@ -333,7 +333,7 @@ bool norm_fine(const heal_norm_t *n)
 bool lora_sizes(const heal_lora_bank_t *b, int64_t tokens)
 {
     const int64_t lim = (int64_t)1 << 24;
-    return b && b->adapters >= 1 && b->adapters < ((int64_t)1 << 31) && b->rank >= 1 && b->rank <= 1024 && b->K >= 1 &&
+    return b && b->adapters >= 1 && b->adapters < ((int64_t)1 << 31) && b->rank >= 1 && b->rank <= 512 && b->K >= 1 &&
            b->K <= lim && b->N >= 1 && b->N <= lim && b->type >= HEAL_FP32 && b->type <= HEAL_FP16 && tokens >= 0 &&
            tokens <= kMaxLoraTokens;
 }

@@ -1,9 +1,11 @@
 """heal_lora_add against its formula in 64 bits.
 
-v = A x is a sum of K FP32 products (16-bit weights are exact): off by 4 sqrt(K) 2^-24 of the
-sum of their magnitudes (roundings as random as their operands, four deviations).  B v adds what its
-terms inherit, and 4 sqrt(rank) 2^-24 of its own terms' magnitudes; scaling and adding to y are
-three roundings of 2^-24 at most."""
+A product of two values is up to six products of their bf16 parts; those that are left out are below
+2^-26 of it (each rest after rounding to 8 bits is at most 2^-9 of what it is the rest of: second times third
+part 2^-27, twice).  So v = A x is a sum of 6 K exact products in FP32: off by 4 sqrt(6 K) 2^-24 of
+the sum of their magnitudes (roundings as random as their operands, four deviations) and 2^-26.
+B v adds what its terms inherit, and as much of its own terms' magnitudes with 6 rank of them;
+scaling and adding to y are three roundings of 2^-24 at most."""
 import numpy as np
 import pytest
 import torch
@@ -49,10 +51,10 @@ def reference(y, x, bank, owner):
         A, B = bank.a[a, :r].double().cpu().numpy(), bank.b[a, :, :r].double().cpu().numpy()
         xa = X[rows]
         v = xa @ A.T
-        ev = 4 * np.sqrt(bank.K) * 2.0 ** -24 * (np.abs(xa) @ np.abs(A).T)
+        ev = (4 * np.sqrt(6 * bank.K) * 2.0 ** -24 + 2.0 ** -26) * (np.abs(xa) @ np.abs(A).T)
         d = s * (v @ B.T)
         terms = abs(s) * (np.abs(v) @ np.abs(B).T)
-        limit[rows] = (abs(s) * (ev @ np.abs(B).T) + 4 * np.sqrt(max(r, 1)) * 2.0 ** -24 * terms
+        limit[rows] = (abs(s) * (ev @ np.abs(B).T) + (4 * np.sqrt(6 * max(r, 1)) * 2.0 ** -24 + 2.0 ** -26) * terms
                        + 3 * 2.0 ** -24 * (np.abs(out[rows]) + np.abs(d)) + 2.0 ** -140)
         out[rows] += d
     return out, limit
