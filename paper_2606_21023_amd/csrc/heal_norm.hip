@@ -79,6 +79,124 @@ __device__ __forceinline__ double normed(const Norm &n, const Stats &st, float y
     return n.bias ? v + (double)n.bias[c] : v;
 }
 
+// T threads a row, U times four columns of it each, all of the row in registers between the sums and the
+// stores: every stream is read once and written once.  With VEC the four columns lie side by side in 16
+// bytes; else (rows of other lengths or alignment) T apart.
+template <int T, int U, bool VEC>
+struct Line {
+    static __device__ __forceinline__ int column(int u, int e)
+    {
+        const int t = threadIdx.x % T;
+        return VEC ? (u * T + t) * 4 + e : (u * 4 + e) * T + t;
+    }
+    static __device__ __forceinline__ void load(const float *p, int dim, float (&v)[U][4])
+    {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (VEC) {
+                const int c = column(u, 0);
+                const f32x4 q = c < dim ? *reinterpret_cast<const f32x4 *>(p + c) : f32x4{};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[u][e] = q[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[u][e] = column(u, e) < dim ? p[column(u, e)] : 0.0f;
+            }
+        }
+    }
+    static __device__ __forceinline__ void store(float *p, int dim, const float (&v)[U][4])
+    {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (VEC) {
+                const int c = column(u, 0);
+                if (c < dim) *reinterpret_cast<f32x4 *>(p + c) = f32x4{v[u][0], v[u][1], v[u][2], v[u][3]};
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (column(u, e) < dim) p[column(u, e)] = v[u][e];
+            }
+        }
+    }
+    static __device__ __forceinline__ Stats stats_of(const Norm &n, int dim, const float (&v)[U][4], double pivot, double *part)
+    {
+        double s = 0.0, q = 0.0;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const double d = column(u, e) < dim ? (double)v[u][e] - pivot : 0.0;
+                s += d;
+                q += d * d;
+            }
+        row_sums<T>(s, q, n.centred, part);
+        return stats(n, dim, pivot, s, q);
+    }
+};
+
+// The norm of one value with its weight and bias.
+__device__ __forceinline__ double normed(const Stats &st, float y, float w, float b)
+{
+    return ((double)y - st.shift) * st.inv * (double)w + (double)b;
+}
+
+template <int T, int U, bool VEC>
+__global__ void __launch_bounds__(T < 256 ? 256 : T) norm_kernel(NormArgs a, int32_t row0)
+{
+    typedef Line<T, U, VEC> L;
+    __shared__ double part[2][T > 64 ? 2 * T / 64 : 1];
+    const int32_t r = row0 + (T < 256 ? blockIdx.x * (256 / T) + threadIdx.x / T : blockIdx.x);
+    if (T < 256 && r >= a.rows) return;   // (T > 64: never)
+    const Row p = row_of(a, r);
+    float h[U][4], w[U][4], b[U][4] = {};
+    L::load(p.h, a.dim, h);
+    if (p.x) {
+        float x[U][4], g[U][4];
+        L::load(p.x, a.dim, x);
+        if (a.post.weight) L::load(a.post.weight, a.dim, w);
+        if (a.post.bias) L::load(a.post.bias, a.dim, b);
+        if (p.gate && a.gate_col) L::load(p.gate, a.dim, g);
+        const double f = (double)a.scale * (p.gate && !a.gate_col ? (double)*p.gate : 1.0);
+        Stats st = {0.0, 1.0};
+        if (a.post.weight) st = L::stats_of(a.post, a.dim, x, a.post.centred ? (double)*p.x : 0.0, part[0]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const double y = a.post.weight ? normed(st, x[u][e], w[u][e], b[u][e]) : (double)x[u][e];
+                const double fu = p.gate && a.gate_col ? f * (double)g[u][e] : f;
+                h[u][e] = (float)((double)h[u][e] + fu * y);
+            }
+    }
+    if (p.out) {
+        L::load(a.pre.weight, a.dim, w);
+        if (a.pre.bias) L::load(a.pre.bias, a.dim, b);
+        // the pivot: the row's first element, from the thread that has it
+        double pivot = 0.0;
+        if (a.pre.centred) {
+            if (T <= 64) {
+                pivot = (double)__shfl(h[0][0], 0, T);
+            } else {
+                __shared__ float first;
+                if (threadIdx.x == 0) first = h[0][0];
+                __syncthreads();
+                pivot = (double)first;
+            }
+        }
+        const Stats st = L::stats_of(a.pre, a.dim, h, pivot, part[1]);
+        float o[U][4];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                o[u][e] = (float)normed(st, h[u][e], w[u][e], a.pre.bias ? b[u][e] : 0.0f);
+        L::store(p.out, a.dim, o);
+    }
+    // (an output may lie on an input: every thread writes the columns that it alone reads, and the
+    // first element, which all threads of a centred row read, is written behind a sum of theirs)
+    if (p.ho) L::store(p.ho, a.dim, h);
+}
+
 // h' of column c.
 __device__ __forceinline__ float added(const NormArgs &a, const Row &p, const Stats &post, int c)
 {
@@ -134,10 +252,37 @@ norm_any_kernel(NormArgs a, int32_t row0)
     }
 }
 
+template <int T, int U>
+hipError_t launch(const NormArgs &a, hipStream_t stream)
+{
+    constexpr int rows = T < 256 ? 256 / T : 1;   // of a workgroup
+    for (int64_t r = 0; r < a.rows;) {
+        const int64_t left = (a.rows - r + rows - 1) / rows, n = left < (1 << 21) ? left : 1 << 21;
+        const dim3 grid((unsigned)n), block(T < 256 ? 256 : T);
+        if (a.vec)
+            norm_kernel<T, U, true><<<grid, block, 0, stream>>>(a, (int32_t)r);
+        else
+            norm_kernel<T, U, false><<<grid, block, 0, stream>>>(a, (int32_t)r);
+        const hipError_t err = hipGetLastError();
+        if (err != hipSuccess) return err;
+        r += n * rows;
+    }
+    return hipSuccess;
+}
+
 }  // namespace
 
 hipError_t launch_block_norm(const NormArgs &a, hipStream_t stream)
 {
+    if (a.dim <= 64) return launch<16, 1>(a, stream);
+    if (a.dim <= 128) return launch<32, 1>(a, stream);
+    if (a.dim <= 256) return launch<64, 1>(a, stream);
+    if (a.dim <= 512) return launch<64, 2>(a, stream);
+    if (a.dim <= 1024) return launch<256, 1>(a, stream);
+    if (a.dim <= 2048) return launch<256, 2>(a, stream);
+    if (a.dim <= 4096) return launch<256, 4>(a, stream);
+    if (a.dim <= 8192) return launch<512, 4>(a, stream);
+    if (a.dim <= 16384) return launch<512, 8>(a, stream);
     for (int32_t r = 0; r < a.rows;) {
         const int32_t n = a.rows - r < (1 << 21) ? a.rows - r : 1 << 21;
         norm_any_kernel<<<dim3((unsigned)n), dim3(kMaxThreads), 0, stream>>>(a, r);
