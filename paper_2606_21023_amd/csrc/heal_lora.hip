@@ -11,11 +11,13 @@
 // (FP32 MFMA: 256 cycles, more than the memory takes from rank 64 on; and the compiler
 // does not keep the registers of their addends from being written too early).
 //
-// Work units.  A unit is a tile of 64 tokens and one of the adapters in it: the first
-// sequence of the tile with that adapter leads, and its workgroup takes all of the tile's rows of
-// the adapter, packed into blocks of 16.  So a decode step reads an adapter once for 64
+// Tiles.  A workgroup has a tile of 64 tokens, finds the adapter of each, and takes the
+// tile's adapters one after another (or every n-th, where n workgroups share the tile), the
+// rows of each packed into blocks of 16.  So a decode step reads an adapter once for 64
 // tokens, whatever their order, and a prompt fills its tiles.
 #include <string.h>
+
+#include <algorithm>
 
 #include "heal_device.h"
 #include "heal_kv.h"
@@ -26,14 +28,17 @@ namespace heal {
 namespace {
 
 constexpr int kTile = 64;                 // tokens of a unit
-constexpr int kDownWaves = 8, kUpWaves = 4;
+constexpr int kDownWaves = 4, kUpWaves = 4;
 constexpr int kGroup = 128;               // ranks that a workgroup of the first kernel takes
+// Strips of the second kernel are as narrow as this many workgroups allow: 5094 tokens of 4096 columns 44 us
+// (512: 63), 64 tokens with 24 adapters at 14336 columns 15 us (512: 32, 1024: 19).
+constexpr int64_t kUpWorkgroups = 2048;
 
-// Depth of a part of K: the waves of a workgroup share it in runs of whole 32s.
+// Depth of a part of K, whole 32s for each wave; 16 parts at most.
 __host__ __device__ inline int64_t part_depth(int64_t K)
 {
-    int64_t d = 1024;
-    while (K > 8 * d) d *= 2;
+    int64_t d = 512;
+    while (K > 16 * d) d *= 2;
     return d;
 }
 
@@ -42,123 +47,93 @@ __host__ __device__ inline int parts_of(int64_t K) { return (int)((K + part_dept
 // Ranks of a row of v, whole 16s.
 __host__ __device__ inline int32_t padded(int32_t rank) { return (rank + 15) / 16 * 16; }
 
-struct Unit {
-    int32_t first, count;     // tile, rows of it that are the unit's (0: nothing to do)
-    int32_t id, rank;         // adapter (-1: none)
-    int32_t row;              // lane i: the tile's row that is the i-th of the unit
-};
-
-__device__ __forceinline__ int32_t known(const LoraArgs &a, int32_t id) { return id >= 0 && id < a.adapters ? id : -1; }
-
-__device__ __forceinline__ uint64_t bits(int32_t lo, int32_t hi)   // lo <= hi <= 64
-{
-    return (hi < 64 ? ((uint64_t)1 << hi) : 0) - (lo < 64 ? ((uint64_t)1 << lo) : 0);
-}
-
-// Rows of the tile at `first` that sequences of adapter id among j0 .. j0 + 63 own: lane l
-// has the tokens begin .. end - 1 and the adapter of sequence j0 + l.
-__device__ __forceinline__ uint64_t rows_of(int32_t first, int32_t id, int32_t begin, int32_t end, int32_t other)
-{
-    const int32_t lo = max(begin - first, 0), hi = min(end - first, kTile);
-    uint64_t mine = __ballot(other == id && lo < hi), rows = 0;
-    while (mine) {
-        const int l = __builtin_ctzll(mine);
-        mine &= mine - 1;
-        rows |= bits(__builtin_amdgcn_readlane(lo, l), __builtin_amdgcn_readlane(hi, l));
-    }
-    return rows;
-}
-
-// Unit u, found by every wave for itself.
-__device__ __forceinline__ Unit unit_of(const LoraArgs &a, int32_t u)
+// The adapter of token first + lane (-1: none; -2: no such token, or of no sequence).
+__device__ __forceinline__ int32_t adapter_of_lane(const LoraArgs &a, int32_t first)
 {
     const int lane = threadIdx.x & 63;
-    Unit r = {0, 0, -1, 0, 0};
-    uint64_t rows = 0;
-    if (!a.cu) {   // a token a sequence, a unit each
-        r.first = u / kTile * kTile;
-        const int32_t t = r.first + lane;
-        const int32_t other = t < a.tokens ? known(a, a.ids[t]) : -2;
-        r.id = __builtin_amdgcn_readlane(other, u - r.first);
-        rows = __ballot(other == r.id);
-        if (__builtin_ctzll(rows) != u - r.first) return r;
-    } else {
-        // sequence i has the units first / 64 + i and on, one for each tile that it may reach
-        int32_t i, begin, end, other, j0 = 0;
-        auto load = [&](int32_t j) {
-            const bool is = j >= 0 && j < a.seqs;
-            begin = is ? kv_clamp(a.cu[j], 0, a.tokens) : a.tokens;
-            end = is ? kv_clamp(a.cu[j + 1], begin, a.tokens) : a.tokens;
-            other = is ? known(a, a.ids[j]) : -2;
-        };
-        if (a.seqs <= 64) {
-            load(lane);
-            const uint64_t below = __ballot(lane < a.seqs && begin / kTile + lane <= u);
-            i = below ? 63 - __builtin_clzll(below) : 0;
-        } else {
-            i = kv_last_at_most(a.seqs, u, [&](int32_t j) { return (int64_t)kv_clamp(a.cu[j], 0, a.tokens) / kTile + j; });
-            j0 = i;
-            load(j0 + lane);
-        }
-        i = __builtin_amdgcn_readfirstlane(i);
-        const int32_t at = __builtin_amdgcn_readlane(begin, i - j0), to = __builtin_amdgcn_readlane(end, i - j0);
-        r.id = __builtin_amdgcn_readlane(other, i - j0);
-        const int32_t tile = at / kTile + (u - (at / kTile + i));
-        r.first = tile * kTile;
-        if (u < at / kTile + i || r.first >= to || at >= to) return r;
-        // the tile's rows from this sequence on, and whether an earlier one leads
-        bool led = false;
-        if (a.seqs <= 64) {
-            rows = rows_of(r.first, r.id, begin, end, other);
-            led = rows && __builtin_ctzll(rows) < max(at - r.first, 0);
-        } else {
-            for (int32_t j = j0;; j += 64) {
-                if (j != j0) load(j + lane);
-                rows |= rows_of(r.first, r.id, begin, end, other);
-                if (__builtin_amdgcn_readlane(end, 63) >= r.first + kTile || j + 64 >= a.seqs) break;
-            }
-            for (int32_t j = j0 - 64; at > r.first && j > -64; j -= 64) {
-                load(j + lane);
-                led |= __ballot(other == r.id && begin < end && end > r.first) != 0;
-                // (lane 0, or the first sequence there is)
-                if (led || __builtin_amdgcn_readlane(begin, j < 0 ? -j : 0) <= r.first) break;
-            }
-        }
-        if (led) return r;
+    const int32_t t = first + lane;
+    auto known = [&](int32_t id) { return id >= 0 && id < a.adapters ? id : -1; };
+    if (!a.cu) return t < a.tokens ? known(a.ids[t]) : -2;
+    // sequences j0 .. j0 + 63, from the last one that begins at the tile's first token or before it
+    int32_t j0 = 0, found = -2;
+    if (a.seqs > 64)
+        j0 = __builtin_amdgcn_readfirstlane(
+            kv_last_at_most(a.seqs, first, [&](int32_t j) { return (int64_t)kv_clamp(a.cu[j], 0, a.tokens); }));
+    for (;;) {
+        const int32_t j = j0 + lane;
+        const bool is = j < a.seqs;
+        const int32_t begin = is ? kv_clamp(a.cu[j], 0, a.tokens) : a.tokens;
+        const int32_t end = is ? kv_clamp(a.cu[j + 1], begin, a.tokens) : a.tokens;
+        const int32_t id = is ? known(a.ids[j]) : -2;
+        int at = 0;   // the last of these sequences that begins at t or before it
+#pragma unroll
+        for (int step = 32; step > 0; step >>= 1) at = __shfl(begin, at + step) <= t ? at + step : at;
+        const int32_t b = __shfl(begin, at), e = __shfl(end, at), other = __shfl(id, at);
+        if (b <= t && t < e) found = other;
+        if (__builtin_amdgcn_readlane(end, 63) >= first + kTile || j0 + 64 >= a.seqs) return found;
+        j0 += 64;
     }
-    r.count = __popcll(rows);
-    // the i-th set bit to lane i, the others behind
-    const int below = __popcll(rows & (((uint64_t)1 << lane) - 1));
-    const int to = rows >> lane & 1 ? below : r.count + lane - below;
-    r.row = __builtin_amdgcn_ds_permute(to * 4, lane);
-    if (r.id >= 0) {
-        const int32_t rank = a.ranks ? a.ranks[r.id] : a.rank;
-        r.rank = __builtin_amdgcn_readfirstlane(rank < 0 ? 0 : rank > a.rank ? a.rank : rank);
-    }
-    return r;
 }
 
-__host__ __device__ inline int64_t units_of(bool ragged, int64_t tokens, int64_t seqs)
+// The rows of a tile that share an adapter.
+struct Group {
+    int32_t first, count, id;   // tile, rows, adapter (-1: none)
+    int32_t row;                // lane i: the tile's row that is the i-th of the group
+};
+
+// f for every `share`-th group of the tile, from `turn` on; every wave finds them for itself.
+template <class F>
+__device__ __forceinline__ void for_groups(const LoraArgs &a, int32_t first, int32_t turn, int32_t share, F f)
 {
-    return ragged ? tokens / kTile + seqs : tokens;
+    const int lane = threadIdx.x & 63;
+    const int32_t id = adapter_of_lane(a, first);
+    uint64_t todo = __ballot(id != -2);
+    for (int32_t n = 0; todo; ++n) {
+        const int32_t mine = __builtin_amdgcn_readlane(id, __builtin_ctzll(todo));
+        const uint64_t rows = __ballot(id == mine);
+        todo &= ~rows;
+        if (n != turn) continue;
+        turn += share;
+        const int32_t count = __popcll(rows);
+        // the i-th set bit to lane i, the others behind
+        const int below = __popcll(rows & (((uint64_t)1 << lane) - 1));
+        const int to = rows >> lane & 1 ? below : count + lane - below;
+        f(Group{first, count, mine, __builtin_amdgcn_ds_permute(to * 4, lane)});
+    }
 }
 
-// Eight consecutive elements, of which the first n exist (the others are 0).  Rows may begin at any
-// element: the loads need no alignment.
+__device__ __forceinline__ int32_t rank_of(const LoraArgs &a, int32_t id)
+{
+    const int32_t rank = id < 0 ? 0 : a.ranks ? a.ranks[id] : a.rank;
+    return __builtin_amdgcn_readfirstlane(min(max(rank, 0), a.rank));
+}
+
+// What a lane (row fr, place fg) has of 32 columns: of FP32 adapters' products the four from 4 fg on and the
+// four 16 further on, so that the four lanes of a row ask for 64 bytes of it in one piece (32 bytes a
+// lane side by side asked for every line twice); of 16-bit ones' the eight from 8 fg on, 16 bytes.
+// Rows may begin at any element: the loads need no alignment.
+template <class T> constexpr int kNext = sizeof(T) == 4 ? 16 : 4;     // from the first four to the others
+template <class T> constexpr int kLane = sizeof(T) == 4 ? 4 : 8;      // from lane to lane
+
+template <class T>
+__device__ __forceinline__ int32_t column_of(int e) { return e < 4 ? e : kNext<T> + e - 4; }
+
 template <class T>
 struct Run {
     T v[8];
 };
 
-template <class T>
-__device__ __forceinline__ Run<T> load_run(const T *p, int64_t n)
+// W: the adapters' type.  CHECK: only the first n elements from p on exist; the others are 0.
+template <class W, bool CHECK, class T>
+__device__ __forceinline__ Run<T> load_run(const T *p, int64_t n = 0)
 {
     Run<T> r;
-    if (n >= 8) {
-        memcpy(&r, p, sizeof(r));
+    if (!CHECK) {
+        memcpy(r.v, p, 4 * sizeof(T));
+        memcpy(r.v + 4, p + kNext<W>, 4 * sizeof(T));
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r.v[e] = e < n ? p[e] : T(0);
+        for (int e = 0; e < 8; ++e) r.v[e] = column_of<W>(e) < n ? p[column_of<W>(e)] : T(0);
     }
     return r;
 }
@@ -229,61 +204,99 @@ __device__ __forceinline__ void products(f32x4 (&acc)[MB][NB], const Parts<3> (&
         }
 }
 
-// v of a unit's rows over one part of K, 128 ranks at most.  Eight waves take an eighth of
-// the part each, 32 columns at a time straight from memory into operands (lane fr + 16
-// fg: row fr, columns 8 fg .. 8 fg + 7, whole 128-byte lines of a row), then add their sums up in
-// LDS, in the order of the waves.  MB: row blocks.
+// v of a group's rows over one part of K, 128 ranks at most.  The waves take 32 columns of the part each in
+// turn, straight from memory into operands (Run has which columns a lane takes)
+// and a turn ahead, then add their sums up in LDS, in the order of the waves.
+// MB: row blocks, from row m0 of the group on.  Of one row block the weights are most of what is read, and all
+// are a turn ahead; of more, the rows.
 template <class T, int NB, int MB>
-__device__ __forceinline__ void down(const LoraArgs &a, const Unit &un, int64_t depth, f32x4 (*part)[4][64])
+__device__ __forceinline__ void down(const LoraArgs &a, const Group &un, int m0, int64_t depth, f32x4 (*part)[4][64])
 {
-    const int32_t j0 = blockIdx.z * kGroup, rank = min(un.rank - j0, 16 * NB);
+    constexpr bool FEW = MB == 1 && NB <= 4;
+    constexpr int N2 = NB < 2 || NB > 4 ? 1 : 2;   // weights' blocks at a time (their parts take registers)
+    const int count = min(un.count - m0, 16 * MB);
+    const int32_t j0 = blockIdx.z * kGroup;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), fr = lane & 15, fg = lane / 16;
-    const int64_t run = depth / kDownWaves, k0 = blockIdx.y * depth + wave * run;
-    const int64_t k1 = min(k0 + run, a.K);
-
+    constexpr int64_t stride = 32 * kDownWaves;
+    const int64_t k0 = blockIdx.y * depth + wave * 32, k1 = min((blockIdx.y + 1) * depth, a.K);
     const float *x[MB];
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
-        const int32_t row = __shfl(un.row, mb * 16 + fr < un.count ? mb * 16 + fr : 0);
-        x[mb] = a.x + (int64_t)(un.first + row) * a.ldx;
+        const int32_t row = __shfl(un.row, m0 + (mb * 16 + fr < count ? mb * 16 + fr : 0));
+        x[mb] = a.x + (int64_t)(un.first + row) * a.ldx + kLane<T> * fg;
     }
-    const T *w = static_cast<const T *>(a.a) + ((int64_t)un.id * a.rank + j0) * a.K;
-    constexpr int N2 = NB < 2 || NB > 4 ? 1 : 2;   // weights' blocks at a time (their parts take registers)
+    struct In {
+        Run<float> x[MB];
+        Run<T> w[FEW ? NB : N2];   // all blocks' weights, or the first ones'
+    };
+    // (cut: true_type for the columns that K cuts)
+    auto load_x = [&](In &o, int64_t kk, auto cut) {
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) o.x[mb] = load_run<T, decltype(cut)::value>(x[mb] + kk, a.K - kk - kLane<T> * fg);
+    };
+    const std::false_type whole;
+    const std::true_type cut;
+    const int64_t steps = k1 >= k0 + 32 ? (k1 - k0 - 32) / stride + 1 : 0;   // whole ones; only K's end cuts one
+    In now = {};
+    if (steps > 0) load_x(now, k0, whole);
+    const int32_t rank = min(rank_of(a, un.id) - j0, 16 * NB);
+    if (rank <= 0) return;
+    const T *w = static_cast<const T *>(a.a) + ((int64_t)un.id * a.rank + j0) * a.K + kLane<T> * fg;
+    // ranks that are not there read the last one's weights and are zeroed at their use
+    auto load_w = [&](int nb, int64_t kk, auto cut) {
+        return load_run<T, decltype(cut)::value>(w + (int64_t)min(nb * 16 + fr, rank - 1) * a.K + kk, a.K - kk - kLane<T> * fg);
+    };
+    auto load_ws = [&](In &o, int64_t kk, auto cut) {
+#pragma unroll
+        for (int n = 0; n < (FEW ? NB : N2); ++n)
+            if (n == 0 || n * 16 < rank) o.w[n] = load_w(n, kk, cut);
+    };
     f32x4 acc[NB / N2][MB][N2] = {};
-    auto step = [&](int64_t kk, int64_t left) {   // left: columns from kk + 8 fg on, 8 or more in whole steps
-        const int64_t k = kk + 8 * fg;
-        Run<float> xr[MB];
-        Run<T> wr[2][N2];   // one turn ahead
-        auto load = [&](int nb) {
-#pragma unroll
-            for (int n = 0; n < N2; ++n) {
-                const int32_t j = (nb + n) * 16 + fr;
-                wr[nb / N2 & 1][n] = load_run(w + (int64_t)(j < rank ? j : 0) * a.K + k, j < rank ? left : 0);
-            }
-        };
-        load(0);
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb) xr[mb] = load_run(x[mb] + k, left);
+    auto step = [&](const In &in, int64_t kk, auto cut) {
         Parts<3> xp[MB];
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb) xp[mb] = parts_of_run(xr[mb]);
+        for (int mb = 0; mb < MB; ++mb) xp[mb] = parts_of_run(in.x[mb]);
+        Run<T> wr[N2];
 #pragma unroll
         for (int nb = 0; nb < NB; nb += N2) {
-            if (nb + N2 < NB) load(nb + N2);
+            if (nb > 0 && nb * 16 >= rank) break;
             Parts<kParts<T>> wp[N2];
 #pragma unroll
-            for (int n = 0; n < N2; ++n) wp[n] = parts_of_run(wr[nb / N2 & 1][n]);
+            for (int n = 0; n < N2; ++n) {
+                if (FEW || nb == 0) wr[n] = in.w[nb + n];
+                if ((nb + n + 1) * 16 > rank && (nb + n) * 16 + fr >= rank) wr[n] = Run<T>{};
+                wp[n] = parts_of_run(wr[n]);
+            }
+            if (!FEW && nb + N2 < NB) {
+#pragma unroll
+                for (int n = 0; n < N2; ++n)
+                    if ((nb + N2 + n) * 16 < rank) wr[n] = load_w(nb + N2 + n, kk, cut);
+            }
             products(acc[nb / N2], xp, wp);
         }
     };
-    int64_t kk = k0;
-    for (; kk + 32 <= k1; kk += 32) step(kk, 8);
-    if (kk < k1) step(kk, a.K - kk - 8 * fg);   // (runs are whole 32s: only K's end cuts one)
+    if (steps > 0) load_ws(now, k0, whole);
+#pragma unroll 1
+    for (int64_t i = 0; i < steps; ++i) {   // (the last one loads itself once more)
+        const int64_t kk = k0 + stride * i, after = i + 1 < steps ? kk + stride : kk;
+        In next = {};
+        load_x(next, after, whole);
+        load_ws(next, after, whole);
+        step(now, kk, whole);
+        now = next;
+    }
+    if (k0 + stride * steps < k1) {
+        const int64_t kk = k0 + stride * steps;
+        load_x(now, kk, cut);
+        load_ws(now, kk, cut);
+        step(now, kk, cut);
+    }
 
     const int32_t cols = padded(a.rank);
     float *v = a.v + (int64_t)blockIdx.y * a.tokens * cols;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
+        if (nb * 16 >= rank) break;
         if (nb > 0) __syncthreads();
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) part[wave][mb][lane] = acc[nb / N2][mb][nb % N2];
@@ -292,198 +305,322 @@ __device__ __forceinline__ void down(const LoraArgs &a, const Unit &un, int64_t 
             f32x4 s = part[0][wave][lane];
 #pragma unroll
             for (int q = 1; q < kDownWaves; ++q) s += part[q][wave][lane];
-            const int32_t row = __shfl(un.row, (wave * 16 + fr) & 63);
-            if (wave * 16 + fr < un.count && nb * 16 < rank)
+            const int32_t row = __shfl(un.row, (m0 + wave * 16 + fr) & 63);
+            if (wave * 16 + fr < count)
                 *reinterpret_cast<f32x4 *>(v + (int64_t)(un.first + row) * cols + j0 + nb * 16 + 4 * fg) = s;
         }
     }
 }
 
 template <class T, int NB>
-__global__ void __launch_bounds__(64 * kDownWaves) lora_down_kernel(LoraArgs a, int32_t unit0, int64_t depth)
+__global__ void __launch_bounds__(64 * kDownWaves, NB == 1 ? 3 : 2) lora_down_kernel(LoraArgs a, int32_t wg0, int32_t share, int64_t depth)
 {
     __shared__ f32x4 part[kDownWaves][4][64];
-    const Unit un = unit_of(a, unit0 + blockIdx.x);
-    if (un.count == 0 || un.rank <= (int32_t)blockIdx.z * kGroup) return;
-    if (un.count <= 16)
-        down<T, NB, 1>(a, un, depth, part);
-    else
-        down<T, NB, 4>(a, un, depth, part);
+    const int32_t wg = wg0 + blockIdx.x, tile = __builtin_amdgcn_readfirstlane(wg / share);
+    constexpr int MB = NB <= 4 ? 4 : 2;   // (256 registers)
+    bool again = false;
+    for_groups(a, tile * kTile, wg - tile * share, share, [&](const Group &un) {
+        if (un.id < 0) return;
+        for (int m0 = 0; m0 < un.count; m0 += 16 * MB) {
+            if (again) __syncthreads();   // (of one use of LDS and the next)
+            again = true;
+            if (un.count - m0 <= 16)
+                down<T, NB, 1>(a, un, m0, depth, part);
+            else
+                down<T, NB, MB>(a, un, m0, depth, part);
+        }
+    });
 }
 
-// out = y + s B v for a unit's rows and a strip of columns.  The parts of v are added up in their order and split
-// into LDS; then a wave takes 32 columns at a time (as the rows of the matrix
-// instruction, so that a lane ends up with four columns of a token) and MB row blocks against
-// them.  QB: blocks of 32 ranks, or 0 for ranks above 128, which take one row block
-// at a time.
+// out = y + s B v for a group's rows and a strip of columns.  The parts of v are added up in
+// their order and split into LDS; then a wave takes 32 columns (as the rows of the
+// matrix instruction, so that a lane ends up with four columns of a token) and MB row blocks at a
+// time, y a turn ahead.
+// Of more than 32 rows each half has waves of its own.  QB: blocks of 32 ranks, or
+// 0 for ranks above 128, which take 16 rows at a time.
 template <class T, int QB, int MB>
-__device__ __forceinline__ void up(const LoraArgs &a, const Unit &un, const int32_t *rows, u32x4 *vs, int32_t parts, int32_t strip)
+__device__ __forceinline__ void up(const LoraArgs &a, const Group &un, const int32_t *rows, u32x4 *vs, int32_t rank,
+                                   int32_t parts, int32_t strip, int32_t col)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), fr = lane & 15, fg = lane / 16;
-    const int32_t cols = padded(a.rank), held = padded(un.rank) / 8, qs = QB ? QB : (held + 3) / 4;
+    const int32_t cols = padded(a.rank), qs = QB ? QB : (a.rank + 31) / 32, q_end = (rank + 31) / 32;
+    const int32_t held = padded(rank);
     const int32_t pitch = 3 * 4 * qs + 1;   // 16-byte units of a row: 4 of each part for 32 ranks
     const T *b = static_cast<const T *>(a.b) + (int64_t)un.id * a.N * a.rank;
     const float scale = a.scales ? a.scales[un.id] : 1.0f;
-    const int64_t n_begin = (int64_t)blockIdx.y * strip, n_end = min(a.N, n_begin + strip);
+    const int halves = QB && un.count > 16 * MB ? 2 : 1;
+    const int half = halves == 2 ? wave & 1 : 0, turns = kUpWaves >> (halves - 1);
+    const int32_t N = (int32_t)a.N;   // (below 2^25)
+    const int32_t n_end = (int32_t)min(a.N, ((int64_t)col + 1) * strip);
 
-    for (int m0 = 0; m0 < un.count; m0 += 16 * MB) {
-        const int count = min(un.count - m0, 16 * MB);
+    for (int m0 = 0; m0 < un.count; m0 += 16 * MB * halves) {
+        const int count = min(un.count - m0, 16 * MB * halves);   // rows in LDS
         if (m0 > 0) __syncthreads();
-        for (int i = threadIdx.x; i < count * 4 * qs; i += 64 * kUpWaves) {
-            const int m = i / (4 * qs), j = i - m * 4 * qs;
-            float s[8] = {};
-            if (j < held) {
-                const float *p = a.v + (int64_t)rows[m0 + m] * cols + 8 * j;
-                for (int q = 0; q < parts; ++q, p += (int64_t)a.tokens * cols) {
-                    const f32x4 lo = *reinterpret_cast<const f32x4 *>(p), hi = *reinterpret_cast<const f32x4 *>(p + 4);
+        auto stage = [&] {
+            constexpr int PARTS = MB == 1 ? 4 : 2;
+#pragma unroll 1
+            for (int i = threadIdx.x; i < count * 4 * q_end; i += 64 * kUpWaves) {
+                const int m = i / (4 * q_end), j = i - m * 4 * q_end;
+                float s[8] = {};
+                const int32_t k = j / 4 * 32 + j % 4 * kLane<T>;   // as load_run has them
+                if (k < held) {
+                    const bool both = k + kNext<T> < held;
+                    const float *p = a.v + (int64_t)rows[m0 + m] * cols + k;
+                    for (int q0 = 0; q0 < parts; q0 += PARTS) {   // so many at once; behind the last one it is read again
+                        f32x4 v[PARTS][2];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        s[e] += lo[e];
-                        s[4 + e] += hi[e];
+                        for (int q = 0; q < PARTS; ++q) {
+                            const float *r = p + (int64_t)min(q0 + q, parts - 1) * a.tokens * cols;
+                            v[q][0] = *reinterpret_cast<const f32x4 *>(r);
+                            v[q][1] = *reinterpret_cast<const f32x4 *>(both ? r + kNext<T> : r);
+                        }
+#pragma unroll
+                        for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                s[e] += q0 + q < parts && (e < 4 || both) ? v[q][e / 4][e % 4] : 0.0f;
+                    }
+                }
+                const Parts<3> o = split<3>(s);
+#pragma unroll
+                for (int e = 0; e < 3; ++e) vs[m * pitch + e * 4 * qs + j] = o.p[e];
+            }
+            __syncthreads();
+        };
+        // Results leave the matrix instructions with 16 rows of 64 bytes; whole_lines turns two of them into
+        // 8 rows of 128 bytes, whole lines (half lines: 1.4 times the bytes written).  Those rows of
+        // y and out, and the row of vs
+        int64_t row[MB][2];
+        bool is[MB][2];
+        int at[MB];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            const int block = half * 16 * MB + mb * 16;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int m = block + 8 * h + (fr & 7);
+                is[mb][h] = m < count;
+                row[mb][h] = rows[m0 + (m < count ? m : 0)];
+            }
+            at[mb] = (block + fr < count ? block + fr : 0) * pitch + fg;
+        }
+        const int32_t col4 = 16 * (fr >> 3) + 4 * fg;   // a lane's columns of 32
+        constexpr int AT = QB == 2 ? 2 : 1;   // blocks of ranks read at once
+        struct Out {
+            float v[MB][2][4];
+        };
+        // 32 columns, and where ranks are no whole fours not the last: their loads run on into the next row
+        auto is_whole = [&](int32_t n0) { return n0 + 32 <= N - (a.rank % 4 != 0); };
+        // (what the adapter lacks may be anything, up to the array's ranks in whole fours)
+        auto load_w = [&](Run<T> (&w)[2], int32_t n0, int q, auto whole) {
+            const int32_t j = 32 * q + kLane<T> * fg;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int32_t n = n0 + 16 * h + fr;
+                if (decltype(whole)::value) {
+                    const T *p = b + (int64_t)n * a.rank + j;
+                    w[h] = Run<T>{};
+                    if (j < a.rank) memcpy(w[h].v, p, 4 * sizeof(T));
+                    if (32 * q + kNext<T> < a.rank && j + kNext<T> < a.rank) memcpy(w[h].v + 4, p + kNext<T>, 4 * sizeof(T));
+                } else {
+                    const T *p = b + (int64_t)min(n, N - 1) * a.rank;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int32_t k = j + column_of<T>(e);
+                        const T v = p[min(k, a.rank - 1)];
+                        w[h].v[e] = k < a.rank ? v : T(0);
                     }
                 }
             }
-            const Parts<3> o = split<3>(s);
+        };
+        const std::true_type whole;
+        const std::false_type cut;
+        auto load_y = [&](float (&y)[MB][2][4], int32_t n0, auto whole) {
 #pragma unroll
-            for (int e = 0; e < 3; ++e) vs[m * pitch + e * 4 * qs + j] = o.p[e];
-        }
-        __syncthreads();
-        int64_t row[MB];   // of y and out
-        int at[MB];        // of vs
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb) {
-            const int m = mb * 16 + fr < count ? mb * 16 + fr : 0;
-            row[mb] = rows[m0 + m];
-            at[mb] = m * pitch + fg;
-        }
-
-        for (int64_t n0 = n_begin + wave * 32; n0 < n_end; n0 += 32 * kUpWaves) {
-            f32x4 acc[MB][2] = {};
-            float y[MB][2][4];
-            Run<T> br[2][2];
-            auto fragment = [&](int q, Run<T> (&f)[2]) {
+            for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int64_t n = n0 + 16 * h + fr;
-                    const int32_t j = 32 * q + 8 * fg;
-                    f[h] = load_run(b + (n < a.N ? n : 0) * a.rank + j, un.rank - j);
+                    const int32_t n = n0 + col4;
+                    const float *p = a.y + row[mb][h] * a.ldy + n;
+                    if (decltype(whole)::value) {
+                        memcpy(y[mb][h], p, 16);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[mb][h][e] = p[min(n + e, N - 1) - n];
+                    }
                 }
-            };
-            auto product = [&](int q, const Run<T> (&f)[2]) {
+        };
+        // (addresses are made from n0 in each turn: kept from turn to turn they take more registers
+        // than there are)
+        auto load = [&](Out &o, int32_t n0) {
+            asm volatile("" : "+s"(n0));
+            if (is_whole(n0))
+                load_y(o.v, n0, whole);
+            else
+                load_y(o.v, n0, cut);
+        };
+        auto weights = [&](Run<T> (&w)[2], int32_t n0, int q) {
+            asm volatile("" : "+s"(n0));
+            if (is_whole(n0))
+                load_w(w, n0, q, whole);
+            else
+                load_w(w, n0, q, cut);
+        };
+        auto columns = [&](const Out &y, Run<T> (&w)[AT][2], int32_t n0) {
+            asm volatile("" : "+s"(n0));
+            f32x4 acc[2][MB][1] = {};
+            auto turn = [&](int q, Run<T> (&w)[2]) {
                 Parts<3> vp[MB];
 #pragma unroll
                 for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
                     for (int e = 0; e < 3; ++e) vp[mb].p[e] = vs[at[mb] + e * 4 * qs + 4 * q];
-                const Parts<kParts<T>> bp[2] = {parts_of_run(f[0]), parts_of_run(f[1])};
-                products(acc, vp, bp);
-            };
-            fragment(0, br[0]);
+                const int32_t j = 32 * q + kLane<T> * fg;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < 2; ++h) {   // (one after the other: both halves' parts take more registers than there are)
+                    if ((rank < a.rank || a.rank % 4 != 0) && 32 * q + 32 > rank) {
 #pragma unroll
-                for (int mb = 0; mb < MB; ++mb) {
-                    const int64_t n = n0 + 16 * h + 4 * fg;
-                    const float *p = a.y + row[mb] * a.ldy + n;
-                    if (n + 4 <= a.N) {
-                        memcpy(y[mb][h], p, 16);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) y[mb][h][e] = n + e < a.N ? p[e] : 0.0f;
+                        for (int e = 0; e < 8; ++e) w[h].v[e] = j + column_of<T>(e) < rank ? w[h].v[e] : T(0);
                     }
+                    const Parts<kParts<T>> wp[1] = {parts_of_run(w[h])};
+                    products(acc[h], vp, wp);
                 }
-            if (QB == 1) {
-                product(0, br[0]);
-            } else {
+            };
+            turn(0, w[0]);
+            if (QB == 2) {
+                if (q_end > 1) turn(1, w[AT - 1]);
+            } else if (QB != 1) {
 #pragma unroll 1
-                for (int q = 0; q < qs; q += 2) {   // a block of ranks ahead
-                    if (q + 1 < qs) fragment(q + 1, br[1]);
-                    product(q, br[0]);
-                    if (q + 1 >= qs) break;
-                    if (q + 2 < qs) fragment(q + 2, br[0]);
-                    product(q + 1, br[1]);
+                for (int q = 1; q < q_end; ++q) {
+                    weights(w[0], n0, q);
+                    turn(q, w[0]);
                 }
             }
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int mb = 0; mb < MB; ++mb) {
+                f32x4 line[2];
+                whole_lines(acc[0][mb][0], acc[1][mb][0], fr, line[0], line[1]);
 #pragma unroll
-                for (int mb = 0; mb < MB; ++mb) {
-                    if (mb * 16 + fr >= count) continue;
-                    const int64_t n = n0 + 16 * h + 4 * fg;
-                    float *o = a.out + row[mb] * a.ldo + n;
+                for (int h = 0; h < 2; ++h) {
+                    if (!is[mb][h]) continue;
+                    const int32_t n = n0 + col4;
+                    float *o = a.out + row[mb][h] * a.ldo + n;
                     float r[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) r[e] = fmaf(scale, acc[mb][h][e], y[mb][h][e]);
-                    if (n + 4 <= a.N) {
+                    for (int e = 0; e < 4; ++e) r[e] = fmaf(scale, line[h][e], y.v[mb][h][e]);
+                    if (n0 + 32 <= N) {
                         memcpy(o, r, sizeof(r));
                     } else {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (n + e < a.N) o[e] = r[e];
+                            if (n + e < N) o[e] = r[e];
                     }
                 }
+            }
+        };
+        const int32_t stride = 32 * turns;
+        int32_t n0 = col * strip + (wave >> (halves - 1)) * 32;
+        Out now = {};
+        if (n0 < n_end) load(now, n0);
+        stage();
+#pragma unroll 1
+        for (; n0 < n_end; n0 += stride) {
+            Run<T> w[AT][2];
+            weights(w[0], n0, 0);
+            if (QB == 2 && q_end > 1) weights(w[AT - 1], n0, 1);
+            Out next = {};
+            if (n0 + stride < n_end) load(next, n0 + stride);
+            columns(now, w, n0);
+            now = next;
         }
     }
 }
 
 template <class T, int QB>
-__global__ void __launch_bounds__(64 * kUpWaves, 2) lora_up_kernel(LoraArgs a, int32_t unit0, int32_t parts, int32_t strip)
+__global__ void __launch_bounds__(64 * kUpWaves, QB == 1 ? 3 : 2)
+lora_up_kernel(LoraArgs a, int64_t wg0, int32_t share, int32_t parts, int32_t strip)
 {
     extern __shared__ u32x4 vs[];
     __shared__ int32_t rows[kTile];
-    const Unit un = unit_of(a, unit0 + blockIdx.x);
-    if (un.count == 0 || (un.rank == 0 && a.out == a.y)) return;
-    if (threadIdx.x < kTile) rows[threadIdx.x] = un.first + un.row;
-    __syncthreads();
-    if (un.rank == 0) {   // out is y
-        const int64_t n_begin = (int64_t)blockIdx.y * strip, n_end = min(a.N, n_begin + strip);
-        for (int m = 0; m < un.count; ++m)
-            for (int64_t n = n_begin + threadIdx.x; n < n_end; n += 64 * kUpWaves)
-                a.out[rows[m] * a.ldo + n] = a.y[rows[m] * a.ldy + n];
-        return;
-    }
-    if (QB == 0 || un.count <= 16)
-        up<T, QB, 1>(a, un, rows, vs, parts, strip);
-    else
-        up<T, QB, QB ? 4 : 1>(a, un, rows, vs, parts, strip);
+    const int32_t strips = (int32_t)((a.N + strip - 1) / strip);
+    const int64_t wgi = wg0 + blockIdx.x;
+    // (divisions are made by vector instructions, even of scalars)
+    const int32_t wg = __builtin_amdgcn_readfirstlane((int32_t)(wgi / strips));
+    const int32_t col = (int32_t)(wgi - (int64_t)wg * strips);
+    const int32_t tile = __builtin_amdgcn_readfirstlane(wg / share);
+    bool again = false;
+    for_groups(a, tile * kTile, wg - tile * share, share, [&](const Group &un) {
+        if (un.id < 0 && a.out == a.y) return;
+        if (again) __syncthreads();   // (of one use of LDS and the next)
+        again = true;
+        if (threadIdx.x < kTile) rows[threadIdx.x] = un.first + un.row;
+        __syncthreads();
+        const int32_t rank = rank_of(a, un.id);
+        if (rank == 0) {   // out is y
+            const int64_t n_begin = (int64_t)col * strip, n_end = min(a.N, n_begin + strip);
+            if (a.out != a.y)
+                for (int m = 0; m < un.count; ++m)
+                    for (int64_t n = n_begin + threadIdx.x; n < n_end; n += 64 * kUpWaves)
+                        a.out[rows[m] * a.ldo + n] = a.y[rows[m] * a.ldy + n];
+            return;
+        }
+        if (QB == 0 || un.count <= 16)
+            up<T, QB, 1>(a, un, rows, vs, rank, parts, strip, col);
+        else
+            up<T, QB, QB ? 2 : 1>(a, un, rows, vs, rank, parts, strip, col);
+    });
+}
+
+// Workgroups that share a tile: as many as adapters can meet there where there are few tiles (64 tokens that
+// decode); one where there are many (prompts, with one adapter a tile as a rule).
+int64_t shares(const LoraArgs &a)
+{
+    const int64_t tiles = (a.tokens + kTile - 1) / kTile;
+    const int64_t met = std::min({(int64_t)kTile, (int64_t)a.tokens, (int64_t)a.seqs, (int64_t)a.adapters + 1});
+    return std::max<int64_t>(1, std::min(met, 64 / tiles));
 }
 
 template <class T, int NB>
-hipError_t launch_down(const LoraArgs &a, int64_t units, hipStream_t stream)
+hipError_t launch_down(const LoraArgs &a, hipStream_t stream)
 {
-    return in_parts(units, [&](int64_t at, unsigned n) {
-        lora_down_kernel<T, NB><<<dim3(n, (unsigned)parts_of(a.K), (unsigned)((a.rank + kGroup - 1) / kGroup)),
-                                  dim3(64 * kDownWaves), 0, stream>>>(a, (int32_t)at, part_depth(a.K));
+    const int64_t tiles = (a.tokens + kTile - 1) / kTile, parts = parts_of(a.K);
+    const int64_t share = shares(a);
+    return in_parts(tiles * share, [&](int64_t at, unsigned n) {
+        lora_down_kernel<T, NB><<<dim3(n, (unsigned)parts, (unsigned)((a.rank + kGroup - 1) / kGroup)), dim3(64 * kDownWaves),
+                                  0, stream>>>(a, (int32_t)at, (int32_t)share, part_depth(a.K));
     });
 }
 
 template <class T, int QB>
-hipError_t launch_up(const LoraArgs &a, int64_t units, hipStream_t stream)
+hipError_t launch_up(const LoraArgs &a, hipStream_t stream)
 {
+    const int64_t tiles = (a.tokens + kTile - 1) / kTile;
+    const int64_t share = shares(a);
     int64_t strip = 32 * kUpWaves;
-    while ((a.N + strip - 1) / strip > 32768) strip *= 2;
+    auto strips = [&] { return (a.N + strip - 1) / strip; };
+    while (tiles * share * strips() > kUpWorkgroups && strip < 1024) strip *= 2;
+    while (strips() > 32768) strip *= 2;
     const int32_t rows = QB ? (a.tokens < kTile ? a.tokens : kTile) : 16, qs = QB ? QB : (a.rank + 31) / 32;
     const size_t lds = (size_t)rows * (3 * 4 * qs + 1) * sizeof(u32x4);
-    return in_parts(units, [&](int64_t at, unsigned n) {
-        lora_up_kernel<T, QB><<<dim3(n, (unsigned)((a.N + strip - 1) / strip)), dim3(64 * kUpWaves), lds, stream>>>(
-            a, (int32_t)at, parts_of(a.K), (int32_t)strip);
+    return in_parts(tiles * share * strips(), [&](int64_t at, unsigned n) {
+        lora_up_kernel<T, QB><<<dim3(n), dim3(64 * kUpWaves), lds, stream>>>(
+            a, at, (int32_t)share, parts_of(a.K), (int32_t)strip);
     });
 }
 
 template <class T>
 hipError_t launch(const LoraArgs &a, hipStream_t stream)
 {
-    const int64_t units = units_of(a.cu != nullptr, a.tokens, a.seqs);
     const int blocks = a.rank < kGroup ? (a.rank + 15) / 16 : kGroup / 16;
-    hipError_t err = blocks == 1   ? launch_down<T, 1>(a, units, stream)
-                     : blocks == 2 ? launch_down<T, 2>(a, units, stream)
-                     : blocks <= 4 ? launch_down<T, 4>(a, units, stream)
-                                   : launch_down<T, 8>(a, units, stream);
+    hipError_t err = blocks == 1   ? launch_down<T, 1>(a, stream)
+                     : blocks == 2 ? launch_down<T, 2>(a, stream)
+                     : blocks <= 4 ? launch_down<T, 4>(a, stream)
+                                   : launch_down<T, 8>(a, stream);
     if (err != hipSuccess) return err;
-    return a.rank > kGroup ? launch_up<T, 0>(a, units, stream)
-           : a.rank <= 32  ? launch_up<T, 1>(a, units, stream)
-           : a.rank <= 64  ? launch_up<T, 2>(a, units, stream)
-                           : launch_up<T, 4>(a, units, stream);
+    return a.rank > kGroup ? launch_up<T, 0>(a, stream)
+           : a.rank <= 32  ? launch_up<T, 1>(a, stream)
+           : a.rank <= 64  ? launch_up<T, 2>(a, stream)
+                           : launch_up<T, 4>(a, stream);
 }
 
 }  // namespace

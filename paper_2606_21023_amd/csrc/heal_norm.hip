@@ -153,12 +153,16 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) norm_kernel(NormArgs a, int
     if (p.x) {
         float x[U][4], g[U][4];
         L::load(p.x, a.dim, x);
-        if (a.post.weight) L::load(a.post.weight, a.dim, w);
-        if (a.post.bias) L::load(a.post.bias, a.dim, b);
-        if (p.gate && a.gate_col) L::load(p.gate, a.dim, g);
+        auto rest = [&] {
+            if (a.post.weight) L::load(a.post.weight, a.dim, w);
+            if (a.post.bias) L::load(a.post.bias, a.dim, b);
+            if (p.gate && a.gate_col) L::load(p.gate, a.dim, g);
+        };
+        if (U <= 4) rest();   // (longer rows' would not stay in registers)
         const double f = (double)a.scale * (p.gate && !a.gate_col ? (double)*p.gate : 1.0);
         Stats st = {0.0, 1.0};
         if (a.post.weight) st = L::stats_of(a.post, a.dim, x, a.post.centred ? (double)*p.x : 0.0, part[0]);
+        if (U > 4) rest();
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -169,8 +173,10 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) norm_kernel(NormArgs a, int
             }
     }
     if (p.out) {
-        L::load(a.pre.weight, a.dim, w);
-        if (a.pre.bias) L::load(a.pre.bias, a.dim, b);
+        if (U <= 4) {
+            L::load(a.pre.weight, a.dim, w);
+            if (a.pre.bias) L::load(a.pre.bias, a.dim, b);
+        }
         // the pivot: the row's first element, from the thread that has it
         double pivot = 0.0;
         if (a.pre.centred) {
@@ -185,6 +191,10 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) norm_kernel(NormArgs a, int
         }
         const Stats st = L::stats_of(a.pre, a.dim, h, pivot, part[1]);
         float o[U][4];
+        if (U > 4) {
+            L::load(a.pre.weight, a.dim, w);
+            if (a.pre.bias) L::load(a.pre.bias, a.dim, b);
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
