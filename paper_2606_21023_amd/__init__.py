@@ -805,9 +805,14 @@ def _kv_pool(pool, table):
     return rows, stride[0] if rows > 1 else cols or 1, cols
 
 
+def _kv_ints_new(pool, n):
+    like = pool.refs
+    return like.new_empty(n) if type(like) is torch.Tensor else torch.empty(n, dtype=torch.int32, device=pool.device)
+
+
 def _kv_scratch(pool, size):
     """size bytes of workspace beside the pool, or None."""
-    return torch.empty((size + 3) // 4, dtype=torch.int32, device=pool.device) if size > 0 else None
+    return _kv_ints_new(pool, (size + 3) // 4) if size > 0 else None
 
 
 def heal_kv_release(pool, table, lens):
@@ -839,13 +844,15 @@ def heal_kv_reserve(pool, tokens, table, lens, cu=None, missing=None):
         cu = _kv_list(pool, cu, "cu", rows + 1)
     elif tokens != rows:
         raise HealError("%d tokens of %d sequences need cu" % (tokens, rows))
+    missing_at = None
     if missing is None:
-        missing = torch.empty(1, dtype=torch.int32, device=pool.device)
+        missing = _kv_ints_new(pool, 1)
+        missing_at = missing.data_ptr()
     batch = _CBatch(rows, tokens, cu, _kv_list(pool, lens, "lens", rows), None, 1, 0, None)
     ref, L = ctypes.byref(batch), _lib or lib()
     size = L.heal_kv_reserve_workspace(pool._ref, ref)
     space = _kv_scratch(pool, size)
-    _check(L.heal_kv_reserve(pool._ref, ref, table.data_ptr(), ld, cols, _kv_list(pool, missing, "missing", 1),
+    _check(L.heal_kv_reserve(pool._ref, ref, table.data_ptr(), ld, cols, missing_at or _kv_list(pool, missing, "missing", 1),
                              space.data_ptr() if space is not None else None, max(size, 0), _stream()),
            "heal_kv_reserve")
     return missing
@@ -860,7 +867,8 @@ def heal_kv_compact(pool, table, src=None, dst=None, count=None):
 
     def ints(t, name, n):
         if t is None:
-            t = torch.empty(n, dtype=torch.int32, device=pool.device)
+            t = _kv_ints_new(pool, n)
+            return t, t.data_ptr()
         return t, _kv_list(pool, t, name, n)
     src, at_src = ints(src, "src", most)
     dst, at_dst = ints(dst, "dst", most)
@@ -912,6 +920,12 @@ class _CBank(ctypes.Structure):
 
 def _norm_rows(t, name, shape, index):
     """A float32 tensor of that shape (2-D or 3-D); its address and two strides."""
+    try:
+        stride = t.stride()
+        if (t.dtype is torch.float32 and t.shape == shape and t.get_device() == index and stride[-1] == 1):
+            return t.data_ptr(), stride[0], stride[1] if len(shape) == 3 else 0
+    except AttributeError:
+        pass
     got, stride = _tensor(t, name, torch.float32, len(shape))
     if got != shape:
         raise HealError("%s has shape %s, expected %s" % (name, tuple(got), tuple(shape)))
@@ -923,6 +937,11 @@ def _norm_rows(t, name, shape, index):
 def _norm_vector(t, name, dim, index):
     if t is None:
         return None
+    try:
+        if t.dtype is torch.float32 and t.shape == (dim,) and t.get_device() == index and t.stride(0) == 1:
+            return t.data_ptr()
+    except AttributeError:
+        pass
     (n,), _ = _tensor(t, name, torch.float32, 1)
     if n != dim or t.get_device() != index:
         raise HealError("%s must be a vector of %d beside h" % (name, dim))
@@ -934,8 +953,14 @@ def _norm_spec(weight, bias, name, dim, index, eps, centred):
         if bias is not None:
             raise HealError("%s_bias without %s" % (name, name))
         return None
-    return ctypes.byref(_CNorm(_norm_vector(weight, name, dim, index), _norm_vector(bias, name + "_bias", dim, index),
-                               eps, 1 if centred else 0))
+    return ctypes.byref(_CNorm(_norm_vector(weight, name, dim, index),
+                               None if bias is None else _norm_vector(bias, name + "_bias", dim, index), eps,
+                               1 if centred else 0))
+
+
+def _like(t, shape):
+    """A new float32 tensor beside t."""
+    return t.new_empty(shape) if type(t) is torch.Tensor else torch.empty(shape, dtype=torch.float32, device=t.device)
 
 
 def heal_block_norm(h, x=None, post=None, gate=None, scale=1.0, pre=None, eps=1e-6, centred=False, post_bias=None,
@@ -967,22 +992,26 @@ def heal_block_norm(h, x=None, post=None, gate=None, scale=1.0, pre=None, eps=1e
         if gate.get_device() != index or any(a != b and a != 1 for a, b in zip(got, shape)):
             raise HealError("gate %s does not broadcast to h %s" % (tuple(got), tuple(shape)))
         g = (gate.data_ptr(), gs[0] if got[0] > 1 else 0, gs[1] if wide and got[1] > 1 else 0, 1 if got[-1] > 1 else 0)
-    specs = [_norm_spec(post, post_bias, "post", dim, index, eps, centred),
-             _norm_spec(pre, pre_bias, "pre", dim, index, eps, centred)]
+    spec_post = _norm_spec(post, post_bias, "post", dim, index, eps, centred)
+    spec_pre = _norm_spec(pre, pre_bias, "pre", dim, index, eps, centred)
     ho_at = out_at = (None, 0, 0)
     if x is not None:
         if h_out is None:
-            h_out = torch.empty(shape, dtype=torch.float32, device=h.device)
-        ho_at = _norm_rows(h_out, "h_out", shape, index)
+            h_out = _like(h, shape)
+            ho_at = (h_out.data_ptr(), *h_out.stride()[:2])
+        else:
+            ho_at = _norm_rows(h_out, "h_out", shape, index)
     if pre is not None:
         if out is None:
-            out = torch.empty(shape, dtype=torch.float32, device=h.device)
-        out_at = _norm_rows(out, "out", shape, index)
+            out = _like(h, shape)
+            out_at = (out.data_ptr(), *out.stride()[:2])
+        else:
+            out_at = _norm_rows(out, "out", shape, index)
     elif out is not None:
         raise HealError("out without pre")
     _check((_lib or lib()).heal_block_norm(
-        shape[0], shape[1] if wide else 1, dim, h.data_ptr(), stride[0], stride[1] if wide else 0, *x_at, specs[0], *g,
-        scale, specs[1], *ho_at, *out_at, _stream()), "heal_block_norm")
+        shape[0], shape[1] if wide else 1, dim, h.data_ptr(), stride[0], stride[1] if wide else 0, *x_at, spec_post, *g,
+        scale, spec_pre, *ho_at, *out_at, _stream()), "heal_block_norm")
     return (h if x is None else h_out), out
 
 
@@ -1025,6 +1054,22 @@ class LoraBank:
         raise HealError("a LoraBank keeps the addresses of its arrays: %s stays" % name)
 
 
+def _lora_rows(bank, t, name, cols):
+    """A float32 (tokens, cols) tensor on the bank's device; its shape and row stride."""
+    try:
+        shape, stride = t.shape, t.stride()
+        if (t.dtype is torch.float32 and t.get_device() == bank._index and len(shape) == 2 and shape[1] == cols
+                and stride[1] == 1):
+            return shape, stride[0] if shape[0] > 1 else cols
+    except AttributeError:
+        pass
+    shape, stride = _tensor(t, name, torch.float32, 2)
+    _kv_on(bank, t, name)
+    if shape[1] != cols:
+        raise HealError("%s has shape %s for adapters of %d by %d" % (name, tuple(shape), bank.K, bank.N))
+    return shape, _ld(shape, stride)
+
+
 def heal_lora_add(y, x, bank, ids, cu=None, out=None):
     """out = y + s B (A x) with the adapter of each token's sequence.
 
@@ -1036,15 +1081,17 @@ def heal_lora_add(y, x, bank, ids, cu=None, out=None):
         raise HealError("bank must be a LoraBank")
     if _device() != bank._index:
         raise HealError("the adapters are on %s, the current device is another" % bank.device)
-    shape, x_stride = _tensor(x, "x", torch.float32, 2)
-    y_shape, y_stride = _tensor(y, "y", torch.float32, 2)
+    shape, x_ld = _lora_rows(bank, x, "x", bank.K)
     tokens = shape[0]
-    if shape[1] != bank.K or tuple(y_shape) != (tokens, bank.N):
+    y_shape, y_ld = _lora_rows(bank, y, "y", bank.N)
+    if y_shape[0] != tokens:
         raise HealError("x %s and y %s for adapters of %d by %d" % (tuple(shape), tuple(y_shape), bank.K, bank.N))
-    out, o_stride = _output(out, y, (tokens, bank.N))
-    for name, t in (("x", x), ("y", y), ("out", out)):
-        if t.get_device() != bank._index:
-            raise HealError("%s is on %s, the adapters on %s" % (name, t.device, bank.device))
+    if out is None:
+        out, o_ld = _like(y, y_shape), bank.N
+    else:
+        o_shape, o_ld = _lora_rows(bank, out, "out", bank.N)
+        if o_shape[0] != tokens:
+            raise HealError("out has shape %s, expected %s" % (tuple(o_shape), tuple(y_shape)))
     seqs = len(ids)
     ids = _kv_list(bank, ids, "ids", seqs)
     if cu is not None:
@@ -1055,8 +1102,7 @@ def heal_lora_add(y, x, bank, ids, cu=None, out=None):
         return out
     L = _lib or lib()
     size = L.heal_lora_workspace(bank._ref, tokens)
-    space = torch.empty((size + 3) // 4, dtype=torch.float32, device=bank.device) if size > 0 else None
-    _check(L.heal_lora_add(bank._ref, tokens, seqs, cu, ids, x.data_ptr(), _ld(shape, x_stride), y.data_ptr(),
-                           _ld(y_shape, y_stride), out.data_ptr(), _ld(y_shape, o_stride),
+    space = _like(y, (size + 3) // 4) if size > 0 else None
+    _check(L.heal_lora_add(bank._ref, tokens, seqs, cu, ids, x.data_ptr(), x_ld, y.data_ptr(), y_ld, out.data_ptr(), o_ld,
                            space.data_ptr() if size > 0 else None, max(size, 0), _stream()), "heal_lora_add")
     return out

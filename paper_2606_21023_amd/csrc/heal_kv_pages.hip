@@ -63,8 +63,9 @@ kv_fork_kernel(KvPages p, const int32_t *parents, const int32_t *children, int32
 
 // ---- reserve ---------------------------------------------------------------------
 
-// Units of a call whose state one workgroup keeps in LDS, and sequences whose cu it does.
-constexpr int kSmallUnits = 2048;
+// Units of a call that one workgroup has a thread each for, and sequences whose cu it keeps in LDS.
+constexpr int kSmallUnits = kWide;
+constexpr int kSlots = 2 * kSmallUnits;      // of the table of their blocks
 constexpr int32_t kMark = -2147483647 - 1;   // kMark + unit: the unit keeps the block
 
 // The place of the threads with `mine` among all of the workgroup's, counted on from
@@ -121,25 +122,119 @@ __device__ __forceinline__ Unit unit_of(const KvSeqs &b, int B, int32_t u, F cu)
     return Unit{i, u >= 0 && blk <= t.last && blk < b.cols ? blk : -1};
 }
 
-// One workgroup.  Every touched entry takes one off the count of its block; where the
-// count comes to 0 all holders are here, and the lowest unit of them marks the block as
+// The first `need` free blocks into fresh, 4096 counts a turn, the next turn's on the way; returns how many
+// there are, or more than need.
+__device__ __forceinline__ int32_t find_free(const KvPages &p, int32_t need, int32_t *fresh, int32_t *part)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    const uint64_t lower = ((uint64_t)1 << lane) - 1;
+    auto load = [&](int64_t at) {
+        u32x4 r = {1, 1, 1, 1};
+        if (at + 4 <= p.blocks) {
+            __builtin_memcpy(&r, p.refs + at, sizeof(r));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (at + j < p.blocks) r[j] = p.refs[at + j];
+        }
+        return r;
+    };
+    int32_t found = 0;
+    int turn = 0;
+    u32x4 r = load(threadIdx.x * 4);
+    for (int64_t p0 = 0; p0 < p.blocks && found < need; p0 += 4 * kWide, turn ^= 1) {
+        const int64_t at = p0 + threadIdx.x * 4;
+        const u32x4 next = load(at + 4 * kWide);
+        int32_t place = 0, all = 0;
+        bool free[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            free[j] = (int32_t)r[j] <= 0 && (int32_t)r[j] > kMark / 2;
+            const uint64_t b = __ballot(free[j]);
+            place += __popcll(b & lower);
+            all += __popcll(b);
+        }
+        if (lane == 0) part[32 * turn + wave] = all;
+        __syncthreads();
+        place += found;
+#pragma unroll
+        for (int w = 0; w < kWide / 64; ++w) {
+            place += w < wave ? part[32 * turn + w] : 0;
+            found += part[32 * turn + w];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (free[j] && place < need) fresh[place] = (int32_t)(at + j);
+            place += free[j];
+        }
+        r = next;
+    }
+    return found;
+}
+
+// Up to 1024 units, one workgroup, a thread each.  The touched blocks meet in a table in LDS, which counts
+// their entries and keeps the lowest unit of each; so counts are read once and written once, and
+// nothing is written where the free blocks do not suffice.
+__global__ void __launch_bounds__(kWide) kv_reserve_kernel(KvPages p, KvSeqs b, int32_t units, int32_t *missing)
+{
+    __shared__ int32_t s_cu[kSmallUnits + 1], key[kSlots], count[kSlots], first[kSlots], fresh[kSmallUnits], part[64];
+    const int32_t u = threadIdx.x;
+    const bool staged = b.cu && b.seqs <= kSmallUnits;
+    if (staged)
+        for (int32_t i = u; i <= b.seqs; i += kWide) s_cu[i] = kv_first(b, i);
+    for (int32_t i = u; i < kSlots; i += kWide) {
+        key[i] = -1;
+        count[i] = 0;
+        first[i] = kSmallUnits;
+    }
+    __syncthreads();
+    auto cu = [&](int32_t i) { return staged ? s_cu[i] : kv_first(b, i); };
+    Unit at = {0, -1};
+    int32_t *entry = nullptr, page = -1, was = 0, slot = 0;
+    if (u < units) at = unit_of(b, p.block, u, cu);
+    if (at.block >= 0) {
+        entry = p.table + at.seq * p.table_ld + at.block;
+        page = *entry;
+        if (is_page(p, page)) was = p.refs[page];
+        if (was >= 1) {
+            slot = (uint32_t)page * 2654435761u >> 21;   // (of 2048; at most half of them are taken)
+            for (;;) {
+                const int32_t old = atomicCAS(&key[slot], -1, page);
+                if (old == -1 || old == page) break;
+                slot = (slot + 1) % kSlots;
+            }
+            atomicAdd(&count[slot], 1);
+            atomicMin(&first[slot], u);
+        }
+    }
+    __syncthreads();
+    const bool leads = was >= 1 && first[slot] == u, all_here = was >= 1 && count[slot] >= was;
+    const bool take = at.block >= 0 && !(leads && all_here);
+    int32_t need = 0;
+    const int32_t place = place_of(take, need, part);
+    __syncthreads();
+    const int32_t found = need > 0 ? find_free(p, need, fresh, part) : 0;
+    if (u == 0) *missing = found < need ? need - found : 0;
+    if (found < need) return;
+    __syncthreads();
+    if (leads) p.refs[page] = all_here ? 1 : was - count[slot];
+    if (take) {
+        *entry = fresh[place];
+        p.refs[fresh[place]] = 1;
+    }
+}
+
+// More units: one workgroup with its state in the workspace.  Every touched entry takes one off the count of its
+// block; where the count comes to 0 all holders are here, and the lowest unit of them marks the block as
 // kept.  So an entry needs a new block unless its unit is in the mark.  Nothing but
 // counts of touched blocks has changed by then, and they are put back if the
-// free blocks do not suffice.  Free blocks are counted from the front until there are enough.
-template <bool SMALL>
-__global__ void __launch_bounds__(kWide) kv_reserve_kernel(KvPages p, KvSeqs b, int32_t units, int32_t *ws, int32_t *missing)
+// free blocks do not suffice.
+__global__ void __launch_bounds__(kWide) kv_reserve_many_kernel(KvPages p, KvSeqs b, int32_t units, int32_t *ws, int32_t *missing)
 {
-    __shared__ int32_t s_state[SMALL ? 3 * kSmallUnits : 1], s_cu[SMALL ? kSmallUnits + 1 : 1], part[64];
-    int32_t *pages = SMALL ? s_state : ws;
-    int32_t *was = SMALL ? s_state + kSmallUnits : ws + units;
-    int32_t *fresh = SMALL ? s_state + 2 * kSmallUnits : ws + 2 * (int64_t)units;
+    __shared__ int32_t part[64];
+    int32_t *pages = ws, *was = ws + units, *fresh = ws + 2 * (int64_t)units;
     const int tid = threadIdx.x;
-    const bool staged = SMALL && b.cu && b.seqs <= kSmallUnits;
-    if (staged) {
-        for (int32_t i = tid; i <= b.seqs; i += kWide) s_cu[i] = kv_first(b, i);
-        __syncthreads();
-    }
-    auto cu = [&](int32_t i) { return staged ? s_cu[i] : kv_first(b, i); };
+    auto cu = [&](int32_t i) { return kv_first(b, i); };
     auto load = [](const int32_t *q) { return __hip_atomic_load(q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
 
     // (-2: no block; -1: an entry that holds nothing)
@@ -172,12 +267,9 @@ __global__ void __launch_bounds__(kWide) kv_reserve_kernel(KvPages p, KvSeqs b, 
         const bool keep = page >= 0 && load(p.refs + page) == kMark + u;
         (void)place_of(page != -2 && !keep, need, part + 32 * turn);
     }
-    int32_t found = 0;   // free blocks
-    for (int64_t p0 = 0; p0 < p.blocks && found < need; p0 += kWide, turn ^= 1) {
-        const bool free = p0 + tid < p.blocks && p.refs[p0 + tid] <= 0 && p.refs[p0 + tid] > kMark / 2;
-        const int32_t at = place_of(free, found, part + 32 * turn);
-        if (free && at < need) fresh[at] = (int32_t)(p0 + tid);
-    }
+    __syncthreads();
+    // (counts that this kernel has changed are no free blocks', before or after)
+    const int32_t found = need > 0 ? find_free(p, need, fresh, part) : 0;
     if (tid == 0) *missing = found < need ? need - found : 0;
     const bool fine = found >= need;
     __threadfence();
@@ -391,9 +483,9 @@ hipError_t launch_kv_reserve(const KvPages &p, const KvSeqs &b, int64_t units, v
 {
     int32_t *ws = static_cast<int32_t *>(workspace);
     if (units <= kSmallUnits)
-        kv_reserve_kernel<true><<<dim3(1), dim3(kWide), 0, stream>>>(p, b, (int32_t)units, ws, missing);
+        kv_reserve_kernel<<<dim3(1), dim3(kWide), 0, stream>>>(p, b, (int32_t)units, missing);
     else
-        kv_reserve_kernel<false><<<dim3(1), dim3(kWide), 0, stream>>>(p, b, (int32_t)units, ws, missing);
+        kv_reserve_many_kernel<<<dim3(1), dim3(kWide), 0, stream>>>(p, b, (int32_t)units, ws, missing);
     return hipGetLastError();
 }
 

@@ -191,9 +191,9 @@ def test_counts_that_do_not_agree():
 
 
 @pytest.mark.parametrize("tokens", [1, 40])
-@pytest.mark.parametrize("seqs", [2047, 2048, 2049, 5000])
+@pytest.mark.parametrize("seqs", [1023, 1024, 1025, 2500, 5000])
 def test_reserve_of_many_sequences(seqs, tokens):
-    """More work units, and sequences, than one workgroup keeps in LDS."""
+    """As many work units as one workgroup has threads, and more."""
     w = World(seqs, 4, 3 * seqs + 50, seed=seqs, fill=0.2)
     lens = [n + tokens for n in w.lens]
     announce("reserve %d x %d" % (seqs, tokens))

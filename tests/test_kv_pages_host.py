@@ -108,7 +108,7 @@ def test_workspace():
 
     def reserve(pool=None, **kw):
         return L.heal_kv_reserve_workspace(ctypes.byref(pool or _pool()), ctypes.byref(_batch(**kw)))
-    assert reserve() == 0 and reserve(cu=None, tokens=2000, seqs=2000) == 0
+    assert reserve() == 0 and reserve(cu=None, tokens=1024, seqs=1024) == 0
     assert reserve(cu=None, tokens=5000, seqs=5000) == 12 * 5000
     assert reserve(tokens=640000, seqs=3) == (12 * 10006 + 15) // 16 * 16
     assert reserve(tokens=-1) == -1 and reserve(pool=_pool(block=10)) == -1 and reserve(cu=None) == -1
