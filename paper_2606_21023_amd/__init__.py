@@ -810,6 +810,13 @@ def _kv_ints_new(pool, n):
     return like.new_empty(n) if type(like) is torch.Tensor else torch.empty(n, dtype=torch.int32, device=pool.device)
 
 
+def _count(t, name):
+    try:
+        return len(t)
+    except TypeError:
+        raise HealError("%s must be an int32 CUDA vector" % name) from None
+
+
 def _kv_scratch(pool, size):
     """size bytes of workspace beside the pool, or None."""
     return _kv_ints_new(pool, (size + 3) // 4) if size > 0 else None
@@ -829,7 +836,7 @@ def heal_kv_fork(pool, table, lens, parents, children):
     whose child is a parent too, or the child of an earlier pair, is left out."""
     rows, ld, cols = _kv_pool(pool, table)
     at = _kv_list(pool, lens, "lens", rows)
-    pairs = len(parents)
+    pairs = _count(parents, "parents")
     _check((_lib or lib()).heal_kv_fork(
         pool._ref, rows, at, table.data_ptr(), ld, cols, pairs, _kv_list(pool, parents, "parents", pairs),
         _kv_list(pool, children, "children", pairs), _stream()), "heal_kv_fork")
@@ -894,8 +901,10 @@ def heal_kv_copy(cache, blocks=None, slots=None, count=None):
     def pairs(lists, name):
         if lists is None:
             return 0, None, None
+        if not isinstance(lists, (tuple, list)) or len(lists) != 2:
+            raise HealError("%s must be a pair of int32 CUDA vectors" % name)
         src, dst = lists
-        n = len(src)
+        n = _count(src, name + "[0]")
         return n, _kv_list(cache, src, name + "[0]", n), _kv_list(cache, dst, name + "[1]", n)
     n_blocks, b_src, b_dst = pairs(blocks, "blocks")
     n_slots, s_src, s_dst = pairs(slots, "slots")
@@ -1092,7 +1101,7 @@ def heal_lora_add(y, x, bank, ids, cu=None, out=None):
         o_shape, o_ld = _lora_rows(bank, out, "out", bank.N)
         if o_shape[0] != tokens:
             raise HealError("out has shape %s, expected %s" % (tuple(o_shape), tuple(y_shape)))
-    seqs = len(ids)
+    seqs = _count(ids, "ids")
     ids = _kv_list(bank, ids, "ids", seqs)
     if cu is not None:
         cu = _kv_list(bank, cu, "cu", seqs + 1)

@@ -357,7 +357,7 @@ __device__ __forceinline__ void up(const LoraArgs &a, const Group &un, const int
         const int count = min(un.count - m0, 16 * MB * halves);   // rows in LDS
         if (m0 > 0) __syncthreads();
         auto stage = [&] {
-            constexpr int PARTS = MB == 1 ? 4 : 2;
+            constexpr int PARTS = MB == 1 ? 8 : 4;
 #pragma unroll 1
             for (int i = threadIdx.x; i < count * 4 * q_end; i += 64 * kUpWaves) {
                 const int m = i / (4 * q_end), j = i - m * 4 * q_end;

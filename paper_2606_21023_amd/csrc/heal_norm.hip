@@ -145,8 +145,8 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) norm_kernel(NormArgs a, int
 {
     typedef Line<T, U, VEC> L;
     __shared__ double part[2][T > 64 ? 2 * T / 64 : 1];
-    const int32_t r = row0 + (T < 256 ? blockIdx.x * (256 / T) + threadIdx.x / T : blockIdx.x);
-    if (T < 256 && r >= a.rows) return;   // (T > 64: never)
+    const int32_t r = (int32_t)((uint32_t)row0 + (T < 256 ? blockIdx.x * (256 / T) + threadIdx.x / T : blockIdx.x));
+    if (T < 256 && (uint32_t)r >= (uint32_t)a.rows) return;   // (the last workgroup's may lie past 2^31)
     const Row p = row_of(a, r);
     float h[U][4], w[U][4], b[U][4] = {};
     L::load(p.h, a.dim, h);
@@ -271,7 +271,7 @@ hipError_t launch(const NormArgs &a, hipStream_t stream)
         const dim3 grid((unsigned)n), block(T < 256 ? 256 : T);
         if (a.vec)
             norm_kernel<T, U, true><<<grid, block, 0, stream>>>(a, (int32_t)r);
-        else
+        else if constexpr (U <= 4)   // (longer rows by elements: norm_any_kernel; their registers spilled here)
             norm_kernel<T, U, false><<<grid, block, 0, stream>>>(a, (int32_t)r);
         const hipError_t err = hipGetLastError();
         if (err != hipSuccess) return err;
@@ -292,7 +292,7 @@ hipError_t launch_block_norm(const NormArgs &a, hipStream_t stream)
     if (a.dim <= 2048) return launch<256, 2>(a, stream);
     if (a.dim <= 4096) return launch<256, 4>(a, stream);
     if (a.dim <= 8192) return launch<512, 4>(a, stream);
-    if (a.dim <= 16384) return launch<512, 8>(a, stream);
+    if (a.dim <= 16384 && a.vec) return launch<512, 8>(a, stream);
     for (int32_t r = 0; r < a.rows;) {
         const int32_t n = a.rows - r < (1 << 21) ? a.rows - r : 1 << 21;
         norm_any_kernel<<<dim3((unsigned)n), dim3(kMaxThreads), 0, stream>>>(a, r);

@@ -299,6 +299,20 @@ def test_copy_of_more_units_than_workgroups():
     check_copy(cache, blocks=(order[:1500].tolist(), order[1500:].tolist()))
 
 
+def test_copy_of_blocks_past_32_bits():
+    cache = heal.KVCache.empty(36000, 2, 8, 128, 64)   # 2.4 GB of codes of each kind, 64 KiB a block
+    last = 35999
+    assert cache.k_codes.numel() > 1 << 31
+    for name in ARRAYS[:4]:
+        t = getattr(cache, name)
+        t[1].copy_(torch.randint(-99, 99, t[1].shape, device="cuda"))
+        t[last].zero_()
+    heal.heal_kv_copy(cache, blocks=(ints([1]), ints([last])))
+    for name in ARRAYS[:4]:
+        t = getattr(cache, name)
+        assert torch.equal(t[1], t[last]) and t[last].any()
+
+
 # ---- refusals that need tensors ----------------------------------------------------
 
 def test_tensors_that_do_not_fit_are_refused():
@@ -312,7 +326,8 @@ def test_tensors_that_do_not_fit_are_refused():
               lambda: heal.heal_kv_reserve(pool, 3, t, n, cu=three), lambda: heal.heal_kv_reserve(pool, 3, t, n, missing=two),
               lambda: heal.heal_kv_compact(pool, t, src=ints([0] * 4)), lambda: heal.heal_kv_compact(pool, t, count=two),
               lambda: heal.heal_kv_copy(cache, blocks=(two, three)), lambda: heal.heal_kv_copy(cache, slots=(two, two.cpu())),
-              lambda: heal.heal_kv_copy(cache, count=ints([1])), lambda: heal.heal_kv_copy(cache, blocks=(two, two), count=two),
+              lambda: heal.heal_kv_copy(cache, count=ints([1])), lambda: heal.heal_kv_copy(cache, blocks=two),
+              lambda: heal.heal_kv_copy(cache, slots=(None, two)), lambda: heal.heal_kv_fork(pool, t, n, None, None), lambda: heal.heal_kv_copy(cache, blocks=(two, two), count=two),
               lambda: heal.KVPool(ints([0] * 8)[::2], 16), lambda: heal.KVPool(ints([0] * 8), 17),
               lambda: heal.KVPool(ints([]), 16), lambda: setattr(pool, "refs", n), lambda: delattr(pool, "block")):
         with pytest.raises(heal.HealError):

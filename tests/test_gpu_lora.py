@@ -138,6 +138,21 @@ def test_batches(place):
     check(bank, [4] + some(300) + [4, 5], [3] + [0] * 300 + [300, 2], place=place)
 
 
+def test_adapters_past_32_bits():
+    """The last adapter lies 2^31 elements into the bank and more."""
+    N, rank = 1 << 22, 128
+    a, b = torch.randn(6, rank, 64, device="cuda").bfloat16(), torch.empty((6, N, rank), dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 1, 4095, N // 2, N - 2, N - 1], device="cuda")
+    b[5] = 1.0
+    b[5, at] = torch.randn(6, rank, device="cuda").bfloat16()
+    x, y = torch.randn(3, 64, device="cuda"), torch.randn(3, N, device="cuda")
+    got = heal.heal_lora_add(y, x, heal.LoraBank(a, b), ints([5, -1, 5]))
+    small = heal.LoraBank(a, b[:, at].contiguous())
+    want, limit = reference(y[:, at], x, small, [5, -1, 5])
+    assert np.all(np.abs(got[:, at].double().cpu().numpy() - want) <= limit)
+    assert torch.equal(got[1], y[1])
+
+
 def test_no_adapter_at_all():
     bank = make(3, 16, 128, 64, torch.float32)
     check(bank, [-1, 3, 2**31 - 1, -2**31, 2], [2, 70, 3, 1, 4])   # (2 has rank 0)
@@ -241,7 +256,7 @@ def test_refusals():
               lambda: heal.heal_lora_add(y, x, bank, ids[:3]), lambda: heal.heal_lora_add(y, x, bank, ids.long()),
               lambda: heal.heal_lora_add(y, x.half(), bank, ids), lambda: heal.heal_lora_add(y, x, bank, ids, cu=ids),
               lambda: heal.heal_lora_add(y, x, bank, ids, out=y[:, :31]), lambda: heal.heal_lora_add(y, x, bank, ids, out=x[:, :32]),
-              lambda: heal.heal_lora_add(y, x, bank, ids.cpu()), lambda: heal.heal_lora_add(y, x, (a, b), ids),
+              lambda: heal.heal_lora_add(y, x, bank, ids.cpu()), lambda: heal.heal_lora_add(y, x, bank, None), lambda: heal.heal_lora_add(None, x, bank, ids), lambda: heal.heal_lora_add(y, x, (a, b), ids),
               lambda: heal.heal_lora_add(y, x.t(), bank, ids), lambda: heal.LoraBank(a, b.half()), lambda: heal.LoraBank(a, b[:2]),
               lambda: heal.LoraBank(a, b.transpose(1, 2)), lambda: heal.LoraBank(a[:, :, 1:], b), lambda: heal.LoraBank(a.double(), b.double()),
               lambda: heal.LoraBank(a, b, ranks=ids), lambda: heal.LoraBank(a, b, scales=ids[:3]), lambda: heal.LoraBank(a, b.cpu()),

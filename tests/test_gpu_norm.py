@@ -216,6 +216,17 @@ def test_many_rows():
     assert torch.equal(out[:, 0], out[:, 2])
 
 
+def test_rows_past_32_bits():
+    base = torch.empty(3 << 30, device="cuda")   # rows 2^30 elements apart
+    h = base.as_strided((3, 500), (1 << 30, 1))
+    h.copy_(torch.randn(3, 500, device="cuda"))
+    w = torch.rand(500, device="cuda")
+    want = heal.heal_block_norm(h.contiguous(), pre=w)[1]
+    out = base.as_strided((3, 500), (1 << 30, 1), 512)
+    heal.heal_block_norm(h, pre=w, out=out)
+    assert torch.equal(out, want)
+
+
 def test_captured_and_on_another_stream():
     torch.manual_seed(1)
     h, x, w = torch.randn(33, 4096, device="cuda"), torch.randn(33, 4096, device="cuda"), torch.rand(4096, device="cuda")
