@@ -403,6 +403,84 @@ __global__ void __launch_bounds__(kThreads) kv_moved_kernel(CompactArgs a, int64
     }
 }
 
+// All of it in one workgroup, for pools and tables that are small, the moves in LDS: one launch of
+// 3.5 us (1220 blocks) to 5.5 (3300) instead of three that take 8.5 to 11 and the
+// host 3.6 apiece.
+constexpr int kSmallPool = 8192, kSmallTable = 8192;
+
+__global__ void __launch_bounds__(kWide) kv_compact_kernel(CompactArgs a)
+{
+    constexpr int SEGMENTS = kSmallPool / kSegment;
+    __shared__ uint16_t to[kSmallPool], src[kSmallPool / 2], dst[kSmallPool / 2];
+    __shared__ int32_t part[SEGMENTS][kWide / 64], moves;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    const uint64_t lower = ((uint64_t)1 << lane) - 1;
+    int32_t refs[SEGMENTS][4], before[SEGMENTS];
+#pragma unroll
+    for (int g = 0; g < SEGMENTS; ++g) {
+        int32_t all = 0;
+        before[g] = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int32_t i = g * kSegment + threadIdx.x * 4 + j;
+            refs[g][j] = i < a.p.blocks ? a.p.refs[i] : 0;
+            const uint64_t held = __ballot(refs[g][j] > 0);
+            before[g] += __popcll(held & lower);
+            all += __popcll(held);
+        }
+        if (lane == 0) part[g][wave] = all;
+    }
+    if (threadIdx.x == 0) moves = 0;
+    __syncthreads();
+    int32_t all = 0;
+#pragma unroll
+    for (int g = 0; g < SEGMENTS; ++g) {
+        before[g] += all;
+#pragma unroll
+        for (int w = 0; w < kWide / 64; ++w) {
+            before[g] += w < wave ? part[g][w] : 0;
+            all += part[g][w];
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < SEGMENTS; ++g) {
+        int32_t n = before[g];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int32_t i = g * kSegment + threadIdx.x * 4 + j, move = all - n - 1;
+            const bool held = refs[g][j] > 0;
+            if (i >= a.p.blocks) break;
+            if (i == all) moves = all - n;
+            to[i] = held && i >= all ? (uint16_t)move : (uint16_t)0xffff;
+            if (held && i >= all) src[move] = (uint16_t)i;
+            if (!held && i < all) dst[i - n] = (uint16_t)i;
+            n += held;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int g = 0; g < SEGMENTS; ++g)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int32_t i = g * kSegment + threadIdx.x * 4 + j;
+            if (i >= a.p.blocks || to[i] == 0xffff) continue;
+            a.p.refs[dst[to[i]]] = refs[g][j];
+            a.p.refs[i] = 0;
+        }
+    for (int32_t j = threadIdx.x; j < a.p.blocks / 2; j += kWide) {
+        a.src[j] = j < moves ? src[j] : -1;
+        a.dst[j] = j < moves ? dst[j] : -1;
+    }
+    if (threadIdx.x == 0) *a.count = moves;
+    const int32_t entries = a.p.rows * a.p.cols;
+    for (int32_t e = threadIdx.x; e < entries; e += kWide) {
+        const int32_t row = e / a.p.cols;
+        int32_t *entry = a.p.table + row * a.p.table_ld + (e - row * a.p.cols);
+        const int32_t page = *entry;
+        if (is_page(a.p, page) && to[page] != 0xffff) *entry = dst[to[page]];
+    }
+}
+
 // ---- copy --------------------------------------------------------------------------
 
 constexpr int kCopyBytes = 16384;   // of one array, by a workgroup at a time
@@ -497,6 +575,10 @@ hipError_t launch_kv_compact(const KvPages &p, int32_t *src, int32_t *dst, int32
     CompactArgs a = {p, src, dst, count, static_cast<int32_t *>(workspace), nullptr, 0};
     a.held = a.to + p.blocks;
     a.segments = (int32_t)(((int64_t)p.blocks + kSegment - 1) / kSegment);
+    if (p.blocks <= kSmallPool && (int64_t)p.rows * p.cols <= kSmallTable) {
+        kv_compact_kernel<<<dim3(1), dim3(kWide), 0, stream>>>(a);
+        return hipGetLastError();
+    }
     kv_count_kernel<<<dim3((unsigned)a.segments), dim3(kWide), 0, stream>>>(a);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;

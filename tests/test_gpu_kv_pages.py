@@ -214,7 +214,7 @@ def test_reserve_in_a_large_pool():
     w.compact()
 
 
-@pytest.mark.parametrize("rows,cols,blocks", SIZES + [(3, 1100, 8191), (2, 4, 4097)])
+@pytest.mark.parametrize("rows,cols,blocks", SIZES + [(3, 1100, 8191), (2, 4, 4097), (1, 8192, 8192), (3, 2731, 8192), (2, 8, 8193)])
 @pytest.mark.parametrize("junk", [False, True])
 def test_compact(rows, cols, blocks, junk):
     w = World(rows, cols, blocks, seed=rows + 3, junk=junk, fill=0.5)
