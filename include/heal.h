@@ -505,15 +505,16 @@ int heal_kv_attention_tile(const heal_kv_cache_t *cache, const heal_kv_batch_t *
  * The pages of a cache: which sequences hold which of its blocks.
  *
  * refs[p] is the number of entries of the program's tables that hold block p; a block
- * with refs[p] <= 0 is free (counts are taken to lie above -2^30).  The calls below change refs and table together, on the
- * device, in 32-bit integers whose results do not depend on the order of the work.  A
- * model with a cache for each layer has one table and one pool for all of them, and
- * repeats the copies (heal_kv_copy) for each cache.
+ * with refs[p] <= 0 is free (counts are taken to lie above -2^30). The calls below change
+ * refs and table together, on the device, in 32-bit integers whose results do not depend
+ * on the order of the work. A model with a cache for each layer has one table and one
+ * pool for all of them, and repeats the copies (heal_kv_copy) for each cache.
  *
- * An entry outside [0, blocks) holds nothing.  refs is taken to agree with the tables;
+ * An entry outside [0, blocks) holds nothing. refs is taken to agree with the tables;
  * where it does not, the calls stay within the arrays, and which blocks are held
- * afterwards follows from the rules below as they stand.  Calls on one pool are made one after another (on one stream, or with
- * events between them).  table, refs, lens and the lists must not overlap.
+ * afterwards follows from the rules below as they stand. Calls on one pool are made one
+ * after another (on one stream, or with events between them). table, refs, lens and the
+ * lists must not overlap.
  *
  *   block   : 16, 32, 64 or 128 tokens, as the cache's;
  *   refs    : [blocks] int32 (device), cleared by the program at the beginning;
@@ -530,7 +531,7 @@ typedef struct heal_kv_pool_t {
 /*
  * heal_kv_release -- rows are cut back to lens[i] tokens: the entries behind the first
  * ceil(lens[i] / block) are given up (refs[p] - 1 for one in [0, blocks)) and become -1.
- * lens[i] = 0 frees a row.  Refused drafts need it only where their blocks are wanted
+ * lens[i] = 0 frees a row. Refused drafts need it only where their blocks are wanted
  * back.
  */
 heal_status_t heal_kv_release(const heal_kv_pool_t *pool, int64_t rows, const int32_t *lens,
@@ -540,12 +541,12 @@ heal_status_t heal_kv_release(const heal_kv_pool_t *pool, int64_t rows, const in
 /*
  * heal_kv_fork -- row children[j] becomes a copy of row parents[j]: what the child's row
  * held is given up, and the parent's first ceil(lens[parent] / block) entries are held
- * once more; the entries behind them become -1.  Both then share every block, the
- * incomplete one too: heal_kv_reserve gives whoever appends first a block of its own.
- * The FP32 rows of the parent's last two blocks have to reach the child's slot
- * (heal_kv_copy).  A pair is left out, its row unchanged, where a number is not in
- * [0, rows), where the child is among the call's parents, or the child of an earlier
- * pair of the call.
+ * once more; the entries behind them become -1. Both then share every block, the
+ * incomplete one too: heal_kv_reserve gives whoever appends first a block of its own. The
+ * FP32 rows of the parent's last two blocks have to reach the child's slot
+ * (heal_kv_copy). A pair is left out, its row unchanged, where a number is not in [0,
+ * rows), where the child is among the call's parents, or the child of an earlier pair of
+ * the call.
  *   parents, children : [pairs] int32 (device); pairs <= 65536.
  */
 heal_status_t heal_kv_fork(const heal_kv_pool_t *pool, int64_t rows, const int32_t *lens,
@@ -554,21 +555,23 @@ heal_status_t heal_kv_fork(const heal_kv_pool_t *pool, int64_t rows, const int32
 
 /*
  * heal_kv_reserve -- before heal_kv_append with the same sequences: every block that
- * their new tokens touch becomes one that its sequence alone holds.  In the order of the
+ * their new tokens touch becomes one that its sequence alone holds. In the order of the
  * sequences, and of the blocks in each:
  *   - an entry that holds a block which nothing else holds stays;
- *   - of a block whose entries are all among the touched ones of this call (as many as refs says, or
- *     more), the first keeps it;
- *   - the other entries of shared blocks, entries that hold nothing, and those whose block
- *     refs calls free, get the lowest block that was free before the call, the next one
- *     the next lowest, and so on.
+ *   - of a block whose entries are all among the touched ones of this call (as many as
+ *     refs says, or more), the first keeps it;
+ *   - the other entries of shared blocks, entries that hold nothing, and those whose
+ *     block refs calls free, get the lowest block that was free before the call, the next
+ *     one the next lowest, and so on.
  * Nothing is copied: appending makes a block that is not complete from the FP32 rows.
  * Where there are fewer free blocks than are needed, nothing is changed at all, and
- * *missing (device) is the number that lacks; it is 0 otherwise.  The tokens of such a call must not
- * be appended.  Places past table_cols blocks have no entry and take no block.
- *   batch     : seqs, tokens, cu and lens as for heal_kv_append (its table and slots
- *               are not read);
- *   workspace : heal_kv_reserve_workspace bytes, 16-byte aligned; holds nothing between calls.
+ * *missing (device) is the number that lacks; it is 0 otherwise. The tokens of such a
+ * call must not be appended. Places past table_cols blocks have no entry and take no
+ * block.
+ *   batch     : seqs, tokens, cu and lens as for heal_kv_append (its table and slots are
+ *               not read);
+ *   workspace : heal_kv_reserve_workspace bytes, 16-byte aligned; holds nothing between
+ *               calls.
  */
 heal_status_t heal_kv_reserve(const heal_kv_pool_t *pool, const heal_kv_batch_t *batch,
                               int32_t *table, int64_t table_ld, int64_t table_cols,
@@ -578,11 +581,11 @@ int64_t heal_kv_reserve_workspace(const heal_kv_pool_t *pool, const heal_kv_batc
 
 /*
  * heal_kv_compact -- the held blocks move to the front: with n blocks held, the highest
- * held block moves into the lowest hole below n, the next highest into the next, until the
- * first n are held.  refs and the tables follow (entries that hold nothing stay), and
- * src[j] -> dst[j], j < *count, lists the moves for heal_kv_copy, -1 behind them.  No block is the
- * source of one move and the destination of another.  `rows` has to cover all of the
- * program's tables.
+ * held block moves into the lowest hole below n, the next highest into the next, until
+ * the first n are held. refs and the tables follow (entries that hold nothing stay), and
+ * src[j] -> dst[j], j < *count, lists the moves for heal_kv_copy, -1 behind them. No
+ * block is the source of one move and the destination of another. `rows` has to cover all
+ * of the program's tables.
  *   src, dst  : [blocks / 2] int32 each, count : [1] int32 (device), written;
  *   workspace : heal_kv_compact_workspace bytes, 16-byte aligned.
  */
@@ -593,10 +596,10 @@ heal_status_t heal_kv_compact(const heal_kv_pool_t *pool, int64_t rows, int32_t 
 int64_t heal_kv_compact_workspace(const heal_kv_pool_t *pool);
 
 /*
- * heal_kv_copy -- blocks (codes, scales and means) and slots (FP32 rows) of a cache,
- * bit for bit: block_src[j] to block_dst[j] and slot_src[j] to slot_dst[j].  A pair with a
- * number outside the cache is left out.  A destination must not be listed twice, nor
- * be a source in the same call: what it holds afterwards would be parts of each.
+ * heal_kv_copy -- blocks (codes, scales and means) and slots (FP32 rows) of a cache, bit
+ * for bit: block_src[j] to block_dst[j] and slot_src[j] to slot_dst[j]. A pair with a
+ * number outside the cache is left out. A destination must not be listed twice, nor be a
+ * source in the same call: what it holds afterwards would be parts of each.
  *   blocks, slots : lengths of the lists (device, int32), 0 with NULL lists;
  *   count         : NULL, or a device integer: only the first *count pairs of blocks.
  */
@@ -614,22 +617,22 @@ heal_status_t heal_kv_copy(const heal_kv_cache_t *cache, int64_t blocks, const i
  * with N(y; w, b, eps) = y / sqrt(mean(y^2) + eps) * w + b, or with centred = 1
  *     (y - m) / sqrt(mean((y - m)^2) + eps) * w + b,  m = mean(y).
  * h' and out are FP32, everything between is FP64: h' is rounded once, and out is the
- * norm of h' as it is rounded, rounded once.  So a row may hold any finite values (their
- * squares do not overflow), and a row's bits depend on the row alone (and on dim and the alignment of
- * the arrays).  What is not finite follows IEEE rules within its row; a row of
- * zeros with eps = 0 is no number.  (HEAL-Base keeps the hidden state, the residual and
+ * norm of h' as it is rounded, rounded once. So a row may hold any finite values (their
+ * squares do not overflow), and a row's bits depend on the row alone (and on dim and the
+ * alignment of the arrays). What is not finite follows IEEE rules within its row; a row
+ * of zeros with eps = 0 is no number. (HEAL-Base keeps the hidden state, the residual and
  * the inputs and outputs of norms in FP32: Appendix "HEAL Implementation".)
- *   rows, heads : rows * heads <= 2^31 - 1 rows of dim, at strides in elements, dim 1 .. 2^24,
- *                 the last dimension dense: a residual stream has heads = 1, the
+ *   rows, heads : rows * heads <= 2^31 - 1 rows of dim, at strides in elements, dim 1 ..
+ *                 2^24, the last dimension dense: a residual stream has heads = 1, the
  *                 heads of queries a stride of their own;
- *   x, post, gate : NULL, or the block's output, its norm and the factors of it.  A gate element is at
- *                 gate[i * gate_row + j * gate_head + c * gate_col], gate_col 0 or 1:
- *                 a stride of 0 shares one factor;
+ *   x, post, gate : NULL, or the block's output, its norm and the factors of it. A gate
+ *                   element is at gate[i * gate_row + j * gate_head + c * gate_col],
+ *                   gate_col 0 or 1: a stride of 0 shares one factor;
  *   pre, out    : both or neither;
- *   h_out       : h', or NULL; only with x.
- *   h_out may be h or x, and out may be h or x too, each at the same strides; outputs must not
- *   overlap each other or an input otherwise.  (Arrays that lie side by side in
- *   rows of one stride do not overlap.)
+ *   h_out       : h', or NULL; only with x. h_out may be h or x, and out may be h or x
+ *                 too, each at the same strides; outputs must not overlap each other or
+ *                 an input otherwise. (Arrays that lie side by side in rows of one stride
+ *                 do not overlap.)
  * ========================================================================== */
 
 typedef struct heal_norm_t {
@@ -653,24 +656,29 @@ heal_status_t heal_block_norm(int64_t rows, int64_t heads, int64_t dim,
  *
  * heal_lora_add -- out[t] = y[t] + scales[a] * B_a (A_a x[t]) for every token t, a being
  * the adapter of its sequence: ids[i] for the tokens cu[i] .. cu[i + 1] - 1 (or token i
- * with cu NULL).  y is the shared projection's output (of any product above), A_a the first ranks[a]
- * rows of a[a], B_a the first ranks[a] columns of b[a].
- * A sequence whose id is not in [0, adapters), or whose adapter has rank 0, gets out = y.
- * Tokens of no sequence are left alone, and so are their rows of out.
- * Products and sums are FP32 (weights of 16 bits are exact in it), with no atomics: the
- * sums over K run in parts that follow from K alone, so that a row's bits depend on the row and its adapter
- * only, not on the batch around it.  Ranks above ranks[a] are not read as values: they
- * may hold anything.
- *   x    : tokens (0 .. 2^24) x K FP32, row stride ldx; y, out : tokens x N, ldy, ldo.  out may be y
- *          (with ldo = ldy; rows without an adapter are then not written), and must not overlap x, y or
- *          the adapters otherwise;
- *   bank : the adapters: a [adapters][rank][K], b [adapters][N][rank], dense, of one type;
- *          ranks [adapters] int32 or NULL (rank), bounded to [0, rank];
- *          scales [adapters] FP32 or NULL (1);
- *   ids  : [seqs] int32; cu : [seqs + 1] int32, ascending within [0, tokens], or NULL with
- *          tokens = seqs.  All are read on the device;
- *   workspace : heal_lora_workspace bytes of device memory, 16-byte aligned.  It holds
- *          nothing between calls; calls that may run at the same time need one each.
+ * with cu NULL). y is the shared projection's output (of any product above), A_a the
+ * first ranks[a] rows of a[a], B_a the first ranks[a] columns of b[a]. A sequence whose
+ * id is not in [0, adapters), or whose adapter has rank 0, gets out = y. Tokens of no
+ * sequence are left alone, and so are their rows of out.
+ *
+ * Products.  An FP32 value (x, v = A x, FP32 adapters) goes to the matrix units as three
+ * bf16 parts whose sum it is, an FP16 weight as two, a bf16 weight as it is; of the parts'
+ * products those are left out that are below 2^-26 of the value's.  Sums are FP32, so the
+ * result is FP32's in accuracy.  They run in parts of K that follow from K alone, without
+ * atomics: a row's bits depend on the row, its adapter, K, N and the bank's rank and type,
+ * not on the batch around it.  A row with an element that is not finite, or of 2^128 -
+ * 2^119 and more, has no finite results where an adapter applies; other rows do not notice
+ * it.  Ranks above ranks[a] are not read as values: they may hold anything.
+ *   x    : tokens (0 .. 2^24) x K FP32, row stride ldx; y, out : tokens x N, ldy, ldo.
+ *          out may be y (with ldo = ldy; rows without an adapter are then not written),
+ *          and must not overlap x, y or the adapters otherwise;
+ *   bank : the adapters: a [adapters][rank][K], b [adapters][N][rank], dense, of one
+ *          type; ranks [adapters] int32 or NULL (rank), bounded to [0, rank]; scales
+ *          [adapters] FP32 or NULL (1);
+ *   ids  : [seqs] int32; cu : [seqs + 1] int32, ascending within [0, tokens], or NULL
+ *          with tokens = seqs. All are read on the device;
+ *   workspace : heal_lora_workspace bytes of device memory, 16-byte aligned. It holds
+ *               nothing between calls; calls that may run at the same time need one each.
  * ========================================================================== */
 
 typedef enum heal_type_t { HEAL_FP32 = 0, HEAL_BF16 = 1, HEAL_FP16 = 2 } heal_type_t;

@@ -1,7 +1,7 @@
-// The pages of a cache: which sequences hold which blocks (heal_kv_release, _fork,
-// _reserve, _compact) and copies of blocks and slots (heal_kv_copy).  Tables and counts
-// are 32-bit integers; every result follows from sums and minima of integers, so it
-// does not depend on the order in which workgroups run.
+// The pages of a cache: which sequences hold which blocks (heal_kv_release, _fork, _reserve,
+// _compact) and copies of blocks and slots (heal_kv_copy). Tables and counts are 32-bit integers;
+// every result follows from sums and minima of integers, so it does not depend on the order in
+// which workgroups run.
 #include "heal_device.h"
 #include "heal_kv.h"
 
@@ -38,8 +38,8 @@ __global__ void __launch_bounds__(kThreads) kv_release_kernel(KvPages p, int64_t
     }
 }
 
-// One pair a workgroup.  No pair's child is a parent, so the rows that are read are not
-// written by the call; and each row that is written has one pair.
+// One pair a workgroup. No pair's child is a parent, so the rows that are read are not written by
+// the call; and each row that is written has one pair.
 __global__ void __launch_bounds__(kThreads)
 kv_fork_kernel(KvPages p, const int32_t *parents, const int32_t *children, int32_t pairs)
 {
@@ -68,8 +68,8 @@ constexpr int kSmallUnits = kWide;
 constexpr int kSlots = 2 * kSmallUnits;      // of the table of their blocks
 constexpr int32_t kMark = -2147483647 - 1;   // kMark + unit: the unit keeps the block
 
-// The place of the threads with `mine` among all of the workgroup's, counted on from
-// *base (LDS, moved on); part: LDS of 2 * 16 words, halves in turn.
+// The place of the threads with `mine` among all of the workgroup's, counted on from *base (LDS,
+// moved on); part: LDS of 2 * 16 words, halves in turn.
 __device__ __forceinline__ int32_t place_of(bool mine, int32_t &base, int32_t *part)
 {
     const uint64_t all = __ballot(mine);
@@ -122,8 +122,8 @@ __device__ __forceinline__ Unit unit_of(const KvSeqs &b, int B, int32_t u, F cu)
     return Unit{i, u >= 0 && blk <= t.last && blk < b.cols ? blk : -1};
 }
 
-// The first `need` free blocks into fresh, 4096 counts a turn, the next turn's on the way; returns how many
-// there are, or more than need.
+// The first `need` free blocks into fresh, 4096 counts a turn, the next turn's on the way; returns
+// how many there are, or more than need.
 __device__ __forceinline__ int32_t find_free(const KvPages &p, int32_t need, int32_t *fresh, int32_t *part)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
@@ -172,9 +172,9 @@ __device__ __forceinline__ int32_t find_free(const KvPages &p, int32_t need, int
     return found;
 }
 
-// Up to 1024 units, one workgroup, a thread each.  The touched blocks meet in a table in LDS, which counts
-// their entries and keeps the lowest unit of each; so counts are read once and written once, and
-// nothing is written where the free blocks do not suffice.
+// Up to 1024 units, one workgroup, a thread each. The touched blocks meet in a table in LDS, which
+// counts their entries and keeps the lowest unit of each; so counts are read once and written once,
+// and nothing is written where the free blocks do not suffice.
 __global__ void __launch_bounds__(kWide) kv_reserve_kernel(KvPages p, KvSeqs b, int32_t units, int32_t *missing)
 {
     __shared__ int32_t s_cu[kSmallUnits + 1], key[kSlots], count[kSlots], first[kSlots], fresh[kSmallUnits], part[64];
@@ -224,11 +224,11 @@ __global__ void __launch_bounds__(kWide) kv_reserve_kernel(KvPages p, KvSeqs b, 
     }
 }
 
-// More units: one workgroup with its state in the workspace.  Every touched entry takes one off the count of its
-// block; where the count comes to 0 all holders are here, and the lowest unit of them marks the block as
-// kept.  So an entry needs a new block unless its unit is in the mark.  Nothing but
-// counts of touched blocks has changed by then, and they are put back if the
-// free blocks do not suffice.
+// More units: one workgroup with its state in the workspace. Every touched entry takes one off the
+// count of its block; where the count comes to 0 all holders are here, and the lowest unit of them
+// marks the block as kept. So an entry needs a new block unless its unit is in the mark. Nothing
+// but counts of touched blocks has changed by then, and they are put back if the free blocks do not
+// suffice.
 __global__ void __launch_bounds__(kWide) kv_reserve_many_kernel(KvPages p, KvSeqs b, int32_t units, int32_t *ws, int32_t *missing)
 {
     __shared__ int32_t part[64];
@@ -334,8 +334,8 @@ __global__ void __launch_bounds__(kWide) kv_count_kernel(CompactArgs a)
     if (threadIdx.x == 0) a.held[blockIdx.x] = n;
 }
 
-// The k-th held block from the back, k from 0, at or behind n is the source of move k, the k-th hole
-// below n its destination: there are as many of the one as of the other.
+// The k-th held block from the back, k from 0, at or behind n is the source of move k, the k-th
+// hole below n its destination: there are as many of the one as of the other.
 __global__ void __launch_bounds__(kWide) kv_moves_kernel(CompactArgs a)
 {
     __shared__ int32_t part[3][16];
@@ -404,8 +404,7 @@ __global__ void __launch_bounds__(kThreads) kv_moved_kernel(CompactArgs a, int64
 }
 
 // All of it in one workgroup, for pools and tables that are small, the moves in LDS: one launch of
-// 3.5 us (1220 blocks) to 5.5 (3300) instead of three that take 8.5 to 11 and the
-// host 3.6 apiece.
+// 3.5 us (1220 blocks) to 5.5 (3300) instead of three that take 8.5 to 11 and the host 3.6 apiece.
 constexpr int kSmallPool = 8192, kSmallTable = 8192;
 
 __global__ void __launch_bounds__(kWide) kv_compact_kernel(CompactArgs a)
@@ -485,8 +484,8 @@ __global__ void __launch_bounds__(kWide) kv_compact_kernel(CompactArgs a)
 
 constexpr int kCopyBytes = 16384;   // of one array, by a workgroup at a time
 
-// n pairs of entries of up to three arrays (16-byte units) and of one that goes with the
-// first part of the last one (8-byte units).
+// n pairs of entries of up to three arrays (16-byte units) and of one that goes with the first part
+// of the last one (8-byte units).
 struct CopyArgs {
     const int32_t *src, *dst, *count;
     int64_t n;

@@ -1,20 +1,21 @@
 // heal_lora_add: out[t] = y[t] + s B (A x[t]) with the adapter of each token's sequence.
 //
 // Two kernels: v = A x in parts of K (lora_down_kernel), then the parts' sum, its product with B
-// and the sum with y (lora_up_kernel).  What must move is x, y and out once and each
-// adapter once; the products stay hidden behind that.
+// and the sum with y (lora_up_kernel). What must move is x, y and out once and each adapter once;
+// the products stay hidden behind that.
 //
-// Products.  An FP32 value is the exact sum of three bf16 parts (8 + 8 + 8 bits, each the
-// rest of the one before it rounded), an FP16 weight of two, a bf16 weight is one.  A
-// product of two values is the bf16 MFMAs of their parts i and j with i + j <= 2, up to six; the
-// others are below 2^-26 of it.  So sums are FP32's in accuracy, at 16 cycles an MFMA of 32 columns
-// (FP32 MFMA: 256 cycles, more than the memory takes from rank 64 on; and the compiler
-// does not keep the registers of their addends from being written too early).
+// Products. An FP32 value is the exact sum of three bf16 parts (8 + 8 + 8 bits, each the rest of
+// the one before it rounded), an FP16 weight of two, a bf16 weight is one. A product of two values
+// is the bf16 MFMAs of their parts i and j with i + j <= 2, up to six; the others are below 2^-26
+// of it. So sums are FP32's in accuracy, at 96 cycles for 32 columns of a 16 x 16 block. (FP32
+// matrix instructions take 256, more than the memory does from rank 64 on; and as built by this
+// compiler registers that one still reads as its addend were cleared: every fourth column of a
+// first form was wrong at rank 64.)
 //
-// Tiles.  A workgroup has a tile of 64 tokens, finds the adapter of each, and takes the
-// tile's adapters one after another (or every n-th, where n workgroups share the tile), the
-// rows of each packed into blocks of 16.  So a decode step reads an adapter once for 64
-// tokens, whatever their order, and a prompt fills its tiles.
+// Tiles. A workgroup has a tile of 64 tokens, finds the adapter of each, and takes the tile's
+// adapters one after another (or every n-th, where n workgroups share the tile), the rows of each
+// packed into blocks of 16. So a decode step reads an adapter once for 64 tokens, whatever their
+// order, and a prompt fills its tiles.
 #include <string.h>
 
 #include <algorithm>
@@ -27,14 +28,16 @@ namespace heal {
 
 namespace {
 
-constexpr int kTile = 64;                 // tokens of a unit
+constexpr int kTile = 64;                 // tokens
 constexpr int kDownWaves = 4, kUpWaves = 4;
 constexpr int kGroup = 128;               // ranks that a workgroup of the first kernel takes
-// Strips of the second kernel are as narrow as this many workgroups allow: 5094 tokens of 4096 columns 44 us
-// (512: 63), 64 tokens with 24 adapters at 14336 columns 15 us (512: 32, 1024: 19).
+// Strips of the second kernel are as narrow as this many workgroups allow: 5094 tokens of 4096
+// columns 44 us (512 workgroups: 63), 64 tokens with 24 adapters at 14336 columns 15 us (512: 32,
+// 1024: 19).
 constexpr int64_t kUpWorkgroups = 2048;
 
-// Depth of a part of K, whole 32s for each wave; 16 parts at most.
+// Depth of a part of K, whole 32s for each wave; 16 parts at most (every workgroup of the second
+// kernel reads them all). It follows from K alone, and so does the order of the sums.
 __host__ __device__ inline int64_t part_depth(int64_t K)
 {
     int64_t d = 512;
@@ -108,10 +111,10 @@ __device__ __forceinline__ int32_t rank_of(const LoraArgs &a, int32_t id)
     return __builtin_amdgcn_readfirstlane(min(max(rank, 0), a.rank));
 }
 
-// What a lane (row fr, place fg) has of 32 columns: of FP32 adapters' products the four from 4 fg on and the
-// four 16 further on, so that the four lanes of a row ask for 64 bytes of it in one piece (32 bytes a
-// lane side by side asked for every line twice); of 16-bit ones' the eight from 8 fg on, 16 bytes.
-// Rows may begin at any element: the loads need no alignment.
+// What a lane (row fr, place fg) has of 32 columns: of FP32 adapters' products the four from 4 fg
+// on and the four 16 further on, so that the four lanes of a row ask for 64 bytes of it in one
+// piece (32 bytes a lane side by side asked for every line twice); of 16-bit ones' the eight from 8
+// fg on, 16 bytes. Rows may begin at any element: the loads need no alignment.
 template <class T> constexpr int kNext = sizeof(T) == 4 ? 16 : 4;     // from the first four to the others
 template <class T> constexpr int kLane = sizeof(T) == 4 ? 4 : 8;      // from lane to lane
 
@@ -123,7 +126,7 @@ struct Run {
     T v[8];
 };
 
-// W: the adapters' type.  CHECK: only the first n elements from p on exist; the others are 0.
+// W: the adapters' type. CHECK: only the first n elements from p on exist; the others are 0.
 template <class W, bool CHECK, class T>
 __device__ __forceinline__ Run<T> load_run(const T *p, int64_t n = 0)
 {
@@ -204,11 +207,11 @@ __device__ __forceinline__ void products(f32x4 (&acc)[MB][NB], const Parts<3> (&
         }
 }
 
-// v of a group's rows over one part of K, 128 ranks at most.  The waves take 32 columns of the part each in
-// turn, straight from memory into operands (Run has which columns a lane takes)
-// and a turn ahead, then add their sums up in LDS, in the order of the waves.
-// MB: row blocks, from row m0 of the group on.  Of one row block the weights are most of what is read, and all
-// are a turn ahead; of more, the rows.
+// v of a group's rows over one part of K, 128 ranks at most. The waves take 32 columns of the part
+// each in turn, straight from memory into operands (Run has which columns a lane takes) and a turn
+// ahead, then add their sums up in LDS, in the order of the waves. MB: row blocks, from row m0 of
+// the group on. Of one row block the weights are most of what is read, and all are a turn ahead; of
+// more, the rows.
 template <class T, int NB, int MB>
 __device__ __forceinline__ void down(const LoraArgs &a, const Group &un, int m0, int64_t depth, f32x4 (*part)[4][64])
 {
@@ -332,12 +335,11 @@ __global__ void __launch_bounds__(64 * kDownWaves, NB == 1 ? 3 : 2) lora_down_ke
     });
 }
 
-// out = y + s B v for a group's rows and a strip of columns.  The parts of v are added up in
-// their order and split into LDS; then a wave takes 32 columns (as the rows of the
-// matrix instruction, so that a lane ends up with four columns of a token) and MB row blocks at a
-// time, y a turn ahead.
-// Of more than 32 rows each half has waves of its own.  QB: blocks of 32 ranks, or
-// 0 for ranks above 128, which take 16 rows at a time.
+// out = y + s B v for a group's rows and a strip of columns. The parts of v are added up in their
+// order and split into LDS; then a wave takes 32 columns (as the rows of the matrix instruction, so
+// that a lane ends up with four columns of a token) and MB row blocks at a time, y a turn ahead. Of
+// more than 32 rows each half has waves of its own. QB: blocks of 32 ranks, or 0 for ranks above
+// 128, which take 16 rows at a time.
 template <class T, int QB, int MB>
 __device__ __forceinline__ void up(const LoraArgs &a, const Group &un, const int32_t *rows, u32x4 *vs, int32_t rank,
                                    int32_t parts, int32_t strip, int32_t col)
@@ -387,9 +389,9 @@ __device__ __forceinline__ void up(const LoraArgs &a, const Group &un, const int
             }
             __syncthreads();
         };
-        // Results leave the matrix instructions with 16 rows of 64 bytes; whole_lines turns two of them into
-        // 8 rows of 128 bytes, whole lines (half lines: 1.4 times the bytes written).  Those rows of
-        // y and out, and the row of vs
+        // Results leave the matrix instructions with 16 rows of 64 bytes; whole_lines turns two of
+        // them into 8 rows of 128 bytes, whole lines (half lines: 1.4 times the bytes written).
+        // Those rows of y and out, and the row of vs
         int64_t row[MB][2];
         bool is[MB][2];
         int at[MB];
@@ -409,7 +411,8 @@ __device__ __forceinline__ void up(const LoraArgs &a, const Group &un, const int
         struct Out {
             float v[MB][2][4];
         };
-        // 32 columns, and where ranks are no whole fours not the last: their loads run on into the next row
+        // 32 columns, and where ranks are no whole fours not the last: their loads run on into the
+        // next row
         auto is_whole = [&](int32_t n0) { return n0 + 32 <= N - (a.rank % 4 != 0); };
         // (what the adapter lacks may be anything, up to the array's ranks in whole fours)
         auto load_w = [&](Run<T> (&w)[2], int32_t n0, int q, auto whole) {
@@ -571,8 +574,8 @@ lora_up_kernel(LoraArgs a, int64_t wg0, int32_t share, int32_t parts, int32_t st
     });
 }
 
-// Workgroups that share a tile: as many as adapters can meet there where there are few tiles (64 tokens that
-// decode); one where there are many (prompts, with one adapter a tile as a rule).
+// Workgroups that share a tile: as many as adapters can meet there where there are few tiles (64
+// tokens that decode); one where there are many (prompts, with one adapter a tile as a rule).
 int64_t shares(const LoraArgs &a)
 {
     const int64_t tiles = (a.tokens + kTile - 1) / kTile;

@@ -1,10 +1,9 @@
 // heal_block_norm: the residual stream between two blocks of a layer,
 //     u = N(x; post),  h' = h + scale * gate * u,  out = N(h'; pre),
-// one pass over the data: 4 bytes read for each element of h, x and a full gate, 4
-// written for each of h' and out, so it is bound by HBM.  Statistics and elements
-// are FP64 between the FP32 ends: a row needs no scaling against overflow, results
-// are rounded once, and at four or five streams of 4 bytes an element the FP64
-// instructions stay hidden.
+// one pass over the data: 4 bytes read for each element of h, x and a full gate, 4 written for each
+// of h' and out, so it is bound by HBM. Statistics and elements are FP64 between the FP32 ends: a
+// row needs no scaling against overflow, results are rounded once, and at four or five streams of 4
+// bytes an element the FP64 instructions stay hidden.
 #include "heal_device.h"
 #include "heal_layer.h"
 
@@ -18,8 +17,8 @@ struct Stats {
     double shift, inv;
 };
 
-// Sums s and q over the T threads of a row, in an order that follows from T alone; every
-// thread gets both.  part: LDS of 2 doubles for each wave, its own for each call.
+// Sums s and q over the T threads of a row, in an order that follows from T alone; every thread
+// gets both. part: LDS of 2 doubles for each wave, its own for each call.
 template <int T>
 __device__ __forceinline__ void row_sums(double &s, double &q, bool two, double *part)
 {
@@ -44,9 +43,9 @@ __device__ __forceinline__ void row_sums(double &s, double &q, bool two, double 
     }
 }
 
-// Mean square (about the mean where centred) of a row from the sums of its elements' differences from
-// `pivot`, one of its elements: the sum's square is at most dim times the sum of
-// squares about the mean, so their difference keeps 52 - log2(dim) bits.
+// Mean square (about the mean where centred) of a row from the sums of its elements' differences
+// from `pivot`, one of its elements: the sum's square is at most dim times the sum of squares about
+// the mean, so their difference keeps 52 - log2(dim) bits.
 __device__ __forceinline__ Stats stats(const Norm &n, int dim, double pivot, double s, double q)
 {
     const double mean = n.centred ? s / dim : 0.0;
@@ -79,9 +78,9 @@ __device__ __forceinline__ double normed(const Norm &n, const Stats &st, float y
     return n.bias ? v + (double)n.bias[c] : v;
 }
 
-// T threads a row, U times four columns of it each, all of the row in registers between the sums and the
-// stores: every stream is read once and written once.  With VEC the four columns lie side by side in 16
-// bytes; else (rows of other lengths or alignment) T apart.
+// T threads a row, U times four columns of it each, all of the row in registers between the sums
+// and the stores: every stream is read once and written once. With VEC the four columns lie side by
+// side in 16 bytes; else (rows of other lengths or alignment) T apart.
 template <int T, int U, bool VEC>
 struct Line {
     static __device__ __forceinline__ int column(int u, int e)
@@ -219,7 +218,8 @@ __device__ __forceinline__ float added(const NormArgs &a, const Row &p, const St
     return (float)((double)h + f * u);
 }
 
-// Rows of any length: one workgroup a row, which reads it once for each of its sums and once to write.
+// Rows of any length: one workgroup a row, which reads it once for each of its sums and once to
+// write.
 __global__ void __launch_bounds__(kMaxThreads)
 norm_any_kernel(NormArgs a, int32_t row0)
 {
