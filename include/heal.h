@@ -617,7 +617,8 @@ heal_status_t heal_kv_copy(const heal_kv_cache_t *cache, int64_t blocks, const i
  * with N(y; w, b, eps) = y / sqrt(mean(y^2) + eps) * w + b, or with centred = 1
  *     (y - m) / sqrt(mean((y - m)^2) + eps) * w + b,  m = mean(y).
  * h' and out are FP32, everything between is FP64: h' is rounded once, and out is the
- * norm of h' as it is rounded, rounded once. So a row may hold any finite values (their
+ * norm of h' as it is rounded, rounded once (beside FP64's errors, which for elements
+ * near the mean are in relation to the row's first element). So a row may hold any finite values (their
  * squares do not overflow), and a row's bits depend on the row alone (and on dim and the
  * alignment of the arrays). What is not finite follows IEEE rules within its row; a row
  * of zeros with eps = 0 is no number. (HEAL-Base keeps the hidden state, the residual and
@@ -662,12 +663,13 @@ heal_status_t heal_block_norm(int64_t rows, int64_t heads, int64_t dim,
  * sequence are left alone, and so are their rows of out.
  *
  * Products.  An FP32 value (x, v = A x, FP32 adapters) goes to the matrix units as three
- * bf16 parts whose sum it is, an FP16 weight as two, a bf16 weight as it is; of the parts'
- * products those are left out that are below 2^-26 of the value's.  Sums are FP32, so the
- * result is FP32's in accuracy.  They run in parts of K that follow from K alone, without
- * atomics: a row's bits depend on the row, its adapter, K, N and the bank's rank and type,
- * not on the batch around it.  A row with an element that is not finite, or of 2^128 -
- * 2^119 and more, has no finite results where an adapter applies; other rows do not notice
+ * bf16 parts whose sum it is (but for what lies below 2^-133), an FP16 weight as two, a
+ * bf16 weight as it is; of the parts' products those are left out that are below 2^-26 of
+ * the value's.  Sums are FP32, so the result is FP32's in accuracy.  They run in parts of
+ * K that follow from K alone, without atomics: a row's bits depend on the row, its
+ * adapter, K, N and the bank's rank and type, not on the batch around it.  A row with an
+ * element that is not finite, or of 2^128 - 2^119 and more, has no finite results where
+ * an adapter applies; other rows do not notice
  * it.  Ranks above ranks[a] are not read as values: they may hold anything.
  *   x    : tokens (0 .. 2^24) x K FP32, row stride ldx; y, out : tokens x N, ldy, ldo.
  *          out may be y (with ldo = ldy; rows without an adapter are then not written),

@@ -201,6 +201,27 @@ def test_what_is_not_finite_stays_in_its_row():
     assert torch.equal(heal.heal_lora_add(y, x, bank, ids)[fine], want[fine])
 
 
+@pytest.mark.parametrize("type_", list(TYPES))
+@pytest.mark.parametrize("power", [-125, -118, -100, -60, 60, 100])
+def test_magnitudes(power, type_):
+    """Parts end at bf16's smallest step 2^-133, so an element of x or of v is off by 2^-134 or less, and
+    FP32's products and sums by 2^-150 each."""
+    bank = make(3, 20, 300, 70, TYPES[type_], seed=power + 200)
+    torch.manual_seed(power + 200)
+    x, y = torch.randn(40, 300, device="cuda") * 2.0 ** power, torch.randn(40, 70, device="cuda") * 2.0 ** power
+    ids = [i % 4 - 1 for i in range(40)]
+    got = heal.heal_lora_add(y, x, bank, ints(ids)).double().cpu().numpy()
+    want, limit = reference(y, x, bank, ids)
+    for t, i in enumerate(ids):
+        if i < 0:
+            continue
+        r, s = bank.ranks[i].item(), abs(float(bank.scales[i]))
+        A, B = np.abs(bank.a[i, :r].double().cpu().numpy()), np.abs(bank.b[i, :, :r].double().cpu().numpy())
+        off = 2.0 ** -134 * A.sum(1) + 6 * 300 * 2.0 ** -150 + 2.0 ** -134
+        limit[t] += s * (B @ off + 6 * 20 * 2.0 ** -150)
+    assert np.all(np.abs(got - want) <= limit)
+
+
 def test_captured():
     """Two graphs that share nothing but the bank, replayed with other requests."""
     bank = make(6, 24, 1030, 520, torch.bfloat16)

@@ -18,13 +18,15 @@ pytestmark = [pytest.mark.gpu, needs_gpu]
 
 
 def normed(y, weight, bias, eps, centred):
-    """(value, sum of the magnitudes that make it up) in 64 bits."""
+    """(value, sum of the magnitudes that make it up) in 64 bits.  Where y is near the mean those are not
+    the value's: the mean is a sum about the row's first element, rounded in relation to that."""
     y = y.astype(np.float64)
     d = y - y.mean(-1, keepdims=True) if centred else y
     with np.errstate(all="ignore"):
-        v = d / np.sqrt((d * d).mean(-1, keepdims=True) + np.float64(np.float32(eps))) * weight.astype(np.float64)
+        f = weight.astype(np.float64) / np.sqrt((d * d).mean(-1, keepdims=True) + np.float64(np.float32(eps)))
+        terms = (np.abs(y) + np.abs(y[..., :1]) if centred else np.abs(y)) * np.abs(f)
     b = 0.0 if bias is None else bias.astype(np.float64)
-    return v + b, np.abs(v) + np.abs(b)
+    return d * f + b, terms + np.abs(b)
 
 
 def close(got, want, terms, n, what):
