@@ -618,10 +618,10 @@ heal_status_t heal_kv_copy(const heal_kv_cache_t *cache, int64_t blocks, const i
  *     (y - m) / sqrt(mean((y - m)^2) + eps) * w + b,  m = mean(y).
  * h' and out are FP32, everything between is FP64: h' is rounded once, and out is the
  * norm of h' as it is rounded, rounded once (beside FP64's errors, which for elements
- * near the mean are in relation to the row's first element). So a row may hold any finite values (their
- * squares do not overflow), and a row's bits depend on the row alone (and on dim and the
- * alignment of the arrays). What is not finite follows IEEE rules within its row; a row
- * of zeros with eps = 0 is no number. (HEAL-Base keeps the hidden state, the residual and
+ * near the mean are in relation to the row's first element). So a row may hold any finite
+ * values (their squares do not overflow), and a row's bits depend on the row, its gate
+ * and the norms alone. What is not finite follows IEEE rules within its row; a row of
+ * zeros with eps = 0 is no number. (HEAL-Base keeps the hidden state, the residual and
  * the inputs and outputs of norms in FP32: Appendix "HEAL Implementation".)
  *   rows, heads : rows * heads <= 2^31 - 1 rows of dim, at strides in elements, dim 1 ..
  *                 2^24, the last dimension dense: a residual stream has heads = 1, the

@@ -919,12 +919,6 @@ heal_status_t heal_block_norm(int64_t rows, int64_t heads, int64_t dim, const fl
     a.out = out;
     a.out_row = outs[1].row;
     a.out_head = outs[1].head;
-    a.vec = dim % 4 == 0;
-    for (const Rows *r : {&ins[0], &ins[1], &outs[0], &outs[1]})
-        if (r->at && !(aligned16(r->at) && r->row % 4 == 0 && r->head % 4 == 0)) a.vec = 0;
-    if (gate && gate_col && !(aligned16(gate) && ins[2].row % 4 == 0 && ins[2].head % 4 == 0)) a.vec = 0;
-    for (const heal_norm_t *n : {post, pre})
-        if (n && !(aligned16(n->weight) && aligned16(n->bias))) a.vec = 0;
     return heal::launch_block_norm(a, stream) == hipSuccess ? HEAL_OK : HEAL_ERR_LAUNCH;
 }
 

@@ -28,7 +28,6 @@ struct NormArgs {
     int64_t ho_row, ho_head;
     float *out;
     int64_t out_row, out_head;
-    int vec;                     // 16-byte rows of all arrays that are read or written by rows
 };
 
 hipError_t launch_block_norm(const NormArgs &a, hipStream_t stream);

@@ -78,28 +78,22 @@ __device__ __forceinline__ double normed(const Norm &n, const Stats &st, float y
     return n.bias ? v + (double)n.bias[c] : v;
 }
 
-// T threads a row, U times four columns of it each, all of the row in registers between the sums
-// and the stores: every stream is read once and written once. With VEC the four columns lie side by
-// side in 16 bytes; else (rows of other lengths or alignment) T apart.
-template <int T, int U, bool VEC>
+// T threads a row, U times four columns of it each, side by side; all of the row in registers
+// between the sums and the stores: every stream is read once and written once. Rows may begin at
+// any element: the 16-byte loads and stores need no alignment, and only a row's end is cut.
+template <int T, int U>
 struct Line {
-    static __device__ __forceinline__ int column(int u, int e)
-    {
-        const int t = threadIdx.x % T;
-        return VEC ? (u * T + t) * 4 + e : (u * 4 + e) * T + t;
-    }
+    static __device__ __forceinline__ int column(int u, int e) { return (u * T + threadIdx.x % T) * 4 + e; }
     static __device__ __forceinline__ void load(const float *p, int dim, float (&v)[U][4])
     {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (VEC) {
-                const int c = column(u, 0);
-                const f32x4 q = c < dim ? *reinterpret_cast<const f32x4 *>(p + c) : f32x4{};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[u][e] = q[e];
+            const int c = column(u, 0);
+            if (c + 4 <= dim) {
+                __builtin_memcpy(v[u], p + c, 16);
             } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[u][e] = column(u, e) < dim ? p[column(u, e)] : 0.0f;
+                for (int e = 0; e < 4; ++e) v[u][e] = c + e < dim ? p[c + e] : 0.0f;
             }
         }
     }
@@ -107,13 +101,13 @@ struct Line {
     {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (VEC) {
-                const int c = column(u, 0);
-                if (c < dim) *reinterpret_cast<f32x4 *>(p + c) = f32x4{v[u][0], v[u][1], v[u][2], v[u][3]};
+            const int c = column(u, 0);
+            if (c + 4 <= dim) {
+                __builtin_memcpy(p + c, v[u], 16);
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (column(u, e) < dim) p[column(u, e)] = v[u][e];
+                    if (c + e < dim) p[c + e] = v[u][e];
             }
         }
     }
@@ -139,10 +133,10 @@ __device__ __forceinline__ double normed(const Stats &st, float y, float w, floa
     return ((double)y - st.shift) * st.inv * (double)w + (double)b;
 }
 
-template <int T, int U, bool VEC>
+template <int T, int U>
 __global__ void __launch_bounds__(T < 256 ? 256 : T) norm_kernel(NormArgs a, int32_t row0)
 {
-    typedef Line<T, U, VEC> L;
+    typedef Line<T, U> L;
     __shared__ double part[2][T > 64 ? 2 * T / 64 : 1];
     const int32_t r = (int32_t)((uint32_t)row0 + (T < 256 ? blockIdx.x * (256 / T) + threadIdx.x / T : blockIdx.x));
     if (T < 256 && (uint32_t)r >= (uint32_t)a.rows) return;   // (the last workgroup's may lie past 2^31)
@@ -269,10 +263,7 @@ hipError_t launch(const NormArgs &a, hipStream_t stream)
     for (int64_t r = 0; r < a.rows;) {
         const int64_t left = (a.rows - r + rows - 1) / rows, n = left < (1 << 21) ? left : 1 << 21;
         const dim3 grid((unsigned)n), block(T < 256 ? 256 : T);
-        if (a.vec)
-            norm_kernel<T, U, true><<<grid, block, 0, stream>>>(a, (int32_t)r);
-        else if constexpr (U <= 4)   // (longer rows by elements: norm_any_kernel; their registers spilled here)
-            norm_kernel<T, U, false><<<grid, block, 0, stream>>>(a, (int32_t)r);
+        norm_kernel<T, U><<<grid, block, 0, stream>>>(a, (int32_t)r);
         const hipError_t err = hipGetLastError();
         if (err != hipSuccess) return err;
         r += n * rows;
@@ -292,7 +283,7 @@ hipError_t launch_block_norm(const NormArgs &a, hipStream_t stream)
     if (a.dim <= 2048) return launch<256, 2>(a, stream);
     if (a.dim <= 4096) return launch<256, 4>(a, stream);
     if (a.dim <= 8192) return launch<512, 4>(a, stream);
-    if (a.dim <= 16384 && a.vec) return launch<512, 8>(a, stream);
+    if (a.dim <= 16384) return launch<512, 8>(a, stream);
     for (int32_t r = 0; r < a.rows;) {
         const int32_t n = a.rows - r < (1 << 21) ? a.rows - r : 1 << 21;
         norm_any_kernel<<<dim3((unsigned)n), dim3(kMaxThreads), 0, stream>>>(a, r);

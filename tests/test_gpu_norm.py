@@ -127,6 +127,12 @@ def test_strides_alignment_and_places(dim):
     for a, b in ((base[:, :dim], other[:6, :dim]), (base[:, :dim], other[::2, 4:dim + 4])):
         run(a, b, **kw)
     run(base[:, 1:dim + 1], other[:6, 3:dim + 3], **kw)
+    # the same rows at other alignments: the same bits
+    for off in (1, 2, 3):
+        moved = [torch.empty(6, dim + 9, device="cuda")[:, off:off + dim] for _ in range(2)]
+        moved[0].copy_(base[:, :dim]), moved[1].copy_(other[:6, :dim])
+        got = run(*moved, **kw)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     # in place, with and without a place for h'
     h, x = base[:, :dim].contiguous(), other[:6, :dim].contiguous()
     got = run(h, x, h_out=h, out=x, **kw)
