@@ -4,6 +4,8 @@
 #include <stdint.h>
 #include <hip/hip_runtime.h>
 
+#include "heal_kv.h"
+
 namespace heal {
 
 // N(y; weight, bias): weight NULL where there is no norm.
@@ -45,8 +47,21 @@ struct LoraArgs {
     int64_t ldy;
     float *out;
     int64_t ldo;
-    float *v;                    // parts x tokens x rank
+    float *v;                    // parts x tokens x rank, in whole 16s
 };
+
+// What a lane (row fr, place fg) has of 32 columns: of FP32 adapters' products the four from 4 fg
+// on and the four 16 further on, so that the four lanes of a row ask for 64 bytes of it in one
+// piece (32 bytes a lane side by side asked for every line twice); of 16-bit ones' the eight from 8
+// fg on, 16 bytes. Rows may begin at any element: the loads need no alignment.
+template <class T> constexpr int kNext = sizeof(T) == 4 ? 16 : 4;     // from the first four to the others
+template <class T> constexpr int kLane = sizeof(T) == 4 ? 4 : 8;      // from lane to lane
+
+// Loads of B take four elements of a row at a time, so where the rank is no multiple of four they
+// run on into the rows behind it: three of them at rank 1, one otherwise. Whether they stay within
+// N rows for the 32 from n0 on (the last rows of the last adapter end with the array).
+HEAL_HD int32_t lora_rows_behind(int32_t rank) { return rank == 1 ? 3 : rank % 4 != 0; }
+HEAL_HD bool lora_whole(int32_t n0, int32_t N, int32_t rank) { return n0 + 32 <= N - lora_rows_behind(rank); }
 
 int64_t lora_workspace(int64_t tokens, int64_t rank, int64_t K);   // bytes
 hipError_t launch_lora(int type, const LoraArgs &a, hipStream_t stream);

@@ -111,13 +111,6 @@ __device__ __forceinline__ int32_t rank_of(const LoraArgs &a, int32_t id)
     return __builtin_amdgcn_readfirstlane(min(max(rank, 0), a.rank));
 }
 
-// What a lane (row fr, place fg) has of 32 columns: of FP32 adapters' products the four from 4 fg
-// on and the four 16 further on, so that the four lanes of a row ask for 64 bytes of it in one
-// piece (32 bytes a lane side by side asked for every line twice); of 16-bit ones' the eight from 8
-// fg on, 16 bytes. Rows may begin at any element: the loads need no alignment.
-template <class T> constexpr int kNext = sizeof(T) == 4 ? 16 : 4;     // from the first four to the others
-template <class T> constexpr int kLane = sizeof(T) == 4 ? 4 : 8;      // from lane to lane
-
 template <class T>
 __device__ __forceinline__ int32_t column_of(int e) { return e < 4 ? e : kNext<T> + e - 4; }
 
@@ -411,9 +404,7 @@ __device__ __forceinline__ void up(const LoraArgs &a, const Group &un, const int
         struct Out {
             float v[MB][2][4];
         };
-        // 32 columns, and where ranks are no whole fours not the last: their loads run on into the
-        // next row
-        auto is_whole = [&](int32_t n0) { return n0 + 32 <= N - (a.rank % 4 != 0); };
+        auto is_whole = [&](int32_t n0) { return lora_whole(n0, N, a.rank); };
         // (what the adapter lacks may be anything, up to the array's ranks in whole fours)
         auto load_w = [&](Run<T> (&w)[2], int32_t n0, int q, auto whole) {
             const int32_t j = 32 * q + kLane<T> * fg;
