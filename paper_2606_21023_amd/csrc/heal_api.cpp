@@ -267,14 +267,15 @@ bool kv_pool_sizes(const heal_kv_pool_t *p)
            (p->block == 16 || p->block == 32 || p->block == 64 || p->block == 128);
 }
 
+// lens: NULL where the call has none; with_lens: it reads them, whatever the table has.
 bool kv_pages(const heal_kv_pool_t *pool, int64_t rows, const int32_t *lens, int32_t *table, int64_t table_ld,
-              int64_t table_cols, heal::KvPages *p)
+              int64_t table_cols, heal::KvPages *p, bool with_lens = true)
 {
     if (!kv_pool_sizes(pool) || rows < 0 || rows > kMaxSeqs || table_cols < 0 ||
         table_cols >= ((int64_t)1 << 31) / pool->block || table_ld < (table_cols > 1 ? table_cols : 1) ||
         table_ld > kMaxStride || !aligned4(lens) || !aligned4(table))
         return false;
-    if (rows > 0 && (!lens || (table_cols > 0 && !table)) && !(lens == table && table_cols == 0)) return false;
+    if (rows > 0 && ((with_lens && !lens) || (table_cols > 0 && !table))) return false;
     *p = heal::KvPages{pool->refs, table, lens, table_ld, (int32_t)pool->blocks, (int32_t)pool->block, (int32_t)rows,
                        (int32_t)table_cols};
     return true;
@@ -820,8 +821,7 @@ heal_status_t heal_kv_compact(const heal_kv_pool_t *pool, int64_t rows, int32_t 
                               int64_t workspace_bytes, hipStream_t stream)
 {
     heal::KvPages p;
-    // (lens are not read)
-    if (!kv_pages(pool, rows, table, table, table_ld, table_cols, &p) || !count || !aligned4(count) ||
+    if (!kv_pages(pool, rows, nullptr, table, table_ld, table_cols, &p, false) || !count || !aligned4(count) ||
         (pool->blocks > 1 && (!src || !dst || !aligned4(src) || !aligned4(dst))) || !workspace ||
         !aligned16(workspace) || workspace_bytes < heal::kv_compact_bytes(pool->blocks))
         return HEAL_ERR_INVALID_VALUE;
