@@ -63,13 +63,14 @@ kv_fork_kernel(KvPages p, const int32_t *parents, const int32_t *children, int32
 
 // ---- reserve ---------------------------------------------------------------------
 
-// Units of a call that one workgroup has a thread each for, and sequences whose cu it keeps in LDS.
-constexpr int kSmallUnits = kWide;
+// Units of a call that one workgroup has a thread each for; a ragged call, of two units for each
+// sequence and more, has kSmallSeqs sequences then, whose cu are kept in LDS.
+constexpr int kSmallUnits = kWide, kSmallSeqs = kSmallUnits / 2;
 constexpr int kSlots = 2 * kSmallUnits;      // of the table of their blocks
 constexpr int32_t kMark = -2147483647 - 1;   // kMark + unit: the unit keeps the block
 
-// The place of the threads with `mine` among all of the workgroup's, counted on from *base (LDS,
-// moved on); part: LDS of 2 * 16 words, halves in turn.
+// The place of the threads with `mine` among all of the workgroup's, counted on from base, which every
+// thread has a copy of and moves on alike; part: 16 words of LDS, not those of the call before.
 __device__ __forceinline__ int32_t place_of(bool mine, int32_t &base, int32_t *part)
 {
     const uint64_t all = __ballot(mine);
@@ -177,10 +178,9 @@ __device__ __forceinline__ int32_t find_free(const KvPages &p, int32_t need, int
 // and nothing is written where the free blocks do not suffice.
 __global__ void __launch_bounds__(kWide) kv_reserve_kernel(KvPages p, KvSeqs b, int32_t units, int32_t *missing)
 {
-    __shared__ int32_t s_cu[kSmallUnits + 1], key[kSlots], count[kSlots], first[kSlots], fresh[kSmallUnits], part[64];
+    __shared__ int32_t s_cu[kSmallSeqs + 1], key[kSlots], count[kSlots], first[kSlots], fresh[kSmallUnits], part[64];
     const int32_t u = threadIdx.x;
-    const bool staged = b.cu && b.seqs <= kSmallUnits;
-    if (staged)
+    if (b.cu)
         for (int32_t i = u; i <= b.seqs; i += kWide) s_cu[i] = kv_first(b, i);
     for (int32_t i = u; i < kSlots; i += kWide) {
         key[i] = -1;
@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(kWide) kv_reserve_kernel(KvPages p, KvSeqs b, 
         first[i] = kSmallUnits;
     }
     __syncthreads();
-    auto cu = [&](int32_t i) { return staged ? s_cu[i] : kv_first(b, i); };
+    auto cu = [&](int32_t i) { return s_cu[i]; };
     Unit at = {0, -1};
     int32_t *entry = nullptr, page = -1, was = 0, slot = 0;
     if (u < units) at = unit_of(b, p.block, u, cu);
