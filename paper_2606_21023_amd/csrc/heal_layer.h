@@ -34,6 +34,20 @@ struct NormArgs {
 
 hipError_t launch_block_norm(const NormArgs &a, hipStream_t stream);
 
+// launch(first row, workgroups) for all rows, `per` of them a workgroup: 2^21 workgroups of up to 1024
+// threads at a time (a dispatch counts work-items in 32 bits).
+template <class F>
+inline hipError_t norm_launches(int32_t rows, int per, F launch)
+{
+    for (int64_t r = 0; r < rows;) {
+        const int64_t left = (rows - r + per - 1) / per, n = left < (1 << 21) ? left : 1 << 21;
+        const hipError_t err = launch((int32_t)r, (unsigned)n);
+        if (err != hipSuccess) return err;
+        r += n * per;
+    }
+    return hipSuccess;
+}
+
 struct LoraArgs {
     int32_t adapters, rank, tokens, seqs;
     int64_t K, N;

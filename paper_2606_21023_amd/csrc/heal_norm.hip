@@ -259,16 +259,10 @@ norm_any_kernel(NormArgs a, int32_t row0)
 template <int T, int U>
 hipError_t launch(const NormArgs &a, hipStream_t stream)
 {
-    constexpr int rows = T < 256 ? 256 / T : 1;   // of a workgroup
-    for (int64_t r = 0; r < a.rows;) {
-        const int64_t left = (a.rows - r + rows - 1) / rows, n = left < (1 << 21) ? left : 1 << 21;
-        const dim3 grid((unsigned)n), block(T < 256 ? 256 : T);
-        norm_kernel<T, U><<<grid, block, 0, stream>>>(a, (int32_t)r);
-        const hipError_t err = hipGetLastError();
-        if (err != hipSuccess) return err;
-        r += n * rows;
-    }
-    return hipSuccess;
+    return norm_launches(a.rows, T < 256 ? 256 / T : 1, [&](int32_t row0, unsigned n) {
+        norm_kernel<T, U><<<dim3(n), dim3(T < 256 ? 256 : T), 0, stream>>>(a, row0);
+        return hipGetLastError();
+    });
 }
 
 }  // namespace
@@ -284,14 +278,10 @@ hipError_t launch_block_norm(const NormArgs &a, hipStream_t stream)
     if (a.dim <= 4096) return launch<256, 4>(a, stream);
     if (a.dim <= 8192) return launch<512, 4>(a, stream);
     if (a.dim <= 16384) return launch<512, 8>(a, stream);
-    for (int32_t r = 0; r < a.rows;) {
-        const int32_t n = a.rows - r < (1 << 21) ? a.rows - r : 1 << 21;
-        norm_any_kernel<<<dim3((unsigned)n), dim3(kMaxThreads), 0, stream>>>(a, r);
-        const hipError_t err = hipGetLastError();
-        if (err != hipSuccess) return err;
-        r += n;
-    }
-    return hipSuccess;
+    return norm_launches(a.rows, 1, [&](int32_t row0, unsigned n) {
+        norm_any_kernel<<<dim3(n), dim3(kMaxThreads), 0, stream>>>(a, row0);
+        return hipGetLastError();
+    });
 }
 
 }  // namespace heal
