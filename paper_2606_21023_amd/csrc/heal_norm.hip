@@ -45,7 +45,7 @@ __device__ __forceinline__ void row_sums(double &s, double &q, bool two, double 
 
 // Mean square (about the mean where centred) of a row from the sums of its elements' differences
 // from `pivot`, one of its elements: the sum's square is at most dim times the sum of squares about
-// the mean, so their difference keeps 52 - log2(dim) bits.
+// the mean, so their difference keeps 52 - log2(dim) bits of what the sums have.
 __device__ __forceinline__ Stats stats(const Norm &n, int dim, double pivot, double s, double q)
 {
     const double mean = n.centred ? s / dim : 0.0;
@@ -212,36 +212,42 @@ __device__ __forceinline__ float added(const NormArgs &a, const Row &p, const St
     return (float)((double)h + f * u);
 }
 
+// Statistics of a row from y(c), column c's element. A thread's sums of dim / 1024 terms are off by as
+// many roundings, and what the mean's square takes of the squares makes that larger: a first element
+// of 10^6 before 2^24 threes cost 3.8e-6 of the result. So where it takes all but 2^-14 of them (the
+// pivot lies more than 128 deviations off, which in rows of up to 2^14 it cannot), the sums are taken
+// again about the mean.
+template <class F>
+__device__ __forceinline__ Stats stats_any(const Norm &n, int dim, double pivot, double *part, F y)
+{
+    for (int turn = 0;; ++turn) {
+        double s = 0.0, q = 0.0;
+        for (int c = threadIdx.x; c < dim; c += kMaxThreads) {
+            const double d = y(c) - pivot;
+            s += d;
+            q += d * d;
+        }
+        row_sums<kMaxThreads>(s, q, true, part + turn * (2 * kMaxThreads / 64));
+        const Stats st = stats(n, dim, pivot, s, q);
+        const double mean = s / dim, square = q / dim;
+        if (turn == 1 || !n.centred || !((square - mean * mean) * 16384.0 < square)) return st;
+        pivot = st.shift;
+    }
+}
+
 // Rows of any length: one workgroup a row, which reads it once for each of its sums and once to
 // write.
 __global__ void __launch_bounds__(kMaxThreads)
 norm_any_kernel(NormArgs a, int32_t row0)
 {
-    __shared__ double part[2][2 * kMaxThreads / 64];
+    __shared__ double part[2][2 * (2 * kMaxThreads / 64)];
     const Row p = row_of(a, row0 + blockIdx.x);
     Stats post = {0.0, 1.0}, pre = {0.0, 1.0};
-    if (p.x && a.post.weight) {
-        const double pivot = a.post.centred ? (double)p.x[0] : 0.0;
-        double s = 0.0, q = 0.0;
-        for (int c = threadIdx.x; c < a.dim; c += kMaxThreads) {
-            const double d = (double)p.x[c] - pivot;
-            s += d;
-            q += d * d;
-        }
-        row_sums<kMaxThreads>(s, q, true, part[0]);
-        post = stats(a.post, a.dim, pivot, s, q);
-    }
-    if (p.out) {
-        const double pivot = a.pre.centred ? (double)added(a, p, post, 0) : 0.0;
-        double s = 0.0, q = 0.0;
-        for (int c = threadIdx.x; c < a.dim; c += kMaxThreads) {
-            const double d = (double)added(a, p, post, c) - pivot;
-            s += d;
-            q += d * d;
-        }
-        row_sums<kMaxThreads>(s, q, true, part[1]);
-        pre = stats(a.pre, a.dim, pivot, s, q);
-    }
+    if (p.x && a.post.weight)
+        post = stats_any(a.post, a.dim, a.post.centred ? (double)p.x[0] : 0.0, part[0], [&](int c) { return (double)p.x[c]; });
+    if (p.out)
+        pre = stats_any(a.pre, a.dim, a.pre.centred ? (double)added(a, p, post, 0) : 0.0, part[1],
+                        [&](int c) { return (double)added(a, p, post, c); });
     // (an output may lie on an input: each thread reads and writes its own elements, and
     // what others read of the row, its first element, they have by now)
     for (int c = threadIdx.x; c < a.dim; c += kMaxThreads) {
