@@ -634,7 +634,8 @@ def heal_kv_append(cache, k, v, table, lens, cu=None, slots=None, cos=None, sin=
     k, v: (tokens, heads, dim) float32; table (sequences, columns), lens and slots
     (sequences), cu (sequences + 1): int32.  lens counts the new tokens.  cos, sin:
     (places, rot / 2) float32 or None.  With q (tokens, any heads, dim) the queries
-    are rotated too, into q_out (which may be q) or a new tensor, and returned.
+    are rotated too, into q_out (which may be q) or a new tensor, and returned; rows of
+    tokens of no sequence are not written.
     """
     if not isinstance(cache, KVCache):
         raise HealError("cache must be a KVCache")
@@ -684,7 +685,8 @@ def heal_kv_read(cache, tokens, table, lens, cu=None, slots=None):
 def heal_kv_select(cache, q, n_sel, table, lens, cu=None, slots=None, keep_first=1, keep_last=1, out=None):
     """(tokens, heads, n_sel) int32: for each token and key/value head the first
     keep_first and last keep_last blocks and the others that score highest,
-    ascending, -1 behind the last.  (slots is not needed; it is checked if given.)"""
+    ascending, -1 behind the last.  Rows of tokens of no sequence are not written.
+    (slots is not needed; it is checked if given.)"""
     if not isinstance(cache, KVCache):
         raise HealError("cache must be a KVCache")
     shape, q_token, q_head = _kv_rows(cache, q, "q")
@@ -722,7 +724,7 @@ def heal_kv_attention(cache, q, table, lens, cu=None, slots=None, scale=None, ca
     sel: int32 (tokens, heads, n) of ``heal_kv_select``, or None for all blocks;
     lse: a contiguous float32 (tokens, heads_q) that is written too; chunk: 0, or
     tokens summed at a time (a multiple of 64), for bits that do not depend on the
-    batch.
+    batch.  Rows of tokens of no sequence are not written, in out and in lse.
     """
     if not isinstance(cache, KVCache):
         raise HealError("cache must be a KVCache")
@@ -979,8 +981,8 @@ def heal_block_norm(h, x=None, post=None, gate=None, scale=1.0, pre=None, eps=1e
 
     h: float32 (tokens, dim) or (tokens, heads, dim); x the same, or None: then h' is h
     itself.  post, pre: weights (dim) of the norms, or None for no norm there (without
-    pre, out is None).  gate: a float32 tensor that broadcasts to h, its last dimension
-    dense, or None.  centred: norms about the mean, with biases post_bias and pre_bias where they
+    pre, out is None).  gate: a float32 tensor of as many dimensions that broadcasts to h, its
+    last dimension dense, or None.  centred: norms about the mean, with biases post_bias and pre_bias where they
     are given.  h_out (which may be h or x) and out (h or x likewise) are new tensors by default.
     """
     shape, stride = _tensor(h, "h", torch.float32)
@@ -1082,9 +1084,11 @@ def _lora_rows(bank, t, name, cols):
 def heal_lora_add(y, x, bank, ids, cu=None, out=None):
     """out = y + s B (A x) with the adapter of each token's sequence.
 
-    y (tokens, N), x (tokens, K): float32; ids (sequences) int32, -1 for none; cu
-    (sequences + 1) int32, or None where every token is a sequence.  out may be y, a new
-    tensor by default.
+    y (tokens, N), x (tokens, K): float32; ids (sequences) int32, -1 for none (out is y
+    there); cu (sequences + 1) int32, or None where every token is a sequence.  out may be
+    y, a new tensor by default.  Rows of tokens of no sequence (before cu[0], behind
+    cu[-1]) are not written: out keeps what it held, and in a new tensor they are
+    undefined; with out=y they stay y's.
     """
     if not isinstance(bank, LoraBank):
         raise HealError("bank must be a LoraBank")
