@@ -669,8 +669,8 @@ heal_status_t heal_block_norm(int64_t rows, int64_t heads, int64_t dim,
  * K that follow from K alone, without atomics: a row's bits depend on the row, its
  * adapter, K, N and the bank's rank and type, not on the batch around it.  A row with an
  * element that is not finite, or of 2^128 - 2^119 and more, has no finite results where
- * an adapter applies; other rows do not notice
- * it.  Ranks above ranks[a] are not read as values: they may hold anything.
+ * an adapter applies; other rows do not notice it.  Ranks above ranks[a] are not read as
+ * values: they may hold anything.
  *   x    : tokens (0 .. 2^24) x K FP32, row stride ldx; y, out : tokens x N, ldy, ldo.
  *          out may be y (with ldo = ldy; rows without an adapter are then not written),
  *          and must not overlap x, y or the adapters otherwise;
